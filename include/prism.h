@@ -61,6 +61,8 @@ typedef enum { PRISM_F32 = 0, PRISM_BF16 = 1 } prism_dtype;
 #define PRISM_DEVERR_CACHE_RANGE 2   /* a cache position outside [0, max_ctx) was skipped */
 #define PRISM_DEVERR_NNEW_RANGE 4    /* n_new[b] outside [1, max_new] was clamped */
 #define PRISM_DEVERR_TIMEOUT 8       /* a bounded wait expired */
+#define PRISM_DEVERR_PAGE_RANGE 16   /* paged operators: a block-table entry outside [0, n_pages) */
+#define PRISM_DEVERR_POSITION_RANGE 32 /* paged operators: a rotary position outside the table was clamped */
 
 /* Model and capacity description.  hidden = d, n_q_heads = Hq, n_kv_heads =
  * Hkv (Hq % Hkv == 0), head_dim = D (64 or 128), ffn = F, vocab = V,
@@ -468,6 +470,137 @@ prism_status prism_profile_tree(prism_ctx *ctx, int32_t batch, const int32_t *to
                                 const int32_t *n_new, const int32_t *kv_len, void *k_cache, void *v_cache,
                                 int32_t width, int32_t n_nodes, const prism_tree_outputs *out, void *stream,
                                 float *kernel_ms, int32_t *kernel_kind, int32_t max_kernels, int32_t *n_kernels);
+
+/* ------------------------------------------------------------------------
+ * Operators over a paged key-value cache: the per-head norm of queries and
+ * keys with the position rotation (stored into the cache, or dense with its
+ * gradient), the attention of one new token, and eviction by accumulated
+ * attention weight.  They need no prism_ctx.
+ *
+ * A handle fixes the head layout, the type and the page size, and owns the
+ * workspace.  One handle's calls share that workspace: keep them on one stream
+ * (or order the streams), one host thread at a time.  Calls allocate nothing,
+ * wait for nothing and can be captured into a CUDA graph.  Errors are returned
+ * as above; prism_paged_error gives the message.  Device-only conditions set
+ * the handle's own error word (prism_paged_status): a length outside the block
+ * table or a row that does not fit it (cache bit; the length is clamped, the
+ * row skipped), n_new outside [0, max_new] (clamped), a position outside the
+ * rotation table (clamped), a block-table entry outside the pool (its rows
+ * read as zeros, are not written, and the results are not to be used). */
+
+/* n_q_heads = Hq, n_kv_heads = Hkv (Hq % Hkv == 0), head_dim = D (64 or 128),
+ * dtype PRISM_BF16 or PRISM_F32 ("wtype": queries, keys, values, gains, cache).
+ * page_size >= 1 rows a page; max_batch sequences and max_pages block-table
+ * columns at most in a call with a cache.  track_weights: 1 if attention is to
+ * accumulate weights (the workspace then holds one fp32 score per query head
+ * and row).  softmax_scale: 0 means 1 / sqrt(D).  rms_eps of the norm. */
+typedef struct {
+    int32_t n_q_heads, n_kv_heads, head_dim, dtype;
+    int32_t page_size, max_batch, max_pages, track_weights;
+    float softmax_scale, rms_eps;
+} prism_paged_config;
+
+typedef struct prism_paged prism_paged;
+
+/* A paged cache.  Row `slot` of sequence b and KV head h is element
+ * page * page_stride + h * head_stride + (slot % page_size) * row_stride of
+ * k_pages and of v_pages, page = block_table[b, slot / page_size], followed by
+ * the head's other dims.  Strides in elements, the same for K and V; bases and
+ * strides multiples of 16 bytes.
+ *   weights      fp32 [n_pages, Hkv, page_size], dense, or NULL: each row's
+ *                accumulated attention weight
+ *   block_table  int32 [batch, table_pages]; entries past a sequence's rows
+ *                are not read
+ *   kv_len       int32 [batch]: rows each sequence holds
+ * Sequences may share pages that they only read; with weights every page
+ * belongs to one sequence. */
+typedef struct {
+    void *k_pages, *v_pages;
+    int64_t page_stride, head_stride, row_stride;
+    float *weights;
+    const int32_t *block_table;
+    int32_t *kv_len;
+    int32_t n_pages, table_pages, batch;
+} prism_paged_cache;
+
+/* A wtype [batch, max_new, heads, D] tensor, D dense, the other strides (in
+ * elements) any multiples of 16 bytes, so that the queries, keys and values of
+ * one fused projection, or [batch, heads, max_new, D] tensors, are taken as they
+ * are.  An output may be its own input (same strides). */
+typedef struct {
+    void *data;
+    int64_t batch_stride, row_stride, head_stride;
+} prism_heads;
+
+/* Create / destroy a handle on a device.  Errors: INVALID_ARG, CAPACITY
+ * (sizes beyond 32-bit row numbers), OOM, CUDA.  Destroying waits for the
+ * device's work; NULL is a no-op. */
+prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, prism_paged **out);
+prism_status prism_paged_destroy(prism_paged *p);
+
+/* RMSNorm of every query and key head on its own with gains g_q, g_k (wtype
+ * [D]; both NULL: no norm), then the rotate-half rotation of dims (j, j + D/2)
+ * by the angle of the row's position: row i < n_new[b] of sequence b stands at
+ * position pos[b] + i.
+ *   rope   fp32 [rope_len, 2, D/2]: cosines, then sines of each position
+ *   pos    int32 [batch]; n_new int32 [batch] or NULL (max_new rows each)
+ * Rows past n_new[b] are not written.  All arithmetic in fp32, rounded once.
+ * Errors: INVALID_ARG, SHAPE, CAPACITY (more than 2^24 rows), CUDA. */
+prism_status prism_qk_norm_rope(prism_paged *p, int32_t batch, int32_t max_new, const prism_heads *q, const prism_heads *k,
+                                const prism_heads *q_out, const prism_heads *k_out, const void *g_q, const void *g_k,
+                                const float *rope, int32_t rope_len, const int32_t *pos, const int32_t *n_new, void *stream);
+
+/* Its gradient: from dq_out, dk_out (wtype) and the forward's inputs, dq and dk
+ * (wtype; zeros past n_new[b]) and the gains' gradients dg_q, dg_k (fp32 [D],
+ * summed over rows and heads in a fixed order; NULL when there are no gains).
+ * Errors: as prism_qk_norm_rope. */
+prism_status prism_qk_norm_rope_backward(prism_paged *p, int32_t batch, int32_t max_new, const prism_heads *dq_out,
+                                         const prism_heads *dk_out, const prism_heads *q, const prism_heads *k,
+                                         const prism_heads *dq, const prism_heads *dk, const void *g_q, const void *g_k,
+                                         const float *rope, int32_t rope_len, const int32_t *pos, const int32_t *n_new,
+                                         float *dg_q, float *dg_k, void *stream);
+
+/* The same norm and rotation with the keys, and the values as they are, stored
+ * into the cache: row i < n_new[b] of sequence b goes to slot kv_len[b] + i, its
+ * weight (if the cache has weights) starts at 0.  kv_len is read, not advanced.
+ * pos NULL: rows stand at their slots (after an eviction they no longer do).
+ * Errors: as prism_qk_norm_rope, CAPACITY (batch or table beyond the handle). */
+prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, int32_t max_new, const prism_heads *q,
+                                const prism_heads *k, const prism_heads *v, const prism_heads *q_out, const void *g_q,
+                                const void *g_k, const float *rope, int32_t rope_len, const int32_t *pos,
+                                const int32_t *n_new, void *stream);
+
+/* Attention of one query row per sequence, q wtype [batch, Hq, D] (normed and
+ * rotated), over the kv_len[b] + added rows of its cache (added = 1: a row
+ * appended but not yet counted in kv_len): out wtype [batch, Hq, D], and if
+ * given lse fp32 [batch, Hq], the natural log of the sum of exponentials.  A
+ * sequence without rows gives zeros and -inf.  If the cache has weights, each
+ * row's grows by the sum of its probabilities over the KV head's query heads
+ * (needs track_weights).  Scores, probabilities and sums are fp32; the result
+ * does not depend on the order in which CTAs run.  Errors: INVALID_ARG, SHAPE,
+ * CAPACITY, CUDA. */
+prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,
+                                float *lse, void *stream);
+
+/* Eviction: of the L = kv_len[b] rows of every sequence and KV head, the
+ * min(L, budget) rows to keep go, in order, to slots 0, 1, ... of dst: the first
+ * `sinks`, the last `recent`, and between them the rows with the largest weight
+ * (ties: the lower slot; a NaN weight ranks below all).  src is left as it is;
+ * its pages can be handed back once the call has run.  dst lists other pages
+ * (of the same or of another pool), has at least min(budget, table rows of src)
+ * rows, and receives the rows' weights (if it has weights) and kv_len =
+ * min(L, budget); dst's kv_len may be src's.
+ *   kept  int32 [batch, Hkv, budget] out: the kept slots, ascending, then -1
+ * Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
+prism_status prism_paged_evict(prism_paged *p, const prism_paged_cache *src, const prism_paged_cache *dst, int32_t budget,
+                               int32_t sinks, int32_t recent, int32_t *kept, void *stream);
+
+/* Synchronise `stream`, read and clear the handle's device error word:
+ * PRISM_ERR_DEVICE_FLAG if it was set (bits in *flags if non-NULL). */
+prism_status prism_paged_status(prism_paged *p, void *stream, int32_t *flags);
+
+/* Message for the last failing call on p (or the global one when p is NULL). */
+const char *prism_paged_error(const prism_paged *p);
 
 /* Message for the last failing call on ctx (or a global message when ctx is NULL). */
 const char *prism_get_error(const prism_ctx *ctx);

@@ -13,7 +13,11 @@ import os
 
 import torch
 
-__all__ = ["Drafter", "PrismError", "library", "lm_head_topk_static", "STEP_TENSORS", "KERNEL_KINDS"]
+from . import paged
+from .paged import PagedAttention, PagedCache, rope_table
+
+__all__ = ["Drafter", "PrismError", "library", "lm_head_topk_static", "STEP_TENSORS", "KERNEL_KINDS",
+           "PagedAttention", "PagedCache", "rope_table"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.environ.get("PRISM_LIB") or os.path.join(_HERE, "libprism.so")
@@ -89,6 +93,7 @@ def library() -> ctypes.CDLL:
                   "prism_draft_round_sampled", "prism_accept_sampled", "prism_draft_tree", "prism_accept_tree",
                   "prism_profile_tree", "prism_draft_loop"):
             getattr(lib, f).restype = ctypes.c_int
+        paged.bind(lib)
         _lib = lib
     return _lib
 

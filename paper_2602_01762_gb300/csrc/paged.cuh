@@ -1,0 +1,211 @@
+// Launch interfaces and device helpers of the paged-cache operators
+// (paged_attend.cu, paged_rope.cu, paged_evict.cu; ABI in paged_api.cu).
+#pragma once
+
+#include "common.cuh"
+
+namespace prism {
+
+enum PagedErr : int {
+    kErrPage = 16,      // a block-table entry outside the pool
+    kErrPosition = 32,  // a rotary position outside the table
+};
+
+// A paged cache on the device.  Strides in bytes; row `slot` of sequence b and
+// KV head h lies in page table[b, slot / page_size] at row slot % page_size.
+struct PagedView {
+    char *k, *v;
+    long long page_stride, head_stride, row_stride;
+    float *weights;              // [n_pages, Hkv, page_size] or null
+    const int32_t *table;        // [B, table_pages]
+    int32_t *kv_len;             // [B]
+    int n_pages, table_pages, page_size;
+};
+
+// A [B, max_new, heads, D] tensor by base and byte strides (D contiguous).
+struct HeadsView {
+    char *p;
+    long long sb, st, sh;
+};
+
+struct NormRopeArgs {
+    HeadsView q, k, v, q_out, k_out;     // append: v read, k_out unused
+    PagedView cache;                     // append only
+    const void *g_q, *g_k;               // [D] wtype, or both null: no norm
+    const float *rope;                   // [rope_len, 2, D/2]: cosines, then sines
+    const int32_t *pos, *n_new;          // [B]; n_new null: max_new rows each
+    int rope_len, B, max_new, Hq, Hkv, split;
+    float eps;
+    int *err;
+};
+
+struct NormRopeGradArgs {
+    HeadsView dq_out, dk_out, q, k, dq, dk;
+    const void *g_q, *g_k;
+    const float *rope;
+    const int32_t *pos, *n_new;
+    float *dg_q, *dg_k;                  // [D] fp32 (null without gains)
+    float *part;                         // [CTAs, 2, D]
+    int *counter;                        // last-CTA ticket (left at zero)
+    int rope_len, B, max_new, Hq, Hkv, split;
+    float eps;
+    int *err;
+};
+
+struct AttendArgs {
+    PagedView cache;
+    const void *q;                       // [B, Hq, D]
+    void *out;                           // [B, Hq, D]
+    float *lse;                          // [B, Hq] or null
+    float *scores;                       // [B, Hkv, table rows, G] base-2 scores, or null
+    float2 *stat;                        // [B, Hq]: (maximum score, 1 / sum), with scores
+    float *part;                         // two pieces per CTA
+    int *counter;                        // [B * head tiles] tickets (left at zero)
+    int B, Hq, Hkv, added, min_units;
+    float scale_log2;                    // softmax scale * log2(e)
+    int *err;
+};
+
+struct EvictArgs {
+    PagedView src, dst;
+    int32_t *kept;                       // [B, Hkv, budget]
+    int B, Hkv, budget, sinks, recent;
+    int *err;
+};
+
+constexpr int kAttendUnit = 128;         // keys per unit of the attention's work split
+// Query heads that share one pass over a KV head's rows.
+int attend_head_tile(bool bf16, int G);
+size_t attend_part_floats(bool bf16, int D, int G, int sms);
+// Kernel attributes, before any capture.
+cudaError_t prepare_attend_kernels();
+cudaError_t prepare_evict_kernels();
+cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
+int norm_rope_grad_ctas(int sms);
+cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, cudaStream_t s);
+
+#ifdef __CUDACC__
+// Rows of sequence b, held to [0, table rows] (outside: the cache-range bit).
+__device__ __forceinline__ int paged_len(const PagedView &c, int b, int added, int *err) {
+    const long long n = (long long)c.kv_len[b] + added, cap = (long long)c.table_pages * c.page_size;
+    if (n >= 0 && n <= cap) return (int)n;
+    set_err(err, kErrCache);
+    return n < 0 ? 0 : (int)cap;
+}
+
+// Two floats rounded to bf16 (nearest even, NaN kept), the first in the low half.
+__device__ __forceinline__ uint32_t cvt_bf16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+
+// E values of a 16-byte vector as floats and back (E = 8 bf16 or 4 fp32).
+template <typename T> struct Vec16;
+template <> struct Vec16<uint16_t> {
+    static constexpr int E = 8;
+    static __device__ __forceinline__ void unpack(const uint4 &u, float (&f)[8]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            f[2 * i] = bf16lo(w[i]);
+            f[2 * i + 1] = bf16hi(w[i]);
+        }
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {
+        return make_uint4(cvt_bf16x2(f[0], f[1]), cvt_bf16x2(f[2], f[3]), cvt_bf16x2(f[4], f[5]), cvt_bf16x2(f[6], f[7]));
+    }
+};
+template <> struct Vec16<float> {
+    static constexpr int E = 4;
+    static __device__ __forceinline__ void unpack(const uint4 &u, float (&f)[4]) {
+        f[0] = __uint_as_float(u.x);
+        f[1] = __uint_as_float(u.y);
+        f[2] = __uint_as_float(u.z);
+        f[3] = __uint_as_float(u.w);
+    }
+    static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    }
+};
+
+// Ragged work split into equal contiguous shares.  Sequence b has blocks(b) >= 1
+// blocks of keys, each for `heads` heads; units run over (b, head, block).
+// Every CTA takes `per` units from u0 on; begin() finds the sequence of its
+// first one.  All threads of the CTA call it.
+struct UnitRange {
+    int u0, u1, per;   // this CTA's units; units per CTA
+    int b, first;      // sequence of u0 and that sequence's first unit
+};
+template <int THREADS, typename Blocks>
+__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, int min_units, const Blocks &blocks) {
+    const int tid = threadIdx.x, lane = tid & 31;
+    const int cta = blockIdx.x, ctas = gridDim.x;
+    if (B <= 32) {                       // every warp for itself
+        const int n = lane < B ? blocks(lane) : 0;
+        int s = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xFFFFFFFFu, s, o);
+            if (lane >= o) s += t;
+        }
+        const int units = __shfl_sync(0xFFFFFFFFu, s, 31) * heads;
+        r.per = max(min_units, (units + ctas - 1) / ctas);
+        if ((long long)cta * r.per >= units) return false;
+        r.u0 = cta * r.per;
+        r.u1 = min(r.u0 + r.per, units);
+        const int at = r.u0 / heads;
+        r.b = __popc(__ballot_sync(0xFFFFFFFFu, lane < B && s <= at));
+        r.first = __shfl_sync(0xFFFFFFFFu, s - n, r.b) * heads;
+        return true;
+    }
+    __shared__ int warp_sum[THREADS / 32], found[2];
+    int total = 0;
+    for (int b = tid; b < B; b += THREADS) total += blocks(b);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xFFFFFFFFu, total, o);
+    if (lane == 0) warp_sum[tid >> 5] = total;
+    __syncthreads();
+    total = 0;
+#pragma unroll
+    for (int w = 0; w < THREADS / 32; ++w) total += warp_sum[w];
+    const int units = total * heads;
+    r.per = max(min_units, (units + ctas - 1) / ctas);
+    if ((long long)cta * r.per >= units) return false;
+    r.u0 = cta * r.per;
+    r.u1 = min(r.u0 + r.per, units);
+    const int at = r.u0 / heads;
+    int before = 0;
+    for (int base = 0; base < B && before <= at; base += THREADS) {
+        const int n = base + tid < B ? blocks(base + tid) : 0;
+        int s = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xFFFFFFFFu, s, o);
+            if (lane >= o) s += t;
+        }
+        __syncthreads();                 // the sums of the step before were read
+        if (lane == 31) warp_sum[tid >> 5] = s;
+        __syncthreads();
+        int all = 0;
+#pragma unroll
+        for (int w = 0; w < THREADS / 32; ++w) {
+            if (w < (tid >> 5)) s += warp_sum[w];
+            all += warp_sum[w];
+        }
+        if (n > 0 && before + s - n <= at && at < before + s) {
+            found[0] = base + tid;
+            found[1] = before + s - n;
+        }
+        before += all;
+    }
+    __syncthreads();
+    r.b = found[0];
+    r.first = found[1] * heads;
+    return true;
+}
+#endif
+
+}  // namespace prism

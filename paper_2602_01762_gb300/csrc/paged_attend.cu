@@ -1,0 +1,663 @@
+// Attention of one new token per sequence over a paged key-value cache.
+//
+//   z_j = scale * q_h . k_j,  p_j = exp(z_j) / sum_i exp(z_i),  out_h = sum_j p_j v_j
+//
+// over the rows j < kv_len[b] + added of sequence b, for the G = Hq / Hkv query
+// heads h of each KV head; optionally lse_h = log sum_j exp(z_j), and the
+// accumulated weights w_j += sum_h p_j that eviction ranks by.
+//
+// Bound by the bytes of K and V, read once: 4 D bytes per row and KV head in bf16
+// against 4 G D operations.
+#include "paged.cuh"
+
+namespace prism {
+namespace {
+
+constexpr int kPaWarps = 4;
+constexpr int kPaThreads = 32 * kPaWarps;
+constexpr int kPaStage = 8192;           // bytes of one warp's stage: KT rows of K, then of V
+constexpr int kPaCtasPerSm = 2;
+constexpr float kLn2 = 0.693147180559945309f;
+
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
+    const int n = ok ? 16 : 0;           // 0: the 16 bytes are zero-filled, nothing is read
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+
+__device__ __forceinline__ void lds_x4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void lds_x4_t(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0, %1, %2, %3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {
+    uint32_t y;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
+    return y;
+}
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
+                 "{%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+
+// The maximum to subtract: 0 where no score is above -inf (every exp2 is then 0).
+__device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
+
+// bf16 rows on warp-level tensor-core products, keys in the 16-row dimension M
+// and the query heads in the 8-column dimension N, so that G <= 8 heads share one
+// tile:
+//   S^T[key][h] = K[key][:] . q[h][:]        A = 16 rows of K, B = q^T in registers
+//   O^T[d][h]  += V^T[d][keys] P^T[keys][h]  A = V^T (transposing load), B = P^T
+// q and K enter exactly.  P is split into two bf16 parts, P = hi + lo to 2^-17,
+// so that what the result loses is its own rounding: kPacked (G <= 4) holds the
+// four heads' hi in columns 0-3 and lo in columns 4-7 of one product, the wider
+// forms take two products.  Per warp and tile of 16 keys: 8 + 8 products of
+// 16x8x16 at D = 128 (kPacked), far below the tensor pipe's rate at the speed
+// rows arrive.
+enum HeadMode : int { kPacked = 0, kEight = 1, kSixteen = 2 };
+template <int D_, int MODE> struct Bf16Tile {
+    using T = uint16_t;
+    static constexpr int D = D_, KT = kPaStage / (4 * D), NT = MODE == kSixteen ? 2 : 1;
+    static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
+    static constexpr int kMergeStride = D + 4;
+    static constexpr int kStages = MODE == kSixteen ? 2 : 3;
+    uint32_t qf[D / 16][NT][2];
+    float m[NT][2], l[NT][2], o[D / 16][NT][4];
+
+    // Shared address of 16-byte piece c of row r: pieces exchanged by row, so that
+    // eight rows of one piece lie in different banks.
+    static __device__ __forceinline__ uint32_t piece(int r, int c) {
+        return (uint32_t)(r * (2 * D) + ((c ^ (r & 7)) << 4));
+    }
+    __device__ __forceinline__ void load_q(const T *q, int heads) {
+        const int lane = threadIdx.x & 31, n = lane >> 2;
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            const int h = MODE == kPacked ? (n & 3) : n + 8 * t;
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k)
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+                    qf[k][t][u] = h < heads ? *(const uint32_t *)(q + h * D + 16 * k + 8 * u + 2 * (lane & 3)) : 0u;
+        }
+    }
+    __device__ __forceinline__ void reset() {
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+            m[t][0] = m[t][1] = -INFINITY;
+            l[t][0] = l[t][1] = 0.f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) o[d][t][i] = 0.f;
+        }
+    }
+    // One stage: rows key0 .. key0 + KT - 1, of which those below len count.
+    __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, float *, int key0, int len, float scale, float *scores, int heads) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, c = 2 * (lane & 3);
+#pragma unroll
+        for (int sub = 0; sub < KT / 16; ++sub) {
+            const int base = key0 + 16 * sub;
+            if (sub > 0 && base >= len) break;
+            float s[NT][4];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+            const int kr = 16 * sub + (lane & 15);
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                uint32_t a[4];
+                lds_x4(ks + piece(kr, 2 * k + (lane >> 4)), a);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) mma_bf16(s[t], a, qf[k][t][0], qf[k][t][1]);
+            }
+            const bool in0 = base + g < len, in1 = base + g + 8 < len;
+            float mn[NT][2];
+            bool grew = false;
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[t][i] *= scale;
+                if (scores) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const int h = 8 * t + c + i;
+                        if (h < heads && h < kHeads) {
+                            if (in0) scores[(long long)(base + g) * heads + h] = s[t][i];
+                            if (in1) scores[(long long)(base + g + 8) * heads + h] = s[t][2 + i];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    if (!in0) s[t][i] = -INFINITY;
+                    if (!in1) s[t][2 + i] = -INFINITY;
+                    float v = fmaxf(s[t][i], s[t][2 + i]);
+                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
+                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
+                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
+                    mn[t][i] = fmaxf(m[t][i], v);
+                    grew |= mn[t][i] != m[t][i];
+                }
+            }
+            if (__any_sync(0xFFFFFFFFu, grew)) {
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    const float a0 = exp2f(m[t][0] - base_of(mn[t][0])), a1 = exp2f(m[t][1] - base_of(mn[t][1]));
+                    m[t][0] = mn[t][0];
+                    m[t][1] = mn[t][1];
+                    l[t][0] *= a0;
+                    l[t][1] *= a1;
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        o[d][t][0] *= a0;
+                        o[d][t][1] *= a1;
+                        o[d][t][2] *= a0;
+                        o[d][t][3] *= a1;
+                    }
+                }
+            }
+            uint32_t hi[NT][2], lo[NT][2];
+#pragma unroll
+            for (int t = 0; t < NT; ++t) {
+                const float b0 = base_of(m[t][0]), b1 = base_of(m[t][1]);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float p0 = exp2f(s[t][2 * u] - b0), p1 = exp2f(s[t][2 * u + 1] - b1);
+                    l[t][0] += p0;
+                    l[t][1] += p1;
+                    const uint32_t h = cvt_bf16x2(p0, p1);
+                    const uint32_t r = cvt_bf16x2(p0 - bf16lo(h), p1 - bf16hi(h));
+                    if (MODE == kPacked) {
+                        hi[t][u] = transpose8((lane & 2) ? r : h);
+                    } else {
+                        hi[t][u] = transpose8(h);
+                        lo[t][u] = transpose8(r);
+                    }
+                }
+            }
+            const int vr = 16 * sub + (lane & 7) + ((lane >> 4) << 3);
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+                uint32_t a[4];
+                lds_x4_t(vs + piece(vr, 2 * d + ((lane >> 3) & 1)), a);
+#pragma unroll
+                for (int t = 0; t < NT; ++t) {
+                    mma_bf16(o[d][t], a, hi[t][0], hi[t][1]);
+                    if (MODE != kPacked) mma_bf16(o[d][t], a, lo[t][0], lo[t][1]);
+                }
+            }
+        }
+    }
+    // This warp's state: sums as [head][D] (row stride kMergeStride), maximum and sum per head.
+    __device__ __forceinline__ void store(float *so, float *sm, float *sl) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, c = 2 * (lane & 3);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                float v = l[t][i];
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+                v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+                if (g == 0 && 8 * t + c + i < kHeads) {
+                    sm[8 * t + c + i] = m[t][i];
+                    sl[8 * t + c + i] = v;
+                }
+            }
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float v = o[d][t][i];
+                    if (MODE == kPacked) v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+                    if (8 * t + c < kHeads) so[(8 * t + c + (i & 1)) * kMergeStride + 16 * d + g + 8 * (i >> 1)] = v;
+                }
+            }
+        }
+    }
+};
+
+// fp32 rows on the CUDA cores in full fp32: a lane holds D / 32 dims of q and of
+// the sums, a group of 8 keys x 4 heads gives 32 partial products per lane, which
+// 31 exchanges turn into one whole score per lane (lane = 4 key + head).
+template <int D_, int NG> struct F32Tile {
+    using T = float;
+    static constexpr int D = D_, KT = kPaStage / (8 * D), V = D / 32;
+    static constexpr int kHeads = 4 * NG;
+    static constexpr int kMergeStride = D + 4;
+    static constexpr int kStages = 3;
+    float q[4 * NG][V], o[4 * NG][V], m[NG], l[NG];      // m, l: of head 4 ng + lane % 4
+
+    static __device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)(r * (4 * D) + (c << 4)); }
+    static __device__ __forceinline__ void row(uint32_t addr, float (&f)[V]) {
+        if (V == 4) {
+            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
+                         : "=f"(f[0]), "=f"(f[1]), "=f"(f[V > 2 ? 2 : 0]), "=f"(f[V > 2 ? 3 : 1]) : "r"(addr) : "memory");
+        } else {
+            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f[0]), "=f"(f[1]) : "r"(addr) : "memory");
+        }
+    }
+    __device__ __forceinline__ void load_q(const T *src, int heads) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int h = 0; h < 4 * NG; ++h)
+#pragma unroll
+            for (int i = 0; i < V; ++i) q[h][i] = h < heads ? src[h * D + lane * V + i] : 0.f;
+    }
+    __device__ __forceinline__ void reset() {
+#pragma unroll
+        for (int n = 0; n < NG; ++n) m[n] = -INFINITY, l[n] = 0.f;
+#pragma unroll
+        for (int h = 0; h < 4 * NG; ++h)
+#pragma unroll
+            for (int i = 0; i < V; ++i) o[h][i] = 0.f;
+    }
+    __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, float *pad, int key0, int len, float scale, float *scores, int heads) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll 1
+        for (int sub = 0; sub < KT / 8; ++sub) {
+            const int base = key0 + 8 * sub;
+            if (base >= len) break;
+            const bool in = base + (lane >> 2) < len;
+#pragma unroll
+            for (int n = 0; n < NG; ++n) {
+                float x[32];
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    float f[V];
+                    row(ks + (8 * sub + k) * (4 * D) + lane * (4 * V), f);
+#pragma unroll
+                    for (int h = 0; h < 4; ++h) {
+                        float a = f[0] * q[4 * n + h][0];
+#pragma unroll
+                        for (int i = 1; i < V; ++i) a = fmaf(f[i], q[4 * n + h][i], a);
+                        x[4 * k + h] = a;
+                    }
+                }
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                    for (int i = 0; i < off; ++i) {
+                        const bool up = lane & off;
+                        const float give = up ? x[i] : x[i + off];
+                        x[i] = (up ? x[i + off] : x[i]) + __shfl_xor_sync(0xFFFFFFFFu, give, off);
+                    }
+                float s = x[0] * scale;
+                const int h = 4 * n + (lane & 3);
+                if (scores && in && h < heads) scores[(long long)(base + (lane >> 2)) * heads + h] = s;
+                if (!in) s = -INFINITY;
+                float mx = s;
+                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                mx = fmaxf(m[n], mx);
+                const float b = base_of(mx), alpha = exp2f(m[n] - b), p = exp2f(s - b);
+                m[n] = mx;
+                l[n] = l[n] * alpha + p;
+                pad[lane] = p;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float a = __shfl_sync(0xFFFFFFFFu, alpha, j);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[4 * n + j][i] *= a;
+                }
+                __syncwarp();
+#pragma unroll
+                for (int k = 0; k < 8; ++k) {
+                    const float4 w = *(const float4 *)(pad + 4 * k);
+                    float f[V];
+                    row(vs + (8 * sub + k) * (4 * D) + lane * (4 * V), f);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) {
+                        o[4 * n][i] = fmaf(w.x, f[i], o[4 * n][i]);
+                        o[4 * n + 1][i] = fmaf(w.y, f[i], o[4 * n + 1][i]);
+                        o[4 * n + 2][i] = fmaf(w.z, f[i], o[4 * n + 2][i]);
+                        o[4 * n + 3][i] = fmaf(w.w, f[i], o[4 * n + 3][i]);
+                    }
+                }
+                __syncwarp();
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float *so, float *sm, float *sl) {
+        const int lane = threadIdx.x & 31;
+#pragma unroll
+        for (int n = 0; n < NG; ++n) {
+            float v = l[n];
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+            if (lane < 4) {
+                sm[4 * n + lane] = m[n];
+                sl[4 * n + lane] = v;
+            }
+        }
+#pragma unroll
+        for (int h = 0; h < 4 * NG; ++h)
+#pragma unroll
+            for (int i = 0; i < V; ++i) so[h * kMergeStride + lane * V + i] = o[h][i];
+    }
+};
+
+// The part of one (sequence, KV head, head tile) segment that a CTA works on:
+// blocks [blk0, blk1) of the segment's nblk.
+struct Piece {
+    int u, b, h, blk0, blk1, nblk, len;
+    __device__ __forceinline__ int rows() const { return min(blk1 * kAttendUnit, len) - blk0 * kAttendUnit; }
+};
+__device__ __forceinline__ int blocks_of(int len) { return max(1, (len + kAttendUnit - 1) / kAttendUnit); }
+__device__ __forceinline__ void piece_at(Piece &p, const AttendArgs &a, int u1) {
+    p.len = paged_len(a.cache, p.b, a.added, a.err);
+    p.nblk = blocks_of(p.len);
+    p.blk1 = min(p.nblk, p.blk0 + u1 - p.u);
+}
+__device__ __forceinline__ bool next_piece(Piece &p, const AttendArgs &a, int heads, int u1) {
+    p.u += p.blk1 - p.blk0;
+    if (p.u >= u1) return false;
+    p.blk0 = 0;
+    if (++p.h == heads) {
+        p.h = 0;
+        ++p.b;
+        piece_at(p, a, u1);
+    } else {
+        p.blk1 = min(p.nblk, u1 - p.u);
+    }
+    return true;
+}
+
+// Writes the result of heads h0 .. of one segment from its sums, maxima and totals.
+template <typename T, int D>
+__device__ __forceinline__ void write_out(const AttendArgs &a, long long hq, int d, const float (&x)[4], float m, float l) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;          // no rows (or none above -inf): zeros
+    T *o = (T *)a.out + hq * D + d;
+    if (sizeof(T) == 2) {
+        *(uint2 *)o = make_uint2(cvt_bf16x2(x[0] * inv, x[1] * inv), cvt_bf16x2(x[2] * inv, x[3] * inv));
+    } else {
+        *(float4 *)o = make_float4(x[0] * inv, x[1] * inv, x[2] * inv, x[3] * inv);
+    }
+    if (d == 0) {
+        if (a.lse) a.lse[hq] = l == 0.f ? -INFINITY : base_of(m) * kLn2 + logf(l);
+        if (a.stat) a.stat[hq] = make_float2(base_of(m), inv);
+    }
+}
+
+template <typename P> constexpr size_t attend_smem() {
+    return (size_t)kPaWarps * (P::kStages * kPaStage + 4 * P::kHeads * (P::kMergeStride + 2));
+}
+
+// Persistent CTAs of four warps, two per SM.  The ragged (sequence, KV head,
+// block of 128 keys) units are cut into equal contiguous shares, one per CTA, so
+// that long and short sequences keep every SM equally busy; a segment cut between
+// CTAs is joined by the last of them to finish (in CTA order: the result does not
+// depend on which that is).  Within a CTA the tiles of KT keys go to the warps in
+// turn, each with its own ring of stages filled by cp.async, its own online
+// softmax and no barrier until the segment's end; the ring runs on across
+// segments, so loads never stop.
+template <typename P>
+__global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(AttendArgs a) {
+    using T = typename P::T;
+    constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads;
+    constexpr int kPart = H * (D + 2);                   // floats of a piece: sums [H][D], then (maximum, sum) [H]
+    constexpr int kRow = D * (int)sizeof(T), kChunks = kRow / 16, kRowsPer = 32 / kChunks;
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ int last;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_wait();
+    pdl_trigger();
+
+    const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
+    UnitRange r;
+    if (!unit_range<kPaThreads>(r, a.B, heads, a.min_units,
+                                [&](int b) { return blocks_of(paged_len(a.cache, b, a.added, a.err)); }))
+        return;
+
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * kPaStage);
+    float *merge = (float *)(smem + kPaWarps * S * kPaStage);                       // [warps][H][stride]
+    float *sm = merge + kPaWarps * H * P::kMergeStride, *sl = sm + kPaWarps * H;    // [warps][H]
+    float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
+
+    Piece p;                                             // the piece being computed
+    p.b = r.b;
+    p.u = r.u0;
+    p.len = paged_len(a.cache, p.b, a.added, a.err);
+    p.nblk = blocks_of(p.len);
+    p.h = (r.u0 - r.first) / p.nblk;
+    p.blk0 = (r.u0 - r.first) % p.nblk;
+    p.blk1 = min(p.nblk, p.blk0 + r.u1 - p.u);
+
+    // Loads run ahead of the computation: their own piece, tile and page.
+    Piece f = p;
+    int ft = warp;
+    bool more = true;
+    while (more && ft * KT >= f.rows()) more = next_piece(f, a, heads, r.u1);
+    int f_page = 0, f_row = 0;
+    bool f_in = false;
+    auto look_up = [&]() {                               // lane's row of tile ft (lanes past KT repeat)
+        const int key = f.blk0 * kAttendUnit + ft * KT + (lane % KT);
+        f_in = key < f.len;
+        const int slot = (unsigned)key / (unsigned)a.cache.page_size;
+        f_row = key - slot * a.cache.page_size;
+        if (f_in) f_page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
+    };
+    if (more) look_up();
+    int stage_in = 0;
+    auto issue = [&]() {
+        if (more) {
+            const bool known = (unsigned)f_page < (unsigned)a.cache.n_pages;
+            if (f_in && !known) set_err(a.err, kErrPage);
+            const int ok = f_in && known;
+            const long long off = ok ? f_page * a.cache.page_stride + (f.h / tiles) * a.cache.head_stride + f_row * a.cache.row_stride : 0;
+            const uint32_t ks = ring + stage_in * kPaStage, vs = ks + kPaStage / 2;
+            const int c = lane % kChunks;
+#pragma unroll
+            for (int i = 0; i < KT / kRowsPer; ++i) {
+                const int row = i * kRowsPer + lane / kChunks;
+                const long long at = __shfl_sync(0xFFFFFFFFu, off, row) + 16 * c;
+                const bool in = __shfl_sync(0xFFFFFFFFu, ok, row);
+                cp16(ks + P::piece(row, c), a.cache.k + at, in);
+                cp16(vs + P::piece(row, c), a.cache.v + at, in);
+            }
+            ft += kPaWarps;
+            while (more && ft * KT >= f.rows()) {
+                more = next_piece(f, a, heads, r.u1);
+                ft = warp;
+            }
+            if (more) look_up();
+        }
+        cp_group();
+        stage_in = stage_in + 1 == S ? 0 : stage_in + 1;
+    };
+#pragma unroll
+    for (int i = 0; i < S - 1; ++i) issue();
+
+    int stage = 0;
+    P state;
+    bool go = true;
+    while (go) {
+        const int kvh = p.h / tiles, h0 = (p.h % tiles) * H, n = min(H, G - h0);
+        const long long hq = (long long)p.b * a.Hq + kvh * G + h0;
+        state.load_q((const T *)a.q + hq * D, n);
+        state.reset();
+        float *scores = a.scores ? a.scores + ((long long)p.b * a.Hkv + kvh) * G * a.cache.table_pages * a.cache.page_size +
+                                       (long long)h0 * a.cache.table_pages * a.cache.page_size : nullptr;
+        const int rows = p.rows();
+        for (int t = warp; t * KT < rows; t += kPaWarps) {
+            cp_wait_group<S - 2>();
+            __syncwarp();
+            issue();
+            const uint32_t ks = ring + stage * kPaStage;
+            state.tile(ks, ks + kPaStage / 2, own, p.blk0 * kAttendUnit + t * KT, p.len, a.scale_log2, scores, n);
+            stage = stage + 1 == S ? 0 : stage + 1;
+        }
+        state.store(own, sm + warp * H, sl + warp * H);
+        __syncthreads();
+        const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
+        const int seg = p.b * heads + p.h;
+        const int seg0 = p.u - p.blk0;                   // the segment's first unit
+        const int c0 = seg0 / r.per, c1 = (seg0 + p.nblk - 1) / r.per;
+        const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
+        float *part = a.part + (long long)slot * kPart;
+        for (int e = tid; e < n * (D / 4); e += kPaThreads) {
+            const int h = e / (D / 4), d = 4 * (e % (D / 4));
+            float M = -INFINITY;
+#pragma unroll
+            for (int w = 0; w < kPaWarps; ++w) M = fmaxf(M, sm[w * H + h]);
+            const float base = base_of(M);
+            float x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+#pragma unroll
+            for (int w = 0; w < kPaWarps; ++w) {
+                const float k = exp2f(sm[w * H + h] - base);
+                const float4 y = *(const float4 *)(merge + (w * H + h) * P::kMergeStride + d);
+                L = fmaf(k, sl[w * H + h], L);
+                x[0] = fmaf(k, y.x, x[0]);
+                x[1] = fmaf(k, y.y, x[1]);
+                x[2] = fmaf(k, y.z, x[2]);
+                x[3] = fmaf(k, y.w, x[3]);
+            }
+            if (whole) {
+                write_out<T, D>(a, hq + h, d, x, M, L);
+            } else {
+                __stcg((float4 *)(part + h * D + d), make_float4(x[0], x[1], x[2], x[3]));
+                if (d == 0) {
+                    __stcg(part + H * D + 2 * h, M);
+                    __stcg(part + H * D + 2 * h + 1, L);
+                }
+            }
+        }
+        if (!whole) {
+            __threadfence();
+            __syncthreads();
+            if (tid == 0) last = atomicAdd(a.counter + seg, 1) == c1 - c0;
+            __syncthreads();
+            if (last) {
+                __threadfence();
+                // piece i of the segment: CTA c0's second slot, the others' first
+                auto piece_part = [&](int i) { return a.part + (long long)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * kPart; };
+                for (int e = tid; e < n * (D / 4); e += kPaThreads) {
+                    const int h = e / (D / 4), d = 4 * (e % (D / 4));
+                    float M = -INFINITY, x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+#pragma unroll 4
+                    for (int i = 0; i <= c1 - c0; ++i) M = fmaxf(M, __ldcg(piece_part(i) + H * D + 2 * h));
+                    const float base = base_of(M);
+#pragma unroll 4
+                    for (int i = 0; i <= c1 - c0; ++i) {
+                        const float *q = piece_part(i);
+                        const float4 y = __ldcg((const float4 *)(q + h * D + d));
+                        const float k = exp2f(__ldcg(q + H * D + 2 * h) - base);
+                        L = fmaf(k, __ldcg(q + H * D + 2 * h + 1), L);
+                        x[0] = fmaf(k, y.x, x[0]);
+                        x[1] = fmaf(k, y.y, x[1]);
+                        x[2] = fmaf(k, y.z, x[2]);
+                        x[3] = fmaf(k, y.w, x[3]);
+                    }
+                    write_out<T, D>(a, hq + h, d, x, M, L);
+                }
+                if (tid == 0) a.counter[seg] = 0;
+            }
+        }
+        __syncthreads();                                 // the merge area is free again
+        go = next_piece(p, a, heads, r.u1);
+    }
+    cp_wait_group<0>();
+}
+
+// weights[j] += sum_h 2^(s_jh - M_h) / L_h from the scores the attention kernel
+// left, heads in order; one thread per (KV head, row).
+constexpr int kWtThreads = 256;
+__global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a, int head_tile) {
+    pdl_wait();
+    pdl_trigger();
+    const int G = a.Hq / a.Hkv;
+    constexpr int kRows = 4 * kAttendUnit;
+    auto blocks = [&](int b) { return max(1, (paged_len(a.cache, b, a.added, nullptr) + kRows - 1) / kRows); };
+    UnitRange r;
+    if (!unit_range<kWtThreads>(r, a.B, a.Hkv, 1, blocks)) return;
+    int b = r.b, len = paged_len(a.cache, b, a.added, nullptr), nblk = blocks(b);
+    int h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
+    const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
+    for (int u = r.u0; u < r.u1; ++u) {
+        for (int j = blk * kRows + threadIdx.x; j < min(len, (blk + 1) * kRows); j += kWtThreads) {
+            const int slot = j / a.cache.page_size;
+            const int page = a.cache.table[(long long)b * a.cache.table_pages + slot];
+            if ((unsigned)page >= (unsigned)a.cache.n_pages) continue;   // reported by the attention
+            const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
+            const float2 *st = a.stat + (long long)b * a.Hq + h * G;
+            float w = 0.f;
+            for (int t = 0; t < G; t += head_tile) {
+                const int n = min(head_tile, G - t);
+                const float *z = s + t * cap + (long long)j * n;
+                for (int i = 0; i < n; ++i) {
+                    const float2 ml = st[t + i];
+                    w = fmaf(exp2f(z[i] - ml.x), ml.y, w);
+                }
+            }
+            float *to = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
+            *to += w;
+        }
+        if (++blk == nblk) {
+            blk = 0;
+            if (++h == a.Hkv) {
+                h = 0;
+                if (++b < a.B) {
+                    len = paged_len(a.cache, b, a.added, nullptr);
+                    nblk = blocks(b);
+                }
+            }
+        }
+    }
+}
+
+// The tile form of a type, head dimension and group: 4, 8 or 16 heads of bf16, 4
+// or 8 of fp32 share a pass over the rows; more heads take more passes.
+template <typename F> cudaError_t with_tile(bool bf16, int D, int G, const F &f) {
+    if (bf16) {
+        if (D == 128) return G <= 4 ? f(Bf16Tile<128, kPacked>()) : G <= 8 ? f(Bf16Tile<128, kEight>()) : f(Bf16Tile<128, kSixteen>());
+        return G <= 4 ? f(Bf16Tile<64, kPacked>()) : G <= 8 ? f(Bf16Tile<64, kEight>()) : f(Bf16Tile<64, kSixteen>());
+    }
+    if (D == 128) return G <= 4 ? f(F32Tile<128, 1>()) : f(F32Tile<128, 2>());
+    return G <= 4 ? f(F32Tile<64, 1>()) : f(F32Tile<64, 2>());
+}
+
+}  // namespace
+
+int attend_head_tile(bool bf16, int G) { return G <= 4 ? 4 : G <= 8 || !bf16 ? 8 : 16; }
+
+size_t attend_part_floats(bool bf16, int D, int G, int sms) {
+    return (size_t)2 * sms * kPaCtasPerSm * attend_head_tile(bf16, G) * (D + 2);
+}
+
+cudaError_t prepare_attend_kernels() {
+    for (const bool bf16 : {false, true})
+        for (const int D : {64, 128})
+            for (const int G : {4, 8, 16}) {
+                const cudaError_t e = with_tile(bf16, D, G, [](auto tile) {
+                    using P = decltype(tile);
+                    return cudaFuncSetAttribute(paged_attend_kernel<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
+                });
+                if (e != cudaSuccess) return e;
+            }
+    return cudaSuccess;
+}
+
+cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s) {
+    const int G = a.Hq / a.Hkv, ht = attend_head_tile(bf16, G);
+    const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
+    const long long most = a.B * (long long)a.Hkv * ((G + ht - 1) / ht) * ((cap + kAttendUnit - 1) / kAttendUnit);
+    const int grid = (int)(most < sms * kPaCtasPerSm ? most : sms * kPaCtasPerSm);
+    cudaError_t e = with_tile(bf16, D, G, [&](auto tile) {
+        using P = decltype(tile);
+        return launch_k(paged_attend_kernel<P>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
+    });
+    if (e != cudaSuccess || !a.scores) return e;
+    const long long chunks = a.B * (long long)a.Hkv * ((cap + 4 * kAttendUnit - 1) / (4 * kAttendUnit));
+    const int wt = (int)(chunks < sms * 8 ? chunks : sms * 8);
+    return launch_k(paged_weights_kernel, dim3(wt), dim3(kWtThreads), 0, s, true, a, ht);
+}
+
+}  // namespace prism

@@ -1,0 +1,273 @@
+"""Operators over a paged key-value cache (the paged section of
+``include/prism.h``): the per-head norm of queries and keys with the position
+rotation, stored into the cache (:meth:`PagedAttention.append`) or dense with
+its gradient (:meth:`PagedAttention.qk_norm_rope`,
+:meth:`PagedAttention.qk_norm_rope_backward`), the attention of one new token
+(:meth:`PagedAttention.attend`) and eviction by accumulated attention weight
+(:meth:`PagedAttention.evict`).
+
+A decode step of one layer::
+
+    att = PagedAttention(n_q_heads=32, n_kv_heads=8, head_dim=128, page_size=16,
+                         max_batch=B, max_pages=P, track_weights=True)
+    cache = att.cache(k_pages, v_pages, block_table, kv_len, weights=weights)
+    rope = rope_table(max_positions, 128, theta=500000.0)
+
+    att.append(cache, q, k, v, q_out, rope, g_q=g_q, g_k=g_k, pos=pos)   # row kv_len[b]
+    att.attend(cache, q_out.view(B, 32, 128), out)                       # over kv_len[b] + 1 rows
+    kv_len += 1; pos += 1
+
+and, when the cache has grown past its budget,
+``att.evict(cache, other_cache, kept, sinks=4, recent=512)``.
+
+As in the rest of the package the binding only checks and marshals: every
+result is computed by the library's kernels on the current CUDA stream, and a
+missing library raises.  Tensors belong to the caller; a call that uses a tensor
+on another stream than the one it was allocated on needs the caller's
+``record_stream``, as with any asynchronous torch operation.
+"""
+from __future__ import annotations
+
+import ctypes
+
+import torch
+
+__all__ = ["PagedAttention", "PagedCache", "rope_table"]
+
+_vp, _i32, _i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+
+
+class _PagedConfig(ctypes.Structure):
+    _fields_ = [(n, _i32) for n in ("n_q_heads", "n_kv_heads", "head_dim", "dtype", "page_size", "max_batch",
+                                    "max_pages", "track_weights")] + [("softmax_scale", ctypes.c_float),
+                                                                      ("rms_eps", ctypes.c_float)]
+
+
+class _Cache(ctypes.Structure):
+    _fields_ = [("k_pages", _vp), ("v_pages", _vp), ("page_stride", _i64), ("head_stride", _i64), ("row_stride", _i64),
+                ("weights", _vp), ("block_table", _vp), ("kv_len", _vp), ("n_pages", _i32), ("table_pages", _i32),
+                ("batch", _i32)]
+
+
+class _Heads(ctypes.Structure):
+    _fields_ = [("data", _vp), ("batch_stride", _i64), ("row_stride", _i64), ("head_stride", _i64)]
+
+
+def bind(lib: ctypes.CDLL) -> None:
+    """Argument and result types of the paged entry points."""
+    P = ctypes.POINTER
+    H, C = P(_Heads), P(_Cache)
+    lib.prism_paged_create.argtypes = [P(_PagedConfig), _i32, P(_vp)]
+    lib.prism_paged_destroy.argtypes = [_vp]
+    lib.prism_qk_norm_rope.argtypes = [_vp, _i32, _i32, H, H, H, H, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
+    lib.prism_qk_norm_rope_backward.argtypes = [_vp, _i32, _i32] + [H] * 6 + [_vp, _vp, _vp, _i32] + [_vp] * 5
+    lib.prism_paged_append.argtypes = [_vp, C, _i32, H, H, H, H, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
+    lib.prism_paged_attend.argtypes = [_vp, C, _i32, _vp, _vp, _vp, _vp]
+    lib.prism_paged_evict.argtypes = [_vp, C, C, _i32, _i32, _i32, _vp, _vp]
+    lib.prism_paged_status.argtypes = [_vp, _vp, P(_i32)]
+    lib.prism_paged_error.argtypes = [_vp]
+    lib.prism_paged_error.restype = ctypes.c_char_p
+    for f in ("prism_paged_create", "prism_paged_destroy", "prism_qk_norm_rope", "prism_qk_norm_rope_backward",
+              "prism_paged_append", "prism_paged_attend", "prism_paged_evict", "prism_paged_status"):
+        getattr(lib, f).restype = ctypes.c_int
+
+
+def rope_table(positions: int, head_dim: int, theta: float = 10000.0, device=0) -> torch.Tensor:
+    """fp32 [positions, 2, head_dim / 2]: cosines and sines of
+    position * theta^(-2j / head_dim), computed in fp64."""
+    a = torch.arange(positions, dtype=torch.float64)[:, None] * (
+        float(theta) ** (-torch.arange(0, head_dim, 2, dtype=torch.float64) / head_dim))
+    return torch.stack([torch.cos(a), torch.sin(a)], 1).float().to(device)
+
+
+class PagedCache:
+    """A paged cache bound by :meth:`PagedAttention.cache`: its tensors, checked
+    once, and the struct the calls pass on."""
+
+    def __init__(self, struct, tensors, batch, rows, dtype, device, heads):
+        self.struct, self.ref = struct, ctypes.byref(struct)
+        self.k_pages, self.v_pages, self.block_table, self.kv_len, self.weights = tensors
+        self.batch, self.rows = batch, rows          # sequences; rows a block-table line holds
+        self.key = (dtype, device, heads)
+
+
+class PagedAttention:
+    """Paged-cache operators of one attention layout on one GPU.
+
+    ``dtype`` "bf16" or "f32" is that of queries, keys, values, gains and cache;
+    ``max_batch`` and ``max_pages`` bound the calls that take a cache;
+    ``track_weights`` allots the workspace that accumulating attention weights
+    needs; ``softmax_scale`` None means ``head_dim ** -0.5``.  A handle's calls
+    share its workspace: keep them on one stream."""
+
+    def __init__(self, *, n_q_heads, n_kv_heads, head_dim, page_size, max_batch, max_pages, dtype="bf16",
+                 track_weights=False, softmax_scale=None, rms_eps=1e-5, device=0):
+        from . import library
+        if dtype not in ("bf16", "f32"):
+            raise ValueError("dtype must be 'bf16' or 'f32'")
+        self.h = None
+        self.lib = library()
+        self.tdtype = torch.bfloat16 if dtype == "bf16" else torch.float32
+        self.device = torch.device("cuda", device)
+        self.n_q_heads, self.n_kv_heads, self.head_dim, self.page_size = n_q_heads, n_kv_heads, head_dim, page_size
+        self.max_batch, self.max_pages, self.track_weights = max_batch, max_pages, bool(track_weights)
+        cfg = _PagedConfig(n_q_heads, n_kv_heads, head_dim, 1 if dtype == "bf16" else 0, page_size, max_batch, max_pages,
+                           int(bool(track_weights)), 0.0 if softmax_scale is None else float(softmax_scale), float(rms_eps))
+        h = _vp()
+        self._check(self.lib.prism_paged_create(ctypes.byref(cfg), device, ctypes.byref(h)))
+        self.h = h
+        self._key = (self.tdtype, self.device, (n_kv_heads, page_size, head_dim))
+
+    # ------------------------------------------------------------ checks
+    def _check(self, status):
+        if status != 0:
+            from . import PrismError
+            raise PrismError(status, (self.lib.prism_paged_error(self.h) or b"").decode())
+
+    def _tensor(self, t, shape, dtype, name):
+        """Address of a dense tensor of this device, shape and type."""
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch.Tensor")
+        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)} on {self.device}, got {t.dtype} "
+                             f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
+        return t.data_ptr()
+
+    def _heads(self, t, batch, rows, heads, name):
+        """A [batch, rows, heads, D] tensor, strided but for D."""
+        if not isinstance(t, torch.Tensor):
+            raise TypeError(f"{name}: expected a torch.Tensor")
+        if t.dtype is not self.tdtype or t.shape != (batch, rows, heads, self.head_dim) or t.device != self.device:
+            raise ValueError(f"{name}: expected {self.tdtype} {(batch, rows, heads, self.head_dim)} on {self.device}, got "
+                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
+        s = t.stride()
+        if s[3] != 1:
+            raise ValueError(f"{name}: the head dimension must be dense")
+        return _Heads(t.data_ptr(), s[0], s[1], s[2])
+
+    def _gain(self, g, name):
+        return None if g is None else self._tensor(g, (self.head_dim,), self.tdtype, name)
+
+    def _rope(self, rope):
+        n = rope.shape[0]
+        return self._tensor(rope, (n, 2, self.head_dim // 2), torch.float32, "rope"), n
+
+    def _counts(self, t, batch, name):
+        return None if t is None else self._tensor(t, (batch,), torch.int32, name)
+
+    def _stream(self, stream):
+        if stream is None:
+            return torch.cuda.current_stream(self.device).cuda_stream
+        return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
+
+    def _bound(self, cache):
+        if not isinstance(cache, PagedCache):
+            raise TypeError("expected a PagedCache (PagedAttention.cache)")
+        if cache.key != self._key:
+            raise ValueError("the cache was bound for another layout, type or device")
+        return cache.ref
+
+    # ------------------------------------------------------------ calls
+    def cache(self, k_pages, v_pages, block_table, kv_len, weights=None) -> PagedCache:
+        """Bind a paged cache.  ``k_pages``, ``v_pages`` [n_pages, Hkv, page_size,
+        D], with any equal strides but a dense D (a permuted view of [n_pages,
+        page_size, Hkv, D] storage will do); ``block_table`` int32 [batch, pages];
+        ``kv_len`` int32 [batch]; ``weights`` fp32 [n_pages, Hkv, page_size]."""
+        n_pages = k_pages.shape[0]
+        shape = (n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
+            if t.dtype is not self.tdtype or t.shape != shape or t.device != self.device:
+                raise ValueError(f"{name}: expected {self.tdtype} {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} "
+                                 f"on {t.device}")
+            if t.stride() != k_pages.stride() or t.stride(3) != 1:
+                raise ValueError(f"{name}: K and V need the same strides and a dense head dimension")
+        if block_table.dim() != 2:
+            raise ValueError("block_table: expected two dimensions")
+        batch, pages = block_table.shape
+        self._tensor(block_table, (batch, pages), torch.int32, "block_table")
+        self._tensor(kv_len, (batch,), torch.int32, "kv_len")
+        if weights is not None:
+            self._tensor(weights, (n_pages, self.n_kv_heads, self.page_size), torch.float32, "weights")
+        s = k_pages.stride()
+        struct = _Cache(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2],
+                        None if weights is None else weights.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
+                        n_pages, pages, batch)
+        return PagedCache(struct, (k_pages, v_pages, block_table, kv_len, weights), batch, pages * self.page_size, *self._key)
+
+    def qk_norm_rope(self, q, k, q_out, k_out, rope, pos, g_q=None, g_k=None, n_new=None, stream=None):
+        """``prism_qk_norm_rope``: q, q_out [B, n, Hq, D]; k, k_out [B, n, Hkv, D]
+        (strided but for D); rope fp32 [positions, 2, D / 2]; pos, n_new int32 [B]."""
+        B, n = q.shape[:2]
+        sq, sk = self._heads(q, B, n, self.n_q_heads, "q"), self._heads(k, B, n, self.n_kv_heads, "k")
+        oq, ok = self._heads(q_out, B, n, self.n_q_heads, "q_out"), self._heads(k_out, B, n, self.n_kv_heads, "k_out")
+        table, length = self._rope(rope)
+        self._check(self.lib.prism_qk_norm_rope(
+            self.h, B, n, sq, sk, oq, ok, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), table, length,
+            self._counts(pos, B, "pos"), self._counts(n_new, B, "n_new"), self._stream(stream)))
+
+    def qk_norm_rope_backward(self, dq_out, dk_out, q, k, dq, dk, rope, pos, g_q=None, g_k=None, dg_q=None, dg_k=None,
+                              n_new=None, stream=None):
+        """``prism_qk_norm_rope_backward``: the gradients dq, dk (zeros past
+        n_new) and dg_q, dg_k (fp32 [D]) from those of the outputs and the
+        forward's inputs."""
+        B, n = q.shape[:2]
+        Hq, Hkv = self.n_q_heads, self.n_kv_heads
+        args = [self._heads(t, B, n, H, name) for t, H, name in (
+            (dq_out, Hq, "dq_out"), (dk_out, Hkv, "dk_out"), (q, Hq, "q"), (k, Hkv, "k"), (dq, Hq, "dq"), (dk, Hkv, "dk"))]
+        table, length = self._rope(rope)
+        d = [None if t is None else self._tensor(t, (self.head_dim,), torch.float32, name)
+             for t, name in ((dg_q, "dg_q"), (dg_k, "dg_k"))]
+        self._check(self.lib.prism_qk_norm_rope_backward(
+            self.h, B, n, *args, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), table, length,
+            self._counts(pos, B, "pos"), self._counts(n_new, B, "n_new"), *d, self._stream(stream)))
+
+    def append(self, cache, q, k, v, q_out, rope, g_q=None, g_k=None, pos=None, n_new=None, stream=None):
+        """``prism_paged_append``: q, q_out [B, n, Hq, D]; k, v [B, n, Hkv, D].
+        Rows i < n_new[b] go to slots kv_len[b] + i, at positions pos[b] + i (pos
+        None: their slots).  kv_len is not advanced."""
+        ref = self._bound(cache)
+        B, n = cache.batch, q.shape[1]
+        sq, sk = self._heads(q, B, n, self.n_q_heads, "q"), self._heads(k, B, n, self.n_kv_heads, "k")
+        sv, oq = self._heads(v, B, n, self.n_kv_heads, "v"), self._heads(q_out, B, n, self.n_q_heads, "q_out")
+        table, length = self._rope(rope)
+        self._check(self.lib.prism_paged_append(
+            self.h, ref, n, sq, sk, sv, oq, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), table, length,
+            self._counts(pos, B, "pos"), self._counts(n_new, B, "n_new"), self._stream(stream)))
+
+    def attend(self, cache, q, out, lse=None, added=1, stream=None):
+        """``prism_paged_attend``: q, out [B, Hq, D]; lse fp32 [B, Hq] or None;
+        over kv_len[b] + added rows.  A cache with weights accumulates them."""
+        ref = self._bound(cache)
+        shape = (cache.batch, self.n_q_heads, self.head_dim)
+        self._check(self.lib.prism_paged_attend(
+            self.h, ref, added, self._tensor(q, shape, self.tdtype, "q"), self._tensor(out, shape, self.tdtype, "out"),
+            None if lse is None else self._tensor(lse, shape[:2], torch.float32, "lse"), self._stream(stream)))
+
+    def evict(self, src, dst, kept, sinks=0, recent=0, stream=None):
+        """``prism_paged_evict``: the rows of ``src`` to keep go, in order, to the
+        pages of ``dst``; ``kept`` int32 [B, Hkv, budget] receives their slots."""
+        rs, rd = self._bound(src), self._bound(dst)
+        if kept.dim() != 3:
+            raise ValueError("kept: expected three dimensions")
+        budget = kept.shape[2]
+        at = self._tensor(kept, (src.batch, self.n_kv_heads, budget), torch.int32, "kept")
+        self._check(self.lib.prism_paged_evict(self.h, rs, rd, budget, sinks, recent, at, self._stream(stream)))
+
+    def status(self, stream=None) -> int:
+        """Synchronise; the device error word (0 when clean), cleared."""
+        flags = _i32(0)
+        st = self.lib.prism_paged_status(self.h, self._stream(stream), ctypes.byref(flags))
+        if st not in (0, 7):
+            self._check(st)
+        return int(flags.value)
+
+    def close(self):
+        if getattr(self, "h", None):
+            self.lib.prism_paged_destroy(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
