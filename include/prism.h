@@ -538,37 +538,49 @@ typedef struct {
 prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, prism_paged **out);
 prism_status prism_paged_destroy(prism_paged *p);
 
-/* RMSNorm of every query and key head on its own with gains g_q, g_k (wtype
- * [D]; both NULL: no norm), then the rotate-half rotation of dims (j, j + D/2)
- * by the angle of the row's position: row i < n_new[b] of sequence b stands at
- * position pos[b] + i.
- *   rope   fp32 [rope_len, 2, D/2]: cosines, then sines of each position
- *   pos    int32 [batch]; n_new int32 [batch] or NULL (max_new rows each)
- * Rows past n_new[b] are not written.  All arithmetic in fp32, rounded once.
- * Errors: INVALID_ARG, SHAPE, CAPACITY (more than 2^24 rows), CUDA. */
-prism_status prism_qk_norm_rope(prism_paged *p, int32_t batch, int32_t max_new, const prism_heads *q, const prism_heads *k,
-                                const prism_heads *q_out, const prism_heads *k_out, const void *g_q, const void *g_k,
-                                const float *rope, int32_t rope_len, const int32_t *pos, const int32_t *n_new, void *stream);
+/* A block of new rows: row i < n_new[b] of sequence b stands at position
+ * pos[b] + i.
+ *   q, k, v        [batch, max_new, heads, D], Hq query and Hkv key and value
+ *                  heads (v: prism_paged_append alone)
+ *   q_out, k_out   the normed and rotated rows (k_out: not prism_paged_append,
+ *                  whose keys go to the cache)
+ *   g_q, g_k       gains wtype [D]; both NULL: no norm
+ *   rope           fp32 [rope_len, 2, D/2]: cosines, then sines of each position
+ *   pos            int32 [batch]
+ *   n_new          int32 [batch], or NULL: max_new rows each
+ * Rows past n_new[b] are neither read nor, unless stated, written. */
+typedef struct {
+    prism_heads q, k, v, q_out, k_out;
+    const void *g_q, *g_k;
+    const float *rope;
+    const int32_t *pos, *n_new;
+    int32_t rope_len, batch, max_new;
+} prism_rows;
 
-/* Its gradient: from dq_out, dk_out (wtype) and the forward's inputs, dq and dk
- * (wtype; zeros past n_new[b]) and the gains' gradients dg_q, dg_k (fp32 [D],
- * summed over rows and heads in a fixed order; NULL when there are no gains).
- * Errors: as prism_qk_norm_rope. */
-prism_status prism_qk_norm_rope_backward(prism_paged *p, int32_t batch, int32_t max_new, const prism_heads *dq_out,
-                                         const prism_heads *dk_out, const prism_heads *q, const prism_heads *k,
-                                         const prism_heads *dq, const prism_heads *dk, const void *g_q, const void *g_k,
-                                         const float *rope, int32_t rope_len, const int32_t *pos, const int32_t *n_new,
-                                         float *dg_q, float *dg_k, void *stream);
+/* Gradients of a block of rows: dq_out, dk_out those of the outputs (read), dq,
+ * dk those of q and k, dg_q, dg_k (fp32 [D]; NULL without gains) the gains'. */
+typedef struct {
+    prism_heads dq_out, dk_out, dq, dk;
+    float *dg_q, *dg_k;
+} prism_row_grads;
+
+/* RMSNorm of every query and key head on its own, with gains, then the
+ * rotate-half rotation of dims (j, j + D/2) by the angle of the row's position.
+ * All arithmetic in fp32, rounded once.  Errors: INVALID_ARG, SHAPE, CAPACITY
+ * (more than 2^24 rows), CUDA. */
+prism_status prism_qk_norm_rope(prism_paged *p, const prism_rows *rows, void *stream);
+
+/* Its gradient, from the forward's inputs (q_out and k_out of `rows` are not
+ * used): dq and dk (zeros past n_new[b]), and the gains', summed over rows and
+ * heads in a fixed order.  Errors: as prism_qk_norm_rope. */
+prism_status prism_qk_norm_rope_backward(prism_paged *p, const prism_rows *rows, const prism_row_grads *grads, void *stream);
 
 /* The same norm and rotation with the keys, and the values as they are, stored
  * into the cache: row i < n_new[b] of sequence b goes to slot kv_len[b] + i, its
  * weight (if the cache has weights) starts at 0.  kv_len is read, not advanced.
  * pos NULL: rows stand at their slots (after an eviction they no longer do).
  * Errors: as prism_qk_norm_rope, CAPACITY (batch or table beyond the handle). */
-prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, int32_t max_new, const prism_heads *q,
-                                const prism_heads *k, const prism_heads *v, const prism_heads *q_out, const void *g_q,
-                                const void *g_k, const float *rope, int32_t rope_len, const int32_t *pos,
-                                const int32_t *n_new, void *stream);
+prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, const prism_rows *rows, void *stream);
 
 /* Attention of one query row per sequence, q wtype [batch, Hq, D] (normed and
  * rotated), over the kv_len[b] + added rows of its cache (added = 1: a row

@@ -84,7 +84,7 @@ cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, 
 cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
 int norm_rope_grad_ctas(int sms);
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
-cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, cudaStream_t s);
+cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s);
 
 #ifdef __CUDACC__
 // Rows of sequence b, held to [0, table rows] (outside: the cache-range bit).
@@ -130,6 +130,19 @@ template <> struct Vec16<float> {
         return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
     }
 };
+
+// Add to, or set, the same shared variable in another CTA of the cluster.
+__device__ __forceinline__ uint32_t dsmem_at(const void *local, uint32_t rank) {
+    uint32_t remote;
+    asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
+    return remote;
+}
+__device__ __forceinline__ void dsmem_add(int *local, uint32_t rank, int v) {
+    asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;" ::"r"(dsmem_at(local, rank)), "r"(v) : "memory");
+}
+__device__ __forceinline__ void dsmem_st(int *local, uint32_t rank, int v) {
+    asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(dsmem_at(local, rank)), "r"(v) : "memory");
+}
 
 // Ragged work split into equal contiguous shares.  Sequence b has blocks(b) >= 1
 // blocks of keys, each for `heads` heads; units run over (b, head, block).

@@ -68,14 +68,11 @@ struct Check {
         if (!ok && s == PRISM_OK) s = fail(p, st, "%s", what);
     }
     int es() const { return p->bf16 ? 2 : 4; }
-    HeadsView heads(const prism_heads *h, const char *name) {
-        HeadsView v{};
-        if (!h || !h->data) {
-            if (s == PRISM_OK) s = fail(p, PRISM_ERR_INVALID_ARG, "%s is null", name);
-            return v;
-        }
-        v = {(char *)h->data, h->batch_stride * es(), h->row_stride * es(), h->head_stride * es()};
-        if (s == PRISM_OK && (misaligned(h->data) || ((v.sb | v.st | v.sh) & 15)))
+    HeadsView heads(const prism_heads &h, const char *name) {
+        const HeadsView v = {(char *)h.data, h.batch_stride * es(), h.row_stride * es(), h.head_stride * es()};
+        if (s != PRISM_OK) return v;
+        if (!v.p) s = fail(p, PRISM_ERR_INVALID_ARG, "%s is null", name);
+        else if (misaligned(v.p) || ((v.sb | v.st | v.sh) & 15))
             s = fail(p, PRISM_ERR_INVALID_ARG, "%s: base and strides must be multiples of 16 bytes", name);
         return v;
     }
@@ -99,18 +96,21 @@ struct Check {
                      c->table_pages, p->cfg.max_batch, p->cfg.max_pages);
         return v;
     }
-    void rows(int32_t batch, int32_t max_new) {
-        need(batch >= 1 && max_new >= 1, PRISM_ERR_SHAPE, "batch and max_new must be at least 1");
-        need((long long)batch * max_new <= (1LL << 24), PRISM_ERR_CAPACITY, "batch * max_new exceeds 2^24 rows");
-    }
-    void rope(const float *rope, int32_t len) {
-        need(rope != nullptr, PRISM_ERR_INVALID_ARG, "rope is null");
-        need(!misaligned(rope), PRISM_ERR_INVALID_ARG, "rope must be 16-byte aligned");
-        need(len >= 1, PRISM_ERR_SHAPE, "rope_len must be at least 1");
-    }
-    void gains(const void *g_q, const void *g_k) {
-        need(!g_q == !g_k, PRISM_ERR_INVALID_ARG, "g_q and g_k are given together or not at all");
-        need(!misaligned(g_q) && !misaligned(g_k), PRISM_ERR_INVALID_ARG, "gains must be 16-byte aligned");
+    // What the forward, the append and the gradient have in common.
+    template <typename A> A rows(const prism_rows &r) {
+        A a{};
+        a.q = heads(r.q, "q");
+        a.k = heads(r.k, "k");
+        a.g_q = r.g_q, a.g_k = r.g_k, a.rope = r.rope, a.pos = r.pos, a.n_new = r.n_new, a.rope_len = r.rope_len;
+        a.B = r.batch, a.max_new = r.max_new, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.eps = p->cfg.rms_eps, a.err = p->err;
+        need(r.batch >= 1 && r.max_new >= 1, PRISM_ERR_SHAPE, "batch and max_new must be at least 1");
+        need((long long)r.batch * r.max_new <= (1LL << 24), PRISM_ERR_CAPACITY, "batch * max_new exceeds 2^24 rows");
+        need(r.rope != nullptr, PRISM_ERR_INVALID_ARG, "rope is null");
+        need(!misaligned(r.rope), PRISM_ERR_INVALID_ARG, "rope must be 16-byte aligned");
+        need(r.rope_len >= 1, PRISM_ERR_SHAPE, "rope_len must be at least 1");
+        need(!r.g_q == !r.g_k, PRISM_ERR_INVALID_ARG, "g_q and g_k are given together or not at all");
+        need(!misaligned(r.g_q) && !misaligned(r.g_k), PRISM_ERR_INVALID_ARG, "gains must be 16-byte aligned");
+        return a;
     }
 };
 
@@ -199,75 +199,47 @@ prism_status prism_paged_destroy(prism_paged *p) {
     return cuda_status(nullptr, e, "prism_paged_destroy");
 }
 
-prism_status prism_qk_norm_rope(prism_paged *p, int32_t batch, int32_t max_new, const prism_heads *q, const prism_heads *k,
-                                const prism_heads *q_out, const prism_heads *k_out, const void *g_q, const void *g_k,
-                                const float *rope, int32_t rope_len, const int32_t *pos, const int32_t *n_new, void *stream) {
-    if (!p) return fail(nullptr, PRISM_ERR_INVALID_ARG, "prism_qk_norm_rope: null handle");
+prism_status prism_qk_norm_rope(prism_paged *p, const prism_rows *rows, void *stream) {
+    if (!p || !rows) return fail(p, PRISM_ERR_INVALID_ARG, "prism_qk_norm_rope: null argument");
     Check c{p};
-    NormRopeArgs a{};
-    a.q = c.heads(q, "q");
-    a.k = c.heads(k, "k");
-    a.q_out = c.heads(q_out, "q_out");
-    a.k_out = c.heads(k_out, "k_out");
-    c.rows(batch, max_new);
-    c.rope(rope, rope_len);
-    c.need(pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
-    c.gains(g_q, g_k);
+    NormRopeArgs a = c.rows<NormRopeArgs>(*rows);
+    a.q_out = c.heads(rows->q_out, "q_out");
+    a.k_out = c.heads(rows->k_out, "k_out");
+    c.need(a.pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
     if (c.s != PRISM_OK) return c.s;
-    a.g_q = g_q, a.g_k = g_k, a.rope = rope, a.pos = pos, a.n_new = n_new, a.rope_len = rope_len;
-    a.B = batch, a.max_new = max_new, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.eps = p->cfg.rms_eps, a.err = p->err;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
     return cuda_status(p, launch_norm_rope(a, p->bf16, p->cfg.head_dim, false, p->sms, (cudaStream_t)stream), "prism_qk_norm_rope");
 }
 
-prism_status prism_qk_norm_rope_backward(prism_paged *p, int32_t batch, int32_t max_new, const prism_heads *dq_out,
-                                         const prism_heads *dk_out, const prism_heads *q, const prism_heads *k,
-                                         const prism_heads *dq, const prism_heads *dk, const void *g_q, const void *g_k,
-                                         const float *rope, int32_t rope_len, const int32_t *pos, const int32_t *n_new,
-                                         float *dg_q, float *dg_k, void *stream) {
-    if (!p) return fail(nullptr, PRISM_ERR_INVALID_ARG, "prism_qk_norm_rope_backward: null handle");
+prism_status prism_qk_norm_rope_backward(prism_paged *p, const prism_rows *rows, const prism_row_grads *grads, void *stream) {
+    if (!p || !rows || !grads) return fail(p, PRISM_ERR_INVALID_ARG, "prism_qk_norm_rope_backward: null argument");
     Check c{p};
-    NormRopeGradArgs a{};
-    a.dq_out = c.heads(dq_out, "dq_out");
-    a.dk_out = c.heads(dk_out, "dk_out");
-    a.q = c.heads(q, "q");
-    a.k = c.heads(k, "k");
-    a.dq = c.heads(dq, "dq");
-    a.dk = c.heads(dk, "dk");
-    c.rows(batch, max_new);
-    c.rope(rope, rope_len);
-    c.need(pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
-    c.gains(g_q, g_k);
-    c.need(!g_q == !dg_q && !g_q == !dg_k, PRISM_ERR_INVALID_ARG, "dg_q and dg_k are given with the gains and only then");
+    NormRopeGradArgs a = c.rows<NormRopeGradArgs>(*rows);
+    a.dq_out = c.heads(grads->dq_out, "dq_out");
+    a.dk_out = c.heads(grads->dk_out, "dk_out");
+    a.dq = c.heads(grads->dq, "dq");
+    a.dk = c.heads(grads->dk, "dk");
+    a.dg_q = grads->dg_q, a.dg_k = grads->dg_k, a.part = p->grad_part, a.counter = p->counter + p->counters;
+    c.need(a.pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
+    c.need(!a.g_q == !a.dg_q && !a.g_q == !a.dg_k, PRISM_ERR_INVALID_ARG, "dg_q and dg_k are given with the gains and only then");
     if (c.s != PRISM_OK) return c.s;
-    a.g_q = g_q, a.g_k = g_k, a.rope = rope, a.pos = pos, a.n_new = n_new, a.rope_len = rope_len;
-    a.dg_q = dg_q, a.dg_k = dg_k, a.part = p->grad_part, a.counter = p->counter + p->counters;
-    a.B = batch, a.max_new = max_new, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.eps = p->cfg.rms_eps, a.err = p->err;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
     return cuda_status(p, launch_norm_rope_grad(a, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream), "prism_qk_norm_rope_backward");
 }
 
-prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, int32_t max_new, const prism_heads *q,
-                                const prism_heads *k, const prism_heads *v, const prism_heads *q_out, const void *g_q,
-                                const void *g_k, const float *rope, int32_t rope_len, const int32_t *pos,
-                                const int32_t *n_new, void *stream) {
-    if (!p) return fail(nullptr, PRISM_ERR_INVALID_ARG, "prism_paged_append: null handle");
+prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, const prism_rows *rows, void *stream) {
+    if (!p || !rows) return fail(p, PRISM_ERR_INVALID_ARG, "prism_paged_append: null argument");
     Check c{p};
-    NormRopeArgs a{};
+    NormRopeArgs a = c.rows<NormRopeArgs>(*rows);
     a.cache = c.cache(cache, "cache");
-    a.q = c.heads(q, "q");
-    a.k = c.heads(k, "k");
-    a.v = c.heads(v, "v");
-    a.q_out = c.heads(q_out, "q_out");
-    if (c.s == PRISM_OK) c.rows(cache->batch, max_new);
-    c.rope(rope, rope_len);
-    c.gains(g_q, g_k);
+    a.v = c.heads(rows->v, "v");
+    a.q_out = c.heads(rows->q_out, "q_out");
     if (c.s != PRISM_OK) return c.s;
-    a.g_q = g_q, a.g_k = g_k, a.rope = rope, a.n_new = n_new, a.rope_len = rope_len;
-    a.pos = pos ? pos : cache->kv_len;
-    a.B = cache->batch, a.max_new = max_new, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.eps = p->cfg.rms_eps, a.err = p->err;
+    c.need(rows->batch == cache->batch, PRISM_ERR_SHAPE, "the rows and the cache differ in batch");
+    if (c.s != PRISM_OK) return c.s;
+    if (!a.pos) a.pos = cache->kv_len;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
     return cuda_status(p, launch_norm_rope(a, p->bf16, p->cfg.head_dim, true, p->sms, (cudaStream_t)stream), "prism_paged_append");
@@ -316,7 +288,7 @@ prism_status prism_paged_evict(prism_paged *p, const prism_paged_cache *src, con
     a.kept = kept, a.B = src->batch, a.Hkv = p->cfg.n_kv_heads, a.budget = budget, a.sinks = sinks, a.recent = recent, a.err = p->err;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
-    return cuda_status(p, launch_paged_evict(a, p->cfg.head_dim * c.es(), (cudaStream_t)stream), "prism_paged_evict");
+    return cuda_status(p, launch_paged_evict(a, p->cfg.head_dim * c.es(), p->sms, (cudaStream_t)stream), "prism_paged_evict");
 }
 
 prism_status prism_paged_status(prism_paged *p, void *stream, int32_t *flags) {

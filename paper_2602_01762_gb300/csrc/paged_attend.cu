@@ -345,31 +345,48 @@ template <int D_, int NG> struct F32Tile {
     }
 };
 
-// The part of one (sequence, KV head, head tile) segment that a CTA works on:
-// blocks [blk0, blk1) of the segment's nblk.
-struct Piece {
-    int u, b, h, blk0, blk1, nblk, len;
+__device__ __forceinline__ int blocks_of(int len) { return max(1, (len + kAttendUnit - 1) / kAttendUnit); }
+
+// Walk over the pieces of a CTA's share: the blocks [blk0, blk1) of nblk of one
+// (sequence, KV head, head tile) segment after the other.  Each lane keeps the
+// length of one of the next 32 sequences, so that a step waits for no load.
+struct Pieces {
+    int u, u1, b, h, heads, blk0, blk1, nblk, len;
+    int base, lens;                      // lane i: rows of sequence base + i
+    __device__ __forceinline__ void fetch(const AttendArgs &a) {
+        const int at = b + (int)(threadIdx.x & 31);
+        base = b;
+        lens = at < a.B ? paged_len(a.cache, at, a.added, a.err) : 0;
+    }
+    __device__ __forceinline__ void sequence() {
+        len = __shfl_sync(0xFFFFFFFFu, lens, b - base);
+        nblk = blocks_of(len);
+    }
+    __device__ __forceinline__ void begin(const AttendArgs &a, const UnitRange &r, int n_heads) {
+        u = r.u0;
+        u1 = r.u1;
+        b = r.b;
+        heads = n_heads;
+        fetch(a);
+        sequence();
+        h = (u - r.first) / nblk;
+        blk0 = (u - r.first) % nblk;
+        blk1 = min(nblk, blk0 + u1 - u);
+    }
+    __device__ __forceinline__ bool next(const AttendArgs &a) {
+        u += blk1 - blk0;
+        if (u >= u1) return false;
+        blk0 = 0;
+        if (++h == heads) {
+            h = 0;
+            if (++b - base == 32) fetch(a);
+            sequence();
+        }
+        blk1 = min(nblk, u1 - u);
+        return true;
+    }
     __device__ __forceinline__ int rows() const { return min(blk1 * kAttendUnit, len) - blk0 * kAttendUnit; }
 };
-__device__ __forceinline__ int blocks_of(int len) { return max(1, (len + kAttendUnit - 1) / kAttendUnit); }
-__device__ __forceinline__ void piece_at(Piece &p, const AttendArgs &a, int u1) {
-    p.len = paged_len(a.cache, p.b, a.added, a.err);
-    p.nblk = blocks_of(p.len);
-    p.blk1 = min(p.nblk, p.blk0 + u1 - p.u);
-}
-__device__ __forceinline__ bool next_piece(Piece &p, const AttendArgs &a, int heads, int u1) {
-    p.u += p.blk1 - p.blk0;
-    if (p.u >= u1) return false;
-    p.blk0 = 0;
-    if (++p.h == heads) {
-        p.h = 0;
-        ++p.b;
-        piece_at(p, a, u1);
-    } else {
-        p.blk1 = min(p.nblk, u1 - p.u);
-    }
-    return true;
-}
 
 // Writes the result of heads h0 .. of one segment from its sums, maxima and totals.
 template <typename T, int D>
@@ -403,6 +420,9 @@ template <typename P>
 __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(AttendArgs a) {
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads;
+    constexpr int kJoin = kPaWarps * P::kMergeStride;    // pieces whose maxima the merge area holds
+    constexpr int kJoinCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;   // float4 columns of a thread
+    constexpr int kJoinEarly = 8 / kJoinCols, kJoinBatch = 12 / kJoinCols;
     constexpr int kPart = H * (D + 2);                   // floats of a piece: sums [H][D], then (maximum, sum) [H]
     constexpr int kRow = D * (int)sizeof(T), kChunks = kRow / 16, kRowsPer = 32 / kChunks;
     extern __shared__ __align__(128) unsigned char smem[];
@@ -422,37 +442,42 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     float *sm = merge + kPaWarps * H * P::kMergeStride, *sl = sm + kPaWarps * H;    // [warps][H]
     float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
 
-    Piece p;                                             // the piece being computed
-    p.b = r.b;
-    p.u = r.u0;
-    p.len = paged_len(a.cache, p.b, a.added, a.err);
-    p.nblk = blocks_of(p.len);
-    p.h = (r.u0 - r.first) / p.nblk;
-    p.blk0 = (r.u0 - r.first) % p.nblk;
-    p.blk1 = min(p.nblk, p.blk0 + r.u1 - p.u);
+    Pieces p;                                            // the piece being computed
+    p.begin(a, r, heads);
 
-    // Loads run ahead of the computation: their own piece, tile and page.
-    Piece f = p;
+    // Loads run ahead of the computation: their own walk, and the pool place of each
+    // lane's row of the next two tiles, so that no load waits for a block-table entry.
+    Pieces f = p;
     int ft = warp;
     bool more = true;
-    while (more && ft * KT >= f.rows()) more = next_piece(f, a, heads, r.u1);
-    int f_page = 0, f_row = 0;
-    bool f_in = false;
-    auto look_up = [&]() {                               // lane's row of tile ft (lanes past KT repeat)
-        const int key = f.blk0 * kAttendUnit + ft * KT + (lane % KT);
-        f_in = key < f.len;
-        const int slot = (unsigned)key / (unsigned)a.cache.page_size;
-        f_row = key - slot * a.cache.page_size;
-        if (f_in) f_page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
+    while (more && ft * KT >= f.rows()) more = f.next(a);
+    struct Place {
+        int page, row, head;
+        bool in, live;
     };
-    if (more) look_up();
+    auto look_up = [&]() {                               // lane's row of the walk's tile (lanes past KT repeat), then on
+        Place w{0, 0, f.h / tiles, false, more};
+        if (!more) return w;
+        const int key = f.blk0 * kAttendUnit + ft * KT + (lane % KT);
+        const int slot = (unsigned)key / (unsigned)a.cache.page_size;
+        w.in = key < f.len;
+        w.row = key - slot * a.cache.page_size;
+        if (w.in) w.page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
+        ft += kPaWarps;
+        while (more && ft * KT >= f.rows()) {
+            more = f.next(a);
+            ft = warp;
+        }
+        return w;
+    };
+    Place next0 = look_up(), next1 = look_up();
     int stage_in = 0;
     auto issue = [&]() {
-        if (more) {
-            const bool known = (unsigned)f_page < (unsigned)a.cache.n_pages;
-            if (f_in && !known) set_err(a.err, kErrPage);
-            const int ok = f_in && known;
-            const long long off = ok ? f_page * a.cache.page_stride + (f.h / tiles) * a.cache.head_stride + f_row * a.cache.row_stride : 0;
+        if (next0.live) {
+            const bool known = (unsigned)next0.page < (unsigned)a.cache.n_pages;
+            if (next0.in && !known) set_err(a.err, kErrPage);
+            const int ok = next0.in && known;
+            const long long off = ok ? next0.page * a.cache.page_stride + next0.head * a.cache.head_stride + next0.row * a.cache.row_stride : 0;
             const uint32_t ks = ring + stage_in * kPaStage, vs = ks + kPaStage / 2;
             const int c = lane % kChunks;
 #pragma unroll
@@ -463,14 +488,10 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                 cp16(ks + P::piece(row, c), a.cache.k + at, in);
                 cp16(vs + P::piece(row, c), a.cache.v + at, in);
             }
-            ft += kPaWarps;
-            while (more && ft * KT >= f.rows()) {
-                more = next_piece(f, a, heads, r.u1);
-                ft = warp;
-            }
-            if (more) look_up();
         }
         cp_group();
+        next0 = next1;
+        next1 = look_up();
         stage_in = stage_in + 1 == S ? 0 : stage_in + 1;
     };
 #pragma unroll
@@ -479,10 +500,12 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     int stage = 0;
     P state;
     bool go = true;
+    auto first_head = [&](const Pieces &w) { return (long long)w.b * a.Hq + w.h / tiles * G + w.h % tiles * H; };
+    auto head_count = [&](const Pieces &w) { return min(H, G - w.h % tiles * H); };
+    state.load_q((const T *)a.q + first_head(p) * D, head_count(p));
     while (go) {
-        const int kvh = p.h / tiles, h0 = (p.h % tiles) * H, n = min(H, G - h0);
-        const long long hq = (long long)p.b * a.Hq + kvh * G + h0;
-        state.load_q((const T *)a.q + hq * D, n);
+        const int kvh = p.h / tiles, h0 = (p.h % tiles) * H, n = head_count(p);
+        const long long hq = first_head(p);
         state.reset();
         float *scores = a.scores ? a.scores + ((long long)p.b * a.Hkv + kvh) * G * a.cache.table_pages * a.cache.page_size +
                                        (long long)h0 * a.cache.table_pages * a.cache.page_size : nullptr;
@@ -495,6 +518,9 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
             state.tile(ks, ks + kPaStage / 2, own, p.blk0 * kAttendUnit + t * KT, p.len, a.scale_log2, scores, n);
             stage = stage + 1 == S ? 0 : stage + 1;
         }
+        Pieces after = p;
+        go = after.next(a);
+        if (go) state.load_q((const T *)a.q + first_head(after) * D, head_count(after));   // on its way during the merge
         state.store(own, sm + warp * H, sl + warp * H);
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
@@ -531,38 +557,90 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
             }
         }
         if (!whole) {
-            __threadfence();
-            __syncthreads();
-            if (tid == 0) last = atomicAdd(a.counter + seg, 1) == c1 - c0;
+            __syncthreads();                             // the piece is written; the merge area was read
+            if (tid == 0) {
+                __threadfence();
+                last = atomicAdd(a.counter + seg, 1) == c1 - c0;
+                __threadfence();
+            }
             __syncthreads();
             if (last) {
-                __threadfence();
                 // piece i of the segment: CTA c0's second slot, the others' first
                 auto piece_part = [&](int i) { return a.part + (long long)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * kPart; };
-                for (int e = tid; e < n * (D / 4); e += kPaThreads) {
-                    const int h = e / (D / 4), d = 4 * (e % (D / 4));
-                    float M = -INFINITY, x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
-#pragma unroll 4
-                    for (int i = 0; i <= c1 - c0; ++i) M = fmaxf(M, __ldcg(piece_part(i) + H * D + 2 * h));
-                    const float base = base_of(M);
-#pragma unroll 4
-                    for (int i = 0; i <= c1 - c0; ++i) {
-                        const float *q = piece_part(i);
-                        const float4 y = __ldcg((const float4 *)(q + h * D + d));
-                        const float k = exp2f(__ldcg(q + H * D + 2 * h) - base);
-                        L = fmaf(k, __ldcg(q + H * D + 2 * h + 1), L);
-                        x[0] = fmaf(k, y.x, x[0]);
-                        x[1] = fmaf(k, y.y, x[1]);
-                        x[2] = fmaf(k, y.z, x[2]);
-                        x[3] = fmaf(k, y.w, x[3]);
+                const int pieces = c1 - c0 + 1;
+                float4 early[kJoinCols][kJoinEarly];     // the first pieces' sums come with the maxima
+#pragma unroll
+                for (int c = 0; c < kJoinCols; ++c)
+#pragma unroll
+                    for (int i = 0; i < kJoinEarly; ++i)
+                        if (i < pieces && tid + c * kPaThreads < n * (D / 4)) early[c][i] = __ldcg((const float4 *)piece_part(i) + tid + c * kPaThreads);
+                float *top = merge;                      // [kJoin][H]: maxima of kJoin pieces at a time
+                for (int h = warp; h < n; h += kPaWarps) {
+                    float M = -INFINITY, L = 0.f;
+                    for (int i = lane; i < pieces; i += 32) {
+                        const float2 ml = __ldcg((const float2 *)(piece_part(i) + H * D + 2 * h));
+                        if (i < kJoin) top[i * H + h] = ml.x;
+                        const float m = fmaxf(M, ml.x);
+                        L = L * exp2f(M - base_of(m)) + exp2f(ml.x - base_of(m)) * ml.y;
+                        M = m;
                     }
-                    write_out<T, D>(a, hq + h, d, x, M, L);
+#pragma unroll
+                    for (int o = 16; o > 0; o >>= 1) {
+                        const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, o), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, o);
+                        const float m = fmaxf(M, m2);
+                        L = L * exp2f(M - base_of(m)) + l2 * exp2f(m2 - base_of(m));
+                        M = m;
+                    }
+                    if (lane == 0) sm[h] = M, sl[h] = L;
+                }
+                __syncthreads();
+                float x[kJoinCols][4] = {};
+                for (int i0 = 0; i0 < pieces; i0 += kJoin) {
+                    const int count = min(kJoin, pieces - i0);
+                    if (i0 > 0) {
+                        __syncthreads();
+                        for (int e = tid; e < count * n; e += kPaThreads)
+                            top[e / n * H + e % n] = __ldcg(piece_part(i0 + e / n) + H * D + 2 * (e % n));
+                        __syncthreads();
+                    }
+#pragma unroll
+                    for (int c = 0; c < kJoinCols; ++c) {
+                        const int e = tid + c * kPaThreads, h = e / (D / 4);
+                        if (h >= n) continue;
+                        const float base = base_of(sm[h]);
+                        auto add = [&](int i, const float4 &y) {
+                            const float k = exp2f(top[i * H + h] - base);
+                            x[c][0] = fmaf(k, y.x, x[c][0]);
+                            x[c][1] = fmaf(k, y.y, x[c][1]);
+                            x[c][2] = fmaf(k, y.z, x[c][2]);
+                            x[c][3] = fmaf(k, y.w, x[c][3]);
+                        };
+                        if (i0 == 0) {
+#pragma unroll
+                            for (int i = 0; i < kJoinEarly; ++i)
+                                if (i < count) add(i, early[c][i]);
+                        }
+                        for (int i = i0 == 0 ? kJoinEarly : 0; i < count; i += kJoinBatch) {
+                            float4 y[kJoinBatch];
+#pragma unroll
+                            for (int k = 0; k < kJoinBatch; ++k)
+                                if (i + k < count) y[k] = __ldcg((const float4 *)piece_part(i0 + i + k) + e);
+#pragma unroll
+                            for (int k = 0; k < kJoinBatch; ++k)
+                                if (i + k < count) add(i + k, y[k]);
+                        }
+                    }
+                }
+#pragma unroll
+                for (int c = 0; c < kJoinCols; ++c) {
+                    const int e = tid + c * kPaThreads, h = e / (D / 4);
+                    if (h < n) write_out<T, D>(a, hq + h, 4 * (e % (D / 4)), x[c], sm[h], sl[h]);
                 }
                 if (tid == 0) a.counter[seg] = 0;
             }
         }
         __syncthreads();                                 // the merge area is free again
-        go = next_piece(p, a, heads, r.u1);
+        p = after;
     }
     cp_wait_group<0>();
 }
@@ -570,42 +648,64 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 // weights[j] += sum_h 2^(s_jh - M_h) / L_h from the scores the attention kernel
 // left, heads in order; one thread per (KV head, row).
 constexpr int kWtThreads = 256;
+constexpr int kWtRows = 2 * kWtThreads;  // rows per unit: two a thread, their loads side by side
 __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a, int head_tile) {
-    pdl_wait();
-    pdl_trigger();
-    const int G = a.Hq / a.Hkv;
-    constexpr int kRows = 4 * kAttendUnit;
-    auto blocks = [&](int b) { return max(1, (paged_len(a.cache, b, a.added, nullptr) + kRows - 1) / kRows); };
+    pdl_trigger();                       // before the wait: the attention's own wait has made kv_len final
+    auto rows = [&](int b) { return paged_len(a.cache, b, a.added, nullptr); };
+    auto blocks = [&](int b) { return max(1, (rows(b) + kWtRows - 1) / kWtRows); };
     UnitRange r;
-    if (!unit_range<kWtThreads>(r, a.B, a.Hkv, 1, blocks)) return;
-    int b = r.b, len = paged_len(a.cache, b, a.added, nullptr), nblk = blocks(b);
+    const bool any = unit_range<kWtThreads>(r, a.B, a.Hkv, 1, blocks);
+    pdl_wait();
+    if (!any) return;
+    const int G = a.Hq / a.Hkv;
+    int b = r.b, len = rows(b), nblk = blocks(b);
     int h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
     for (int u = r.u0; u < r.u1; ++u) {
-        for (int j = blk * kRows + threadIdx.x; j < min(len, (blk + 1) * kRows); j += kWtThreads) {
+        const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
+        const float2 *st = a.stat + (long long)b * a.Hq + h * G;
+        float *to[2];
+        float w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int j = blk * kWtRows + i * kWtThreads + threadIdx.x;
+            to[i] = nullptr;
+            w[i] = 0.f;
+            if (j >= len) continue;
             const int slot = j / a.cache.page_size;
             const int page = a.cache.table[(long long)b * a.cache.table_pages + slot];
-            if ((unsigned)page >= (unsigned)a.cache.n_pages) continue;   // reported by the attention
-            const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
-            const float2 *st = a.stat + (long long)b * a.Hq + h * G;
-            float w = 0.f;
-            for (int t = 0; t < G; t += head_tile) {
-                const int n = min(head_tile, G - t);
-                const float *z = s + t * cap + (long long)j * n;
-                for (int i = 0; i < n; ++i) {
-                    const float2 ml = st[t + i];
-                    w = fmaf(exp2f(z[i] - ml.x), ml.y, w);
+            if ((unsigned)page < (unsigned)a.cache.n_pages)   // else reported by the attention
+                to[i] = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
+        }
+        for (int t = 0; t < G; t += head_tile) {
+            const int n = min(head_tile, G - t);
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                if (!to[i]) continue;
+                const float *z = s + t * cap + (long long)(blk * kWtRows + i * kWtThreads + threadIdx.x) * n;
+                auto add = [&](float x, int k) {
+                    const float2 ml = st[t + k];
+                    w[i] = fmaf(exp2f(x - ml.x), ml.y, w[i]);
+                };
+                if (n % 4 == 0) {
+                    for (int k = 0; k < n; k += 4) {
+                        const float4 x = *(const float4 *)(z + k);
+                        add(x.x, k), add(x.y, k + 1), add(x.z, k + 2), add(x.w, k + 3);
+                    }
+                } else {
+                    for (int k = 0; k < n; ++k) add(z[k], k);
                 }
             }
-            float *to = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
-            *to += w;
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            if (to[i]) *to[i] += w[i];
         if (++blk == nblk) {
             blk = 0;
             if (++h == a.Hkv) {
                 h = 0;
                 if (++b < a.B) {
-                    len = paged_len(a.cache, b, a.added, nullptr);
+                    len = rows(b);
                     nblk = blocks(b);
                 }
             }
@@ -655,7 +755,7 @@ cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, 
         return launch_k(paged_attend_kernel<P>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
     });
     if (e != cudaSuccess || !a.scores) return e;
-    const long long chunks = a.B * (long long)a.Hkv * ((cap + 4 * kAttendUnit - 1) / (4 * kAttendUnit));
+    const long long chunks = a.B * (long long)a.Hkv * ((cap + kWtRows - 1) / kWtRows);
     const int wt = (int)(chunks < sms * 8 ? chunks : sms * 8);
     return launch_k(paged_weights_kernel, dim3(wt), dim3(kWtThreads), 0, s, true, a, ht);
 }

@@ -15,6 +15,8 @@ namespace {
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
+constexpr int kEvBatch = 8;              // rows a thread has in flight
+constexpr uint32_t kNan = 0x7FFFFFFFu;
 constexpr int kEvCached = 48 * 1024;     // rows whose keys shared memory holds
 
 // Weight as an unsigned key with the same order: NaN 0, then -inf ... +inf; -0 as +0.
@@ -24,77 +26,125 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
     return (u & 0x80000000u) ? ~u : (u | 0x80000000u);
 }
 
-// One CTA per (sequence, KV head): radix selection of the smallest kept key, eight
-// bits a pass over the keys in shared memory (read from the pool again where there
-// are more than it holds), then the kept slots in order.
-__global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, int cached) {
+// One cluster of cs CTAs per (sequence, KV head), each with a contiguous share of
+// the rows: radix selection of the smallest kept key, eight bits a pass over the
+// keys in shared memory (read from the pool again where a share is more than it
+// holds), the shares' histograms added into every CTA's through distributed shared
+// memory; then the kept slots in order.
+__global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, int cs, int cached) {
     extern __shared__ uint32_t keys[];
-    __shared__ int hist[256], pick[2], warp_eq[kEvWarps], warp_gt[kEvWarps];
+    __shared__ __align__(16) int hist[4][256], total[4][256];   // this share's counts of each pass; the cluster's
+    __shared__ int warp_eq[kEvWarps], warp_gt[kEvWarps], share_eq[8], share_gt[8], pick[2];
     pdl_wait();
     pdl_trigger();
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-    const int b = blockIdx.x / a.Hkv, h = blockIdx.x % a.Hkv;
+    const int row = blockIdx.x / cs, rank = blockIdx.x % cs;
+    const int b = row / a.Hkv, h = row % a.Hkv;
     const int len = paged_len(a.src, b, 0, a.err);
-    int32_t *kept = a.kept + (long long)blockIdx.x * a.budget;
-    if (len <= a.budget) {
-        for (int j = tid; j < a.budget; j += kEvThreads) kept[j] = j < len ? j : -1;
+    int32_t *kept = a.kept + (long long)row * a.budget;
+    if (len <= a.budget) {               // the same for the whole cluster
+        for (int j = rank * kEvThreads + tid; j < a.budget; j += cs * kEvThreads) kept[j] = j < len ? j : -1;
         return;
     }
     const int first = a.sinks, want = a.budget - a.recent - first;
     const int n = want > 0 ? len - a.recent - first : 0;   // rows to choose from, more than want (none to choose: 0)
+    const int share = ((n + cs - 1) / cs + 31) & ~31, s0 = min(n, rank * share), m = min(n, s0 + share) - s0;
     const int32_t *table = a.src.table + (long long)b * a.src.table_pages;
-    auto load = [&](int i) {
-        const int slot = first + i, idx = slot / a.src.page_size, page = table[idx];
-        if ((unsigned)page >= (unsigned)a.src.n_pages) return 0u;      // reported by the copy if it is kept
-        return weight_key(a.src.weights[((long long)page * a.Hkv + h) * a.src.page_size + slot - idx * a.src.page_size]);
+    // Keys of kEvBatch rows of this share, kEvThreads apart: their table entries
+    // together, then their weights together.
+    auto load = [&](int i, uint32_t (&k)[kEvBatch]) {
+        int page[kEvBatch], off[kEvBatch];
+#pragma unroll
+        for (int u = 0; u < kEvBatch; ++u) {
+            const int slot = first + s0 + i + u * kEvThreads, idx = slot / a.src.page_size;
+            off[u] = slot - idx * a.src.page_size;
+            page[u] = i + u * kEvThreads < m ? table[idx] : -1;
+        }
+#pragma unroll
+        for (int u = 0; u < kEvBatch; ++u)                 // a bad entry is reported by the copy if its row is kept
+            k[u] = (unsigned)page[u] < (unsigned)a.src.n_pages
+                       ? __float_as_uint(a.src.weights[((long long)page[u] * a.Hkv + h) * a.src.page_size + off[u]])
+                       : kNan;
+#pragma unroll
+        for (int u = 0; u < kEvBatch; ++u) k[u] = weight_key(__uint_as_float(k[u]));
     };
-    const bool held = n <= cached;
-    auto key = [&](int i) { return held ? keys[i] : load(i); };
+    const bool held = share <= cached;
+    // f(key) for every row of this share
+    auto each = [&](auto f) {
+        for (int i0 = 0; i0 < m; i0 += kEvBatch * kEvThreads) {
+            uint32_t k[kEvBatch];
+            if (!held) load(i0 + tid, k);
+#pragma unroll
+            for (int u = 0; u < kEvBatch; ++u) {
+                const int i = i0 + u * kEvThreads + tid;
+                if (i < m) f(held ? keys[i] : k[u]);
+            }
+        }
+    };
     if (held)
-        for (int i = tid; i < n; i += kEvThreads) keys[i] = load(i);
+        for (int i0 = tid; i0 < m; i0 += kEvBatch * kEvThreads) {
+            uint32_t k[kEvBatch];
+            load(i0, k);
+#pragma unroll
+            for (int u = 0; u < kEvBatch; ++u)
+                if (i0 + u * kEvThreads < m) keys[i0 + u * kEvThreads] = k[u];
+        }
+    hist[tid >> 8][tid & 255] = total[tid >> 8][tid & 255] = 0;
+    static_assert(kEvThreads == 4 * 256, "a thread per counter");
+    cluster_sync_all();                  // every CTA's counts are clear before another adds to them
     uint32_t prefix = 0, mask = 0;
     int need = want;                     // rows still to be taken of those that match the prefix
-    for (int shift = 24; shift >= 0 && need > 0; shift -= 8) {
-        if (tid < 256) hist[tid] = 0;
-        __syncthreads();
-        for (int i0 = 0; i0 < n; i0 += kEvThreads) {
-            const int i = i0 + tid;
-            const uint32_t k = i < n ? key(i) : 0u;
-            const bool in = i < n && (k & mask) == prefix;
-            const uint32_t bin = in ? (k >> shift) & 255u : 256u;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, bin);
-            if (in && lane == __ffs(same) - 1) atomicAdd(hist + bin, __popc(same));
-        }
-        __syncthreads();
-        if (warp == 0) {                 // the bin in which the need-th largest lies
-            int c[8], s = 0;
-#pragma unroll
-            for (int e = 0; e < 8; ++e) s += c[e] = hist[255 - (8 * lane + e)];
-            int up = s;
-#pragma unroll
-            for (int o = 1; o < 32; o <<= 1) {
-                const int t = __shfl_up_sync(0xFFFFFFFFu, up, o);
-                if (lane >= o) up += t;
+    if (n > 0) {
+#pragma unroll 1
+        for (int pass = 0; pass < 4; ++pass) {
+            const int shift = 24 - 8 * pass;
+            each([&](uint32_t k) {
+                if ((k & mask) == prefix) atomicAdd(&hist[pass][(k >> shift) & 255u], 1);
+            });
+            __syncthreads();
+            if (cs > 1) {
+                const int c = tid < 256 ? hist[pass][tid] : 0;
+                if (c)
+                    for (int r = 0; r < cs; ++r) dsmem_add(&total[pass][tid], r, c);
+                cluster_sync_all();
             }
-            int above = up - s;
-            if (above < need && need <= up) {
+            if (warp == 0) {             // the bin of the need-th largest; lane's bins are 255 - 8 lane and the seven below
+                const int *t = (cs > 1 ? total : hist)[pass] + 248 - 8 * lane;
+                const int4 hi = *(const int4 *)(t + 4), lo = *(const int4 *)t;
+                const int c[8] = {hi.w, hi.z, hi.y, hi.x, lo.w, lo.z, lo.y, lo.x};
+                const int s = hi.w + hi.z + hi.y + hi.x + lo.w + lo.z + lo.y + lo.x;
+                int up = s;
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    if (above < need && need <= above + c[e]) {
-                        pick[0] = 255 - (8 * lane + e);
-                        pick[1] = above;
+                for (int o = 1; o < 32; o <<= 1) {
+                    const int t = __shfl_up_sync(0xFFFFFFFFu, up, o);
+                    if (lane >= o) up += t;
+                }
+                int above = up - s;
+                if (above < need && need <= up) {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (above < need && need <= above + c[e]) {
+                            pick[0] = 255 - (8 * lane + e);
+                            pick[1] = above;
+                        }
+                        above += c[e];
                     }
-                    above += c[e];
                 }
             }
+            __syncthreads();
+            prefix |= (uint32_t)pick[0] << shift;
+            need -= pick[1];
+            mask |= 255u << shift;
         }
-        __syncthreads();
-        prefix |= (uint32_t)pick[0] << shift;
-        mask |= 255u << shift;
-        need -= pick[1];
     }
     // the prefix is now that key: larger keys are kept, and the first `need` equal ones
-    const int per = ((n + kEvWarps - 1) / kEvWarps + 31) & ~31, lo = min(n, warp * per), hi = min(n, lo + per);
+    const int per = ((m + kEvWarps - 1) / kEvWarps + 31) & ~31, lo = min(m, warp * per), hi = min(m, lo + per);
+    auto key = [&](int i) {
+        if (held) return keys[i];
+        const int slot = first + s0 + i, idx = slot / a.src.page_size, page = table[idx];
+        if ((unsigned)page >= (unsigned)a.src.n_pages) return weight_key(__uint_as_float(kNan));
+        return weight_key(a.src.weights[((long long)page * a.Hkv + h) * a.src.page_size + slot - idx * a.src.page_size]);
+    };
     int gt = 0, eq = 0;
     for (int i = lo + lane; i < hi; i += 32) {
         const uint32_t k = key(i);
@@ -105,27 +155,35 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, i
     eq = __reduce_add_sync(0xFFFFFFFFu, eq);
     if (lane == 0) warp_gt[warp] = gt, warp_eq[warp] = eq;
     __syncthreads();
+    if (warp == 0) {
+        const int g = __reduce_add_sync(0xFFFFFFFFu, warp_gt[lane]), e = __reduce_add_sync(0xFFFFFFFFu, warp_eq[lane]);
+        if (lane < cs) dsmem_st(&share_gt[rank], lane, g), dsmem_st(&share_eq[rank], lane, e);
+    }
+    static_assert(kEvWarps == 32, "one lane per warp");
+    cluster_sync_all();
     gt = eq = 0;
+    for (int r = 0; r < rank; ++r) gt += share_gt[r], eq += share_eq[r];
     for (int w = 0; w < warp; ++w) gt += warp_gt[w], eq += warp_eq[w];
     for (int i0 = lo; i0 < hi; i0 += 32) {
         const int i = i0 + lane;
         const uint32_t k = i < hi ? key(i) : 0u;
         const bool is_gt = i < hi && k > prefix, is_eq = i < hi && k == prefix;
         const uint32_t bg = __ballot_sync(0xFFFFFFFFu, is_gt), be = __ballot_sync(0xFFFFFFFFu, is_eq), below = (1u << lane) - 1u;
-        const int rank = eq + __popc(be & below);
-        if (is_gt || (is_eq && rank < need)) kept[first + gt + __popc(bg & below) + min(rank, need)] = first + i;
+        const int rank_eq = eq + __popc(be & below);
+        if (is_gt || (is_eq && rank_eq < need)) kept[first + gt + __popc(bg & below) + min(rank_eq, need)] = first + s0 + i;
         gt += __popc(bg);
         eq += __popc(be);
     }
-    for (int j = tid; j < first; j += kEvThreads) kept[j] = j;
-    for (int j = tid; j < a.recent; j += kEvThreads) kept[first + want + j] = len - a.recent + j;
+    for (int j = rank * kEvThreads + tid; j < first; j += cs * kEvThreads) kept[j] = j;
+    for (int j = rank * kEvThreads + tid; j < a.recent; j += cs * kEvThreads) kept[first + want + j] = len - a.recent + j;
 }
 
-// Copies the kept rows of K, V and the weights, 32 destination rows of one KV head
-// per warp: each lane looks one row up, then the warp moves them 512 bytes at a
-// time.  Also sets the destination's lengths.
+// Copies the kept rows of K, V and the weights, kCpRows destination rows of one KV
+// head per warp: a lane each looks the rows up, then the warp moves them 512 bytes
+// at a time.  Also sets the destination's lengths.
 constexpr int kCpThreads = 256;
-constexpr int kCpUnroll = 8;
+constexpr int kCpRows = 8;
+constexpr int kCpUnroll = 4;
 __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int row_bytes) {
     pdl_wait();
     pdl_trigger();
@@ -133,12 +191,12 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
     const long long gid = (long long)blockIdx.x * kCpThreads + threadIdx.x;
     for (long long b = gid; b < a.B; b += (long long)gridDim.x * kCpThreads)
         a.dst.kv_len[b] = min(paged_len(a.src, (int)b, 0, nullptr), a.budget);
-    const int chunks = (a.budget + 31) / 32;
+    const int chunks = (a.budget + kCpRows - 1) / kCpRows;
     const long long w = gid >> 5;
     const long long bh = w / chunks;
     if (bh >= (long long)a.B * a.Hkv) return;
-    const int b = (int)(bh / a.Hkv), h = (int)(bh - (long long)b * a.Hkv), j = (int)(w - bh * chunks) * 32 + lane;
-    const int slot = j < a.budget ? a.kept[bh * a.budget + j] : -1;
+    const int b = (int)(bh / a.Hkv), h = (int)(bh - (long long)b * a.Hkv), j = (int)(w - bh * chunks) * kCpRows + lane;
+    const int slot = lane < kCpRows && j < a.budget ? a.kept[bh * a.budget + j] : -1;
     bool ok = slot >= 0;
     long long from = 0, to = 0;
     if (ok) {
@@ -155,7 +213,7 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
     const int per = row_bytes / 16, both = 2 * per;      // 16-byte pieces of a K row, of a K and a V row
     const uint32_t rows = __ballot_sync(0xFFFFFFFFu, ok);
     if (!rows) return;
-    for (int c0 = 0; c0 < 32 * both; c0 += 32 * kCpUnroll) {
+    for (int c0 = 0; c0 < kCpRows * both; c0 += 32 * kCpUnroll) {
         uint4 x[kCpUnroll];
         char *dst[kCpUnroll];
 #pragma unroll
@@ -178,12 +236,36 @@ cudaError_t prepare_evict_kernels() {
     return cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvCached * 4);
 }
 
-cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, cudaStream_t s) {
+// CTAs per (sequence, KV head) of the selection: as many as give every SM two, up
+// to the portable cluster size, each with 8192 rows or more of the table.
+static int select_cluster(int rows, long long cap, int sms) {
+    int cs = 8;
+    while (cs > 1 && (rows * cs > 2 * sms || cap < 8192LL * cs)) cs >>= 1;
+    return cs;
+}
+
+cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s) {
     const long long cap = (long long)a.src.table_pages * a.src.page_size;
-    const int cached = (int)(cap < kEvCached ? cap : kEvCached);
-    cudaError_t e = launch_k(evict_select_kernel, dim3(a.B * a.Hkv), dim3(kEvThreads), (size_t)cached * 4, s, true, a, cached);
+    const int cs = select_cluster(a.B * a.Hkv, cap, sms);
+    const long long share = (cap + cs - 1) / cs + 32;
+    const int cached = (int)(share < kEvCached ? share : kEvCached);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(a.B * a.Hkv * cs);
+    cfg.blockDim = dim3(kEvThreads);
+    cfg.dynamicSmemBytes = (size_t)cached * 4;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cs;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel, a, cs, cached);
     if (e != cudaSuccess) return e;
-    const long long warps = (long long)a.B * a.Hkv * ((a.budget + 31) / 32);
+    const long long warps = (long long)a.B * a.Hkv * ((a.budget + kCpRows - 1) / kCpRows);
     return launch_k(evict_copy_kernel, dim3((unsigned)((warps * 32 + kCpThreads - 1) / kCpThreads)), dim3(kCpThreads), 0, s, true, a, row_bytes);
 }
 

@@ -29,6 +29,7 @@ on another stream than the one it was allocated on needs the caller's
 from __future__ import annotations
 
 import ctypes
+import struct
 
 import torch
 
@@ -49,19 +50,21 @@ class _Cache(ctypes.Structure):
                 ("batch", _i32)]
 
 
-class _Heads(ctypes.Structure):
-    _fields_ = [("data", _vp), ("batch_stride", _i64), ("row_stride", _i64), ("head_stride", _i64)]
+# prism_rows (five strided tensors of four words, five addresses, three sizes) and
+# prism_row_grads (four strided tensors, two addresses)
+_ROWS, _GRADS = struct.Struct("=20q5Q3i4x"), struct.Struct("=16q2Q")
+_NONE = (0, 0, 0, 0)
 
 
 def bind(lib: ctypes.CDLL) -> None:
     """Argument and result types of the paged entry points."""
     P = ctypes.POINTER
-    H, C = P(_Heads), P(_Cache)
+    C = P(_Cache)
     lib.prism_paged_create.argtypes = [P(_PagedConfig), _i32, P(_vp)]
     lib.prism_paged_destroy.argtypes = [_vp]
-    lib.prism_qk_norm_rope.argtypes = [_vp, _i32, _i32, H, H, H, H, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
-    lib.prism_qk_norm_rope_backward.argtypes = [_vp, _i32, _i32] + [H] * 6 + [_vp, _vp, _vp, _i32] + [_vp] * 5
-    lib.prism_paged_append.argtypes = [_vp, C, _i32, H, H, H, H, _vp, _vp, _vp, _i32, _vp, _vp, _vp]
+    lib.prism_qk_norm_rope.argtypes = [_vp, _vp, _vp]
+    lib.prism_qk_norm_rope_backward.argtypes = [_vp, _vp, _vp, _vp]
+    lib.prism_paged_append.argtypes = [_vp, C, _vp, _vp]
     lib.prism_paged_attend.argtypes = [_vp, C, _i32, _vp, _vp, _vp, _vp]
     lib.prism_paged_evict.argtypes = [_vp, C, C, _i32, _i32, _i32, _vp, _vp]
     lib.prism_paged_status.argtypes = [_vp, _vp, P(_i32)]
@@ -84,8 +87,8 @@ class PagedCache:
     """A paged cache bound by :meth:`PagedAttention.cache`: its tensors, checked
     once, and the struct the calls pass on."""
 
-    def __init__(self, struct, tensors, batch, rows, dtype, device, heads):
-        self.struct, self.ref = struct, ctypes.byref(struct)
+    def __init__(self, fields, tensors, batch, rows, dtype, device, heads):
+        self.fields, self.ref = fields, ctypes.byref(fields)
         self.k_pages, self.v_pages, self.block_table, self.kv_len, self.weights = tensors
         self.batch, self.rows = batch, rows          # sequences; rows a block-table line holds
         self.key = (dtype, device, heads)
@@ -116,6 +119,9 @@ class PagedAttention:
         h = _vp()
         self._check(self.lib.prism_paged_create(ctypes.byref(cfg), device, ctypes.byref(h)))
         self.h = h
+        self._index = self.device.index
+        self._rows, self._grads = ctypes.create_string_buffer(_ROWS.size), ctypes.create_string_buffer(_GRADS.size)
+        self._rows_at, self._grads_at = ctypes.addressof(self._rows), ctypes.addressof(self._grads)
         self._key = (self.tdtype, self.device, (n_kv_heads, page_size, head_dim))
 
     # ------------------------------------------------------------ checks
@@ -128,36 +134,40 @@ class PagedAttention:
         """Address of a dense tensor of this device, shape and type."""
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name}: expected a torch.Tensor")
-        if t.dtype is not dtype or t.shape != shape or t.device != self.device or not t.is_contiguous():
+        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
             raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)} on {self.device}, got {t.dtype} "
                              f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
         return t.data_ptr()
 
-    def _heads(self, t, batch, rows, heads, name):
-        """A [batch, rows, heads, D] tensor, strided but for D."""
-        if not isinstance(t, torch.Tensor):
+    def _heads(self, t, shape, name):
+        """Address and strides of a [batch, rows, heads, D] tensor, D dense."""
+        if isinstance(t, torch.Tensor):
+            s = t.stride()
+            if t.shape == shape and s[3] == 1 and t.dtype is self.tdtype and t.get_device() == self._index:
+                return t.data_ptr(), s[0], s[1], s[2]
+        else:
             raise TypeError(f"{name}: expected a torch.Tensor")
-        if t.dtype is not self.tdtype or t.shape != (batch, rows, heads, self.head_dim) or t.device != self.device:
-            raise ValueError(f"{name}: expected {self.tdtype} {(batch, rows, heads, self.head_dim)} on {self.device}, got "
-                             f"{t.dtype} {tuple(t.shape)} on {t.device}")
-        s = t.stride()
-        if s[3] != 1:
-            raise ValueError(f"{name}: the head dimension must be dense")
-        return _Heads(t.data_ptr(), s[0], s[1], s[2])
+        raise ValueError(f"{name}: expected {self.tdtype} {shape} on {self.device} with a dense head dimension, got {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
 
-    def _gain(self, g, name):
-        return None if g is None else self._tensor(g, (self.head_dim,), self.tdtype, name)
-
-    def _rope(self, rope):
+    def _pack(self, shape_q, shape_k, q, k, v, q_out, k_out, rope, pos, g_q, g_k, n_new):
+        """Checks a block of rows and writes its prism_rows."""
+        i32, B, D = torch.int32, shape_q[0], self.head_dim
         n = rope.shape[0]
-        return self._tensor(rope, (n, 2, self.head_dim // 2), torch.float32, "rope"), n
-
-    def _counts(self, t, batch, name):
-        return None if t is None else self._tensor(t, (batch,), torch.int32, name)
+        _ROWS.pack_into(
+            self._rows, 0, *self._heads(q, shape_q, "q"), *self._heads(k, shape_k, "k"),
+            *(_NONE if v is None else self._heads(v, shape_k, "v")),
+            *(_NONE if q_out is None else self._heads(q_out, shape_q, "q_out")),
+            *(_NONE if k_out is None else self._heads(k_out, shape_k, "k_out")),
+            0 if g_q is None else self._tensor(g_q, (D,), self.tdtype, "g_q"),
+            0 if g_k is None else self._tensor(g_k, (D,), self.tdtype, "g_k"),
+            self._tensor(rope, (n, 2, D // 2), torch.float32, "rope"),
+            0 if pos is None else self._tensor(pos, (B,), i32, "pos"),
+            0 if n_new is None else self._tensor(n_new, (B,), i32, "n_new"), n, B, shape_q[1])
 
     def _stream(self, stream):
         if stream is None:
-            return torch.cuda.current_stream(self.device).cuda_stream
+            return torch._C._cuda_getCurrentRawStream(self._index)
         return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
     def _bound(self, cache):
@@ -189,21 +199,21 @@ class PagedAttention:
         if weights is not None:
             self._tensor(weights, (n_pages, self.n_kv_heads, self.page_size), torch.float32, "weights")
         s = k_pages.stride()
-        struct = _Cache(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2],
+        fields = _Cache(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2],
                         None if weights is None else weights.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
                         n_pages, pages, batch)
-        return PagedCache(struct, (k_pages, v_pages, block_table, kv_len, weights), batch, pages * self.page_size, *self._key)
+        return PagedCache(fields, (k_pages, v_pages, block_table, kv_len, weights), batch, pages * self.page_size, *self._key)
+
+    def _shapes(self, B, n):
+        return (B, n, self.n_q_heads, self.head_dim), (B, n, self.n_kv_heads, self.head_dim)
 
     def qk_norm_rope(self, q, k, q_out, k_out, rope, pos, g_q=None, g_k=None, n_new=None, stream=None):
         """``prism_qk_norm_rope``: q, q_out [B, n, Hq, D]; k, k_out [B, n, Hkv, D]
         (strided but for D); rope fp32 [positions, 2, D / 2]; pos, n_new int32 [B]."""
         B, n = q.shape[:2]
-        sq, sk = self._heads(q, B, n, self.n_q_heads, "q"), self._heads(k, B, n, self.n_kv_heads, "k")
-        oq, ok = self._heads(q_out, B, n, self.n_q_heads, "q_out"), self._heads(k_out, B, n, self.n_kv_heads, "k_out")
-        table, length = self._rope(rope)
-        self._check(self.lib.prism_qk_norm_rope(
-            self.h, B, n, sq, sk, oq, ok, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), table, length,
-            self._counts(pos, B, "pos"), self._counts(n_new, B, "n_new"), self._stream(stream)))
+        sq, sk = self._shapes(B, n)
+        self._pack(sq, sk, q, k, None, q_out, k_out, rope, pos, g_q, g_k, n_new)
+        self._check(self.lib.prism_qk_norm_rope(self.h, self._rows_at, self._stream(stream)))
 
     def qk_norm_rope_backward(self, dq_out, dk_out, q, k, dq, dk, rope, pos, g_q=None, g_k=None, dg_q=None, dg_k=None,
                               n_new=None, stream=None):
@@ -211,28 +221,23 @@ class PagedAttention:
         n_new) and dg_q, dg_k (fp32 [D]) from those of the outputs and the
         forward's inputs."""
         B, n = q.shape[:2]
-        Hq, Hkv = self.n_q_heads, self.n_kv_heads
-        args = [self._heads(t, B, n, H, name) for t, H, name in (
-            (dq_out, Hq, "dq_out"), (dk_out, Hkv, "dk_out"), (q, Hq, "q"), (k, Hkv, "k"), (dq, Hq, "dq"), (dk, Hkv, "dk"))]
-        table, length = self._rope(rope)
-        d = [None if t is None else self._tensor(t, (self.head_dim,), torch.float32, name)
-             for t, name in ((dg_q, "dg_q"), (dg_k, "dg_k"))]
-        self._check(self.lib.prism_qk_norm_rope_backward(
-            self.h, B, n, *args, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), table, length,
-            self._counts(pos, B, "pos"), self._counts(n_new, B, "n_new"), *d, self._stream(stream)))
+        sq, sk = self._shapes(B, n)
+        self._pack(sq, sk, q, k, None, None, None, rope, pos, g_q, g_k, n_new)
+        f32, D = torch.float32, self.head_dim
+        _GRADS.pack_into(
+            self._grads, 0, *self._heads(dq_out, sq, "dq_out"), *self._heads(dk_out, sk, "dk_out"), *self._heads(dq, sq, "dq"),
+            *self._heads(dk, sk, "dk"), 0 if dg_q is None else self._tensor(dg_q, (D,), f32, "dg_q"),
+            0 if dg_k is None else self._tensor(dg_k, (D,), f32, "dg_k"))
+        self._check(self.lib.prism_qk_norm_rope_backward(self.h, self._rows_at, self._grads_at, self._stream(stream)))
 
     def append(self, cache, q, k, v, q_out, rope, g_q=None, g_k=None, pos=None, n_new=None, stream=None):
         """``prism_paged_append``: q, q_out [B, n, Hq, D]; k, v [B, n, Hkv, D].
         Rows i < n_new[b] go to slots kv_len[b] + i, at positions pos[b] + i (pos
         None: their slots).  kv_len is not advanced."""
         ref = self._bound(cache)
-        B, n = cache.batch, q.shape[1]
-        sq, sk = self._heads(q, B, n, self.n_q_heads, "q"), self._heads(k, B, n, self.n_kv_heads, "k")
-        sv, oq = self._heads(v, B, n, self.n_kv_heads, "v"), self._heads(q_out, B, n, self.n_q_heads, "q_out")
-        table, length = self._rope(rope)
-        self._check(self.lib.prism_paged_append(
-            self.h, ref, n, sq, sk, sv, oq, self._gain(g_q, "g_q"), self._gain(g_k, "g_k"), table, length,
-            self._counts(pos, B, "pos"), self._counts(n_new, B, "n_new"), self._stream(stream)))
+        sq, sk = self._shapes(cache.batch, q.shape[1])
+        self._pack(sq, sk, q, k, v, q_out, None, rope, pos, g_q, g_k, n_new)
+        self._check(self.lib.prism_paged_append(self.h, ref, self._rows_at, self._stream(stream)))
 
     def attend(self, cache, q, out, lse=None, added=1, stream=None):
         """``prism_paged_attend``: q, out [B, Hq, D]; lse fp32 [B, Hq] or None;

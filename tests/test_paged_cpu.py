@@ -19,15 +19,14 @@ def lib():
 
 
 def test_null_handles_are_refused(lib):
-    none = [None] * 16
-    assert lib.prism_qk_norm_rope(None, 1, 1, *none[:6], None, 1, None, None, None) == 1
-    assert lib.prism_qk_norm_rope_backward(None, 1, 1, *none[:9], 1, *none[:5]) == 1
-    assert lib.prism_paged_append(None, None, 1, *none[:7], 1, None, None, None) == 1
+    assert lib.prism_qk_norm_rope(None, None, None) == 1
+    assert lib.prism_qk_norm_rope_backward(None, None, None, None) == 1
+    assert lib.prism_paged_append(None, None, None, None) == 1
     assert lib.prism_paged_attend(None, None, 1, None, None, None, None) == 1
     assert lib.prism_paged_evict(None, None, None, 1, 0, 0, None, None) == 1
     assert lib.prism_paged_status(None, None, None) == 1
     assert lib.prism_paged_destroy(None) == 0
-    assert b"null handle" in lib.prism_paged_error(None)
+    assert b"null" in lib.prism_paged_error(None)
 
 
 @pytest.mark.parametrize("field,value", [("head_dim", 80), ("n_kv_heads", 3), ("n_kv_heads", 0), ("page_size", 0), ("max_batch", 0),
