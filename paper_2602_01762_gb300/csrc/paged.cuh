@@ -80,6 +80,7 @@ size_t attend_part_floats(bool bf16, int D, int G, int sms);
 // Kernel attributes, before any capture.
 cudaError_t prepare_attend_kernels();
 cudaError_t prepare_evict_kernels();
+cudaError_t prepare_rope_kernels();
 cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
 int norm_rope_grad_ctas(int sms);
@@ -93,6 +94,19 @@ __device__ __forceinline__ int paged_len(const PagedView &c, int b, int added, i
     if (n >= 0 && n <= cap) return (int)n;
     set_err(err, kErrCache);
     return n < 0 ? 0 : (int)cap;
+}
+
+// 16 bytes from global to shared memory, asynchronously; not ok: zeros, nothing is read.
+__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
+    const int n = ok ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void cp_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t addr) {
+    uint4 u;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(u.x), "=r"(u.y), "=r"(u.z), "=r"(u.w) : "r"(addr) : "memory");
+    return u;
 }
 
 // Two floats rounded to bf16 (nearest even, NaN kept), the first in the low half.
@@ -144,20 +158,23 @@ __device__ __forceinline__ void dsmem_st(int *local, uint32_t rank, int v) {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(dsmem_at(local, rank)), "r"(v) : "memory");
 }
 
-// Ragged work split into equal contiguous shares.  Sequence b has blocks(b) >= 1
-// blocks of keys, each for `heads` heads; units run over (b, head, block).
+// Ragged work split into equal contiguous shares.  Sequence b of rows(b) rows has
+// blocks_of(rows) >= 1 blocks of keys, each for `heads` heads; units run over (b, head, block).
 // Every CTA takes `per` units from u0 on; begin() finds the sequence of its
 // first one.  All threads of the CTA call it.
 struct UnitRange {
     int u0, u1, per;   // this CTA's units; units per CTA
     int b, first;      // sequence of u0 and that sequence's first unit
+    int lens;          // lane i: rows of sequence i (B <= 32 alone)
 };
-template <int THREADS, typename Blocks>
-__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, int min_units, const Blocks &blocks) {
+template <int THREADS, typename Rows, typename Blocks>
+__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, int min_units, const Rows &rows, const Blocks &blocks_of) {
     const int tid = threadIdx.x, lane = tid & 31;
     const int cta = blockIdx.x, ctas = gridDim.x;
+    auto blocks = [&](int b) { return blocks_of(rows(b)); };
     if (B <= 32) {                       // every warp for itself
-        const int n = lane < B ? blocks(lane) : 0;
+        r.lens = lane < B ? rows(lane) : 0;
+        const int n = lane < B ? blocks_of(r.lens) : 0;
         int s = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {

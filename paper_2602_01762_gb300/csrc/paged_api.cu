@@ -147,6 +147,7 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, device);
     if (e == cudaSuccess) e = prepare_attend_kernels();
     if (e == cudaSuccess) e = prepare_evict_kernels();
+    if (e == cudaSuccess) e = prepare_rope_kernels();
     if (e != cudaSuccess) {
         delete p;
         return cuda_status(nullptr, e, "prism_paged_create");

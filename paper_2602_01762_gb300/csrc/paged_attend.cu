@@ -19,13 +19,6 @@ constexpr int kPaStage = 8192;           // bytes of one warp's stage: KT rows o
 constexpr int kPaCtasPerSm = 2;
 constexpr float kLn2 = 0.693147180559945309f;
 
-__device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
-    const int n = ok ? 16 : 0;           // 0: the 16 bytes are zero-filled, nothing is read
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void cp_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N> __device__ __forceinline__ void cp_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
-
 __device__ __forceinline__ void lds_x4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -367,7 +360,12 @@ struct Pieces {
         u1 = r.u1;
         b = r.b;
         heads = n_heads;
-        fetch(a);
+        if (a.B <= 32) {
+            base = 0;
+            lens = r.lens;
+        } else {
+            fetch(a);
+        }
         sequence();
         h = (u - r.first) / nblk;
         blk0 = (u - r.first) % nblk;
@@ -434,7 +432,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
     UnitRange r;
     if (!unit_range<kPaThreads>(r, a.B, heads, a.min_units,
-                                [&](int b) { return blocks_of(paged_len(a.cache, b, a.added, a.err)); }))
+                                [&](int b) { return paged_len(a.cache, b, a.added, a.err); }, blocks_of))
         return;
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * kPaStage);
@@ -577,12 +575,18 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                 float *top = merge;                      // [kJoin][H]: maxima of kJoin pieces at a time
                 for (int h = warp; h < n; h += kPaWarps) {
                     float M = -INFINITY, L = 0.f;
-                    for (int i = lane; i < pieces; i += 32) {
-                        const float2 ml = __ldcg((const float2 *)(piece_part(i) + H * D + 2 * h));
-                        if (i < kJoin) top[i * H + h] = ml.x;
-                        const float m = fmaxf(M, ml.x);
-                        L = L * exp2f(M - base_of(m)) + exp2f(ml.x - base_of(m)) * ml.y;
-                        M = m;
+                    for (int i0 = lane; i0 < pieces; i0 += 64) {
+                        float2 ml[2];
+#pragma unroll
+                        for (int k = 0; k < 2; ++k)
+                            ml[k] = i0 + 32 * k < pieces ? __ldcg((const float2 *)(piece_part(i0 + 32 * k) + H * D + 2 * h)) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+                        for (int k = 0; k < 2; ++k) {
+                            if (i0 + 32 * k < min(pieces, kJoin)) top[(i0 + 32 * k) * H + h] = ml[k].x;
+                            const float m = fmaxf(M, ml[k].x);
+                            L = L * exp2f(M - base_of(m)) + exp2f(ml[k].x - base_of(m)) * ml[k].y;
+                            M = m;
+                        }
                     }
 #pragma unroll
                     for (int o = 16; o > 0; o >>= 1) {
@@ -650,33 +654,43 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 constexpr int kWtThreads = 256;
 constexpr int kWtRows = 2 * kWtThreads;  // rows per unit: two a thread, their loads side by side
 __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a, int head_tile) {
-    pdl_trigger();                       // before the wait: the attention's own wait has made kv_len final
+    // Before the wait: the attention kernel lets this one start once its own wait is
+    // over, so lengths, table and weights are final; scores and stat are not.
+    pdl_trigger();
     auto rows = [&](int b) { return paged_len(a.cache, b, a.added, nullptr); };
-    auto blocks = [&](int b) { return max(1, (rows(b) + kWtRows - 1) / kWtRows); };
+    auto blocks = [](int n) { return max(1, (n + kWtRows - 1) / kWtRows); };
     UnitRange r;
-    const bool any = unit_range<kWtThreads>(r, a.B, a.Hkv, 1, blocks);
-    pdl_wait();
-    if (!any) return;
+    const bool any = unit_range<kWtThreads>(r, a.B, a.Hkv, 1, rows, blocks);
     const int G = a.Hq / a.Hkv;
-    int b = r.b, len = rows(b), nblk = blocks(b);
-    int h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
-    for (int u = r.u0; u < r.u1; ++u) {
-        const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
-        const float2 *st = a.stat + (long long)b * a.Hq + h * G;
-        float *to[2];
-        float w[2];
+    int b = 0, len = 0, nblk = 1, h = 0, blk = 0;
+    float *to[2];
+    float w[2];
+    auto fetch = [&]() {                 // where the unit's rows have their weights, and these
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int j = blk * kWtRows + i * kWtThreads + threadIdx.x;
             to[i] = nullptr;
-            w[i] = 0.f;
             if (j >= len) continue;
             const int slot = j / a.cache.page_size;
             const int page = a.cache.table[(long long)b * a.cache.table_pages + slot];
-            if ((unsigned)page < (unsigned)a.cache.n_pages)   // else reported by the attention
-                to[i] = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
+            if ((unsigned)page >= (unsigned)a.cache.n_pages) continue;   // reported by the attention
+            to[i] = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
         }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) w[i] = to[i] ? *to[i] : 0.f;
+    };
+    if (any) {
+        b = r.b, len = rows(b), nblk = blocks(len);
+        h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
+        fetch();
+    }
+    pdl_wait();                          // the scores
+    if (!any) return;
+    for (int u = r.u0; u < r.u1; ++u) {
+        const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
+        const float2 *st = a.stat + (long long)b * a.Hq + h * G;
+        float sum[2] = {0.f, 0.f};
         for (int t = 0; t < G; t += head_tile) {
             const int n = min(head_tile, G - t);
 #pragma unroll
@@ -685,7 +699,7 @@ __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a,
                 const float *z = s + t * cap + (long long)(blk * kWtRows + i * kWtThreads + threadIdx.x) * n;
                 auto add = [&](float x, int k) {
                     const float2 ml = st[t + k];
-                    w[i] = fmaf(exp2f(x - ml.x), ml.y, w[i]);
+                    sum[i] = fmaf(exp2f(x - ml.x), ml.y, sum[i]);
                 };
                 if (n % 4 == 0) {
                     for (int k = 0; k < n; k += 4) {
@@ -699,17 +713,18 @@ __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a,
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i)
-            if (to[i]) *to[i] += w[i];
+            if (to[i]) *to[i] = w[i] + sum[i];
+        if (u + 1 == r.u1) break;
         if (++blk == nblk) {
             blk = 0;
             if (++h == a.Hkv) {
                 h = 0;
-                if (++b < a.B) {
-                    len = rows(b);
-                    nblk = blocks(b);
-                }
+                ++b;
+                len = rows(b);
+                nblk = blocks(len);
             }
         }
+        fetch();
     }
 }
 
@@ -756,7 +771,7 @@ cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, 
     });
     if (e != cudaSuccess || !a.scores) return e;
     const long long chunks = a.B * (long long)a.Hkv * ((cap + kWtRows - 1) / kWtRows);
-    const int wt = (int)(chunks < sms * 8 ? chunks : sms * 8);
+    const int wt = (int)(chunks < sms * 6 ? chunks : sms * 6);
     return launch_k(paged_weights_kernel, dim3(wt), dim3(kWtThreads), 0, s, true, a, ht);
 }
 

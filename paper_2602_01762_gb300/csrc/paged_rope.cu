@@ -16,7 +16,8 @@ namespace prism {
 namespace {
 
 constexpr int kNrThreads = 128;
-constexpr int kNrUnroll = 2;             // head groups a warp has in flight
+constexpr int kNrRing = 8;               // head groups a warp has in flight
+constexpr int kNrStage = 1024;           // bytes of one: the lanes' low pieces, then their high ones
 
 template <typename T, int D> struct Rope {
     static constexpr int E = Vec16<T>::E, kLanes = D / 2 / E, kHeads = 32 / kLanes;
@@ -53,12 +54,15 @@ __device__ __forceinline__ int row_count(const int32_t *n_new, int b, int max_ne
     return n < 0 ? 0 : max_new;
 }
 
-// One warp per row and share of its head groups (`split` shares).  APPEND: keys
-// and values go to the paged cache, and their accumulated weights start at 0.
+// One warp per row and share of its head groups (`split` shares), kNrRing - 1 of
+// them on their way at a time: they are requested before the row's position and
+// place are known.  APPEND: keys and values go to the paged cache, and their
+// accumulated weights start at 0.
 template <typename T, int D, bool APPEND>
 __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     using R = Rope<T, D>;
     constexpr int E = R::E;
+    __shared__ __align__(16) unsigned char smem[kNrThreads / 32 * kNrRing * kNrStage];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
@@ -67,11 +71,24 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     const int share = (int)(w - row * a.split);
     const int b = (int)(row / a.max_new), i = (int)(row - (long long)b * a.max_new);
     if (b >= a.B || i >= row_count(a.n_new, b, a.max_new, a.err)) return;
-    R rope;
-    rope.load(a.rope, row_position(a.pos, b, i, a.rope_len, a.err));
-
     const int sub = lane % R::kLanes, own = lane / R::kLanes;
     const int hk = a.Hq, hv = a.Hq + a.Hkv, all = APPEND ? hv + a.Hkv : hv;
+    // each lane copies what it reads itself, so that its own waits are enough
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.x >> 5) * (kNrRing * kNrStage) + lane * 16;
+    auto copy = [&](int g, int stage) {
+        const int h = g * R::kHeads + own;
+        if (h < all) {
+            const HeadsView &x = h < hk ? a.q : h < hv ? a.k : a.v;
+            const char *p = x.p + b * x.sb + i * x.st + (h < hk ? h : h < hv ? h - hk : h - hv) * x.sh + sub * 16;
+            cp16(ring + stage * kNrStage, p, true);
+            cp16(ring + stage * kNrStage + 512, p + D / 2 * sizeof(T), true);
+        }
+        cp_group();
+    };
+#pragma unroll
+    for (int u = 0; u < kNrRing - 1; ++u) copy(share + u * a.split, u);
+    R rope;
+    rope.load(a.rope, row_position(a.pos, b, i, a.rope_len, a.err));
     long long at = 0, wt = 0;            // the new row's place in the pool and in the weights (KV head 0)
     bool stored = true;
     if (APPEND) {
@@ -88,68 +105,59 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
             wt = (long long)page * a.Hkv * a.cache.page_size + off;
         }
     }
-    for (int g0 = share; g0 * R::kHeads < all; g0 += kNrUnroll * a.split) {
-        uint4 lo[kNrUnroll], hi[kNrUnroll];
-#pragma unroll
-        for (int u = 0; u < kNrUnroll; ++u) {
-            const int h = (g0 + u * a.split) * R::kHeads + own;
-            if (h >= all) continue;
-            const HeadsView &x = h < hk ? a.q : h < hv ? a.k : a.v;
-            const char *p = x.p + b * x.sb + i * x.st + (h < hk ? h : h < hv ? h - hk : h - hv) * x.sh;
-            lo[u] = *((const uint4 *)p + sub);
-            hi[u] = *((const uint4 *)(p + D / 2 * sizeof(T)) + sub);
+    int stage = 0;
+    for (int g = share; g * R::kHeads < all; g += a.split) {
+        copy(g + (kNrRing - 1) * a.split, stage == 0 ? kNrRing - 1 : stage - 1);
+        cp_wait_group<kNrRing - 1>();
+        const int h = g * R::kHeads + own;
+        const bool in = h < all;
+        uint4 l = make_uint4(0u, 0u, 0u, 0u), r = l;
+        if (in) {
+            l = lds16(ring + stage * kNrStage);
+            r = lds16(ring + stage * kNrStage + 512);
         }
-#pragma unroll
-        for (int u = 0; u < kNrUnroll; ++u) {
-            const int h = (g0 + u * a.split) * R::kHeads + own;
-            const bool in = h < all;
+        stage = stage + 1 == kNrRing ? 0 : stage + 1;
+        if (g * R::kHeads < hv) {        // a group with query or key heads (the same for the warp)
             float x[E], y[E];
-            if (in) {
-                Vec16<T>::unpack(lo[u], x);
-                Vec16<T>::unpack(hi[u], y);
-            } else {
-#pragma unroll
-                for (int e = 0; e < E; ++e) x[e] = y[e] = 0.f;
-            }
+            Vec16<T>::unpack(l, x);
+            Vec16<T>::unpack(r, y);
             if (a.g_q) {
                 float s = 0.f;
 #pragma unroll
                 for (int e = 0; e < E; ++e) s = fmaf(x[e], x[e], fmaf(y[e], y[e], s));
-                const float r = rsqrtf(lanes_sum<R::kLanes>(s) * (1.f / D) + a.eps);
-                const uint4 *g = (const uint4 *)(h < hk ? a.g_q : a.g_k) + sub;
+                const float f = rsqrtf(lanes_sum<R::kLanes>(s) * (1.f / D) + a.eps);
+                const uint4 *gain = (const uint4 *)(h < hk ? a.g_q : a.g_k) + sub;
                 float gx[E], gy[E];
-                Vec16<T>::unpack(__ldg(g), gx);
-                Vec16<T>::unpack(__ldg(g + R::kLanes), gy);
+                Vec16<T>::unpack(__ldg(gain), gx);
+                Vec16<T>::unpack(__ldg(gain + R::kLanes), gy);
 #pragma unroll
                 for (int e = 0; e < E; ++e) {
-                    x[e] = x[e] * r * gx[e];
-                    y[e] = y[e] * r * gy[e];
+                    x[e] = x[e] * f * gx[e];
+                    y[e] = y[e] * f * gy[e];
                 }
             }
-            if (!in) continue;
             float p[E], q[E];
 #pragma unroll
             for (int e = 0; e < E; ++e) {
                 p[e] = x[e] * rope.cs[e] - y[e] * rope.sn[e];
                 q[e] = y[e] * rope.cs[e] + x[e] * rope.sn[e];
             }
-            uint4 l = Vec16<T>::pack(p), r = Vec16<T>::pack(q);
-            char *to;
-            if (h < hk) {
-                to = a.q_out.p + b * a.q_out.sb + i * a.q_out.st + h * a.q_out.sh;
-            } else if (!APPEND) {
-                to = a.k_out.p + b * a.k_out.sb + i * a.k_out.st + (h - hk) * a.k_out.sh;
-            } else {
-                if (!stored) continue;
-                const int kh = h < hv ? h - hk : h - hv;
-                to = (h < hv ? a.cache.k : a.cache.v) + at + kh * a.cache.head_stride;
-                if (h >= hv) {
-                    l = lo[u];
-                    r = hi[u];
-                } else if (sub == 0 && a.cache.weights) {
-                    a.cache.weights[wt + (long long)kh * a.cache.page_size] = 0.f;
-                }
+            if (h < hv) {                // values stay as they are
+                l = Vec16<T>::pack(p);
+                r = Vec16<T>::pack(q);
             }
+        }
+        char *to = nullptr;
+        if (h < hk) {
+            to = a.q_out.p + b * a.q_out.sb + i * a.q_out.st + h * a.q_out.sh;
+        } else if (!APPEND) {
+            if (in) to = a.k_out.p + b * a.k_out.sb + i * a.k_out.st + (h - hk) * a.k_out.sh;
+        } else if (in && stored) {
+            const int kh = h < hv ? h - hk : h - hv;
+            to = (h < hv ? a.cache.k : a.cache.v) + at + kh * a.cache.head_stride;
+            if (h < hv && sub == 0 && a.cache.weights) a.cache.weights[wt + (long long)kh * a.cache.page_size] = 0.f;
+        }
+        if (to) {
             *((uint4 *)to + sub) = l;
             *((uint4 *)(to + D / 2 * sizeof(T)) + sub) = r;
         }
@@ -163,33 +171,27 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
 // every row and head it meets; lanes, warps and CTAs are then added in a fixed
 // order (the last CTA to finish adds the CTAs' rows in CTA order), so dg does not
 // depend on the order in which they ran.
+// Persistent CTAs, one per SM; each warp walks over its rows' head groups with a
+// ring of kNgRing groups requested ahead by cp.async, across rows.
 constexpr int kNgThreads = 512;
+constexpr int kNgRing = 5;
+constexpr int kNgStage = 2048 + 512;     // x and dy, low and high pieces of each lane; the row's cosines and sines
 
 template <typename T, int D> struct GainGrad {
     float x[Vec16<T>::E], y[Vec16<T>::E];
 };
 
+// The heads of one group: x and dy from the stage, dx to `to` (null: a lane without a head).
 template <typename T, int D>
-__device__ __forceinline__ void grad_heads(const NormRopeGradArgs &a, const HeadsView &gy, const HeadsView &xv, const HeadsView &dx,
-                                           const void *gain, const Rope<T, D> &rope, GainGrad<T, D> &dg, int b, int i, bool valid,
-                                           int h, int heads) {
+__device__ __forceinline__ void grad_group(uint32_t stage, char *to, const void *gain, float eps, const Rope<T, D> &rope, GainGrad<T, D> &dg) {
     using R = Rope<T, D>;
     constexpr int E = R::E;
-    const int sub = (threadIdx.x & 31) % R::kLanes;
-    const bool in = h < heads;
+    const int lane = threadIdx.x & 31, sub = lane % R::kLanes;
     float x[E], y[E], p[E], q[E];
-    if (in && valid) {
-        const char *sx = xv.p + b * xv.sb + i * xv.st + h * xv.sh, *sg = gy.p + b * gy.sb + i * gy.st + h * gy.sh;
-        const uint4 l = *((const uint4 *)sx + sub), r = *((const uint4 *)(sx + D / 2 * sizeof(T)) + sub);
-        const uint4 m = *((const uint4 *)sg + sub), n = *((const uint4 *)(sg + D / 2 * sizeof(T)) + sub);
-        Vec16<T>::unpack(l, x);
-        Vec16<T>::unpack(r, y);
-        Vec16<T>::unpack(m, p);
-        Vec16<T>::unpack(n, q);
-    } else {
-#pragma unroll
-        for (int e = 0; e < E; ++e) x[e] = y[e] = p[e] = q[e] = 0.f;
-    }
+    Vec16<T>::unpack(lds16(stage + lane * 16), x);
+    Vec16<T>::unpack(lds16(stage + 512 + lane * 16), y);
+    Vec16<T>::unpack(lds16(stage + 1024 + lane * 16), p);
+    Vec16<T>::unpack(lds16(stage + 1536 + lane * 16), q);
 #pragma unroll
     for (int e = 0; e < E; ++e) {
         const float u = p[e], v = q[e];
@@ -200,11 +202,11 @@ __device__ __forceinline__ void grad_heads(const NormRopeGradArgs &a, const Head
         float s = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) s = fmaf(x[e], x[e], fmaf(y[e], y[e], s));
-        const float r = rsqrtf(lanes_sum<R::kLanes>(s) * (1.f / D) + a.eps);
+        const float r = rsqrtf(lanes_sum<R::kLanes>(s) * (1.f / D) + eps);
         const uint4 *g = (const uint4 *)gain + sub;
-        float gx[E], gy2[E];
+        float gx[E], gy[E];
         Vec16<T>::unpack(__ldg(g), gx);
-        Vec16<T>::unpack(__ldg(g + R::kLanes), gy2);
+        Vec16<T>::unpack(__ldg(g + R::kLanes), gy);
         float c = 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
@@ -213,7 +215,7 @@ __device__ __forceinline__ void grad_heads(const NormRopeGradArgs &a, const Head
             dg.x[e] = fmaf(p[e], x[e], dg.x[e]);
             dg.y[e] = fmaf(q[e], y[e], dg.y[e]);
             p[e] *= gx[e];
-            q[e] *= gy2[e];
+            q[e] *= gy[e];
             c = fmaf(p[e], x[e], fmaf(q[e], y[e], c));
         }
         c = lanes_sum<R::kLanes>(c) * (1.f / D);
@@ -223,41 +225,118 @@ __device__ __forceinline__ void grad_heads(const NormRopeGradArgs &a, const Head
             q[e] = r * (q[e] - y[e] * c);
         }
     }
-    if (!in) return;
-    char *to = dx.p + b * dx.sb + i * dx.st + h * dx.sh;
+    if (!to) return;
     *((uint4 *)to + sub) = Vec16<T>::pack(p);
     *((uint4 *)(to + D / 2 * sizeof(T)) + sub) = Vec16<T>::pack(q);
 }
+
+// A warp's walk over (row, share) items and the head groups of each.
+struct RowWalk {
+    int w, b, i, g;
+    bool live, valid;
+    __device__ __forceinline__ void at(const NormRopeGradArgs &a, int item, int items) {
+        w = item;
+        live = item < items;
+        valid = false;
+        if (!live) return;
+        const int row = item / a.split;
+        g = item - row * a.split;
+        b = row / a.max_new;
+        i = row - b * a.max_new;
+        valid = i < row_count(a.n_new, b, a.max_new, a.err);
+    }
+};
 
 template <typename T, int D>
 __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGradArgs a) {
     using R = Rope<T, D>;
     constexpr int E = R::E, kWarps = kNgThreads / 32;
-    __shared__ float sum[kWarps][2 * D];
+    extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ int last;
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % R::kLanes, own = lane / R::kLanes;
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dyn) + warp * (kNgRing * kNgStage);
     GainGrad<T, D> dq, dk;
 #pragma unroll
     for (int e = 0; e < E; ++e) dq.x[e] = dq.y[e] = dk.x[e] = dk.y[e] = 0.f;
-    const long long items = (long long)a.B * a.max_new * a.split;
-    const int gq = (a.Hq + R::kHeads - 1) / R::kHeads, gk = (a.Hkv + R::kHeads - 1) / R::kHeads;
-    for (long long w = (long long)blockIdx.x * kWarps + warp; w < items; w += (long long)gridDim.x * kWarps) {
-        const long long row = w / a.split;
-        const int share = (int)(w - row * a.split);
-        const int b = (int)(row / a.max_new), i = (int)(row - (long long)b * a.max_new);
-        const bool valid = i < row_count(a.n_new, b, a.max_new, a.err);
+    const int items = a.B * a.max_new * a.split, step = gridDim.x * kWarps;
+    const int gq = (a.Hq + R::kHeads - 1) / R::kHeads, groups = gq + (a.Hkv + R::kHeads - 1) / R::kHeads;
+    auto head_at = [&](const HeadsView &v, const RowWalk &r, int h) { return v.p + r.b * v.sb + r.i * v.st + h * v.sh; };
+
+    RowWalk f;                           // loads ahead: the next group to request, in rows that count
+    f.at(a, blockIdx.x * kWarps + warp, items);
+    while (f.live && !f.valid) f.at(a, f.w + step, items);
+    bool fresh = true;                   // its row's first group: the row's table line comes with it
+    int stage_in = 0;
+    auto request = [&]() {
+        if (f.live) {
+            const uint32_t to = ring + stage_in * kNgStage;
+            const bool is_q = f.g < gq;
+            const int h = (is_q ? f.g : f.g - gq) * R::kHeads + own;
+            const bool ok = h < (is_q ? a.Hq : a.Hkv);
+            const char *x = ok ? head_at(is_q ? a.q : a.k, f, h) : a.q.p, *y = ok ? head_at(is_q ? a.dq_out : a.dk_out, f, h) : a.q.p;
+            cp16(to + lane * 16, x + sub * 16, ok);
+            cp16(to + 512 + lane * 16, x + D / 2 * sizeof(T) + sub * 16, ok);
+            cp16(to + 1024 + lane * 16, y + sub * 16, ok);
+            cp16(to + 1536 + lane * 16, y + D / 2 * sizeof(T) + sub * 16, ok);
+            if (fresh && lane < D / 4)
+                cp16(to + 2048 + lane * 16, a.rope + (long long)row_position(a.pos, f.b, f.i, a.rope_len, a.err) * D + lane * 4, true);
+            f.g += a.split;
+            fresh = f.g >= groups;
+            if (fresh) {
+                f.at(a, f.w + step, items);
+                while (f.live && !f.valid) f.at(a, f.w + step, items);
+            }
+        }
+        cp_group();
+        stage_in = stage_in + 1 == kNgRing ? 0 : stage_in + 1;
+    };
+#pragma unroll
+    for (int u = 0; u < kNgRing - 1; ++u) request();
+
+    int stage = 0;
+    RowWalk r;
+    for (r.at(a, blockIdx.x * kWarps + warp, items); r.live; r.at(a, r.w + step, items)) {
+        if (!r.valid) {                  // rows past n_new have zero gradients
+            for (; r.g < groups; r.g += a.split) {
+                const bool is_q = r.g < gq;
+                const int h = (is_q ? r.g : r.g - gq) * R::kHeads + own;
+                if (h >= (is_q ? a.Hq : a.Hkv)) continue;
+                char *to = head_at(is_q ? a.dq : a.dk, r, h);
+                *((uint4 *)to + sub) = *((uint4 *)(to + D / 2 * sizeof(T)) + sub) = make_uint4(0u, 0u, 0u, 0u);
+            }
+            continue;
+        }
         R rope;
-        rope.load(a.rope, valid ? row_position(a.pos, b, i, a.rope_len, a.err) : 0);
-        for (int g = share; g < gq; g += a.split)
-            grad_heads<T, D>(a, a.dq_out, a.q, a.dq, a.g_q, rope, dq, b, i, valid, g * R::kHeads + own, a.Hq);
-        // the shares go on over the key groups where those of the queries ended
-        for (int g = (share - gq % a.split + a.split) % a.split; g < gk; g += a.split)
-            grad_heads<T, D>(a, a.dk_out, a.k, a.dk, a.g_k, rope, dk, b, i, valid, g * R::kHeads + own, a.Hkv);
+        for (bool first = true; r.g < groups; r.g += a.split, first = false) {
+            cp_wait_group<kNgRing - 2>();
+            __syncwarp();
+            request();                   // into the stage that was read last
+            const uint32_t at = ring + stage * kNgStage;
+            if (first) {
+#pragma unroll
+                for (int e = 0; e < E; e += 4) {
+                    const uint4 c = lds16(at + 2048 + (sub * E + e) * 4), s = lds16(at + 2048 + (D / 2 + sub * E + e) * 4);
+                    Vec16<float>::unpack(c, *(float(*)[4])(rope.cs + e));
+                    Vec16<float>::unpack(s, *(float(*)[4])(rope.sn + e));
+                }
+            }
+            if (r.g < gq) {
+                const int h = r.g * R::kHeads + own;
+                grad_group<T, D>(at, h < a.Hq ? head_at(a.dq, r, h) : nullptr, a.g_q, a.eps, rope, dq);
+            } else {
+                const int h = (r.g - gq) * R::kHeads + own;
+                grad_group<T, D>(at, h < a.Hkv ? head_at(a.dk, r, h) : nullptr, a.g_k, a.eps, rope, dk);
+            }
+            stage = stage + 1 == kNgRing ? 0 : stage + 1;
+        }
     }
+    cp_wait_group<0>();
     if (!a.g_q) return;
     // lanes that hold the same dims, then warps, then CTAs
+    __syncthreads();                     // the rings are free
+    float(*sum)[2 * D] = (float(*)[2 * D])dyn;
     auto fold = [&](float v) {
 #pragma unroll
         for (int o = R::kLanes; o < 32; o <<= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, o);
@@ -314,6 +393,7 @@ int row_split(long long rows, int groups, int sms) {
     long long s = ((long long)sms * 16 + rows - 1) / rows;
     return (int)(s < 1 ? 1 : s > groups ? groups : s);
 }
+constexpr int kNgSmem = kNgThreads / 32 * kNgRing * kNgStage;
 int heads_per_warp(bool bf16, int D) { return 32 / (D / 2 / (bf16 ? 8 : 4)); }
 
 }  // namespace
@@ -333,6 +413,15 @@ cudaError_t launch_norm_rope(const NormRopeArgs &args, bool bf16, int D, bool ap
     return D == 128 ? go(norm_rope_kernel<float, 128, false>) : go(norm_rope_kernel<float, 64, false>);
 }
 
+cudaError_t prepare_rope_kernels() {
+    auto set = [](auto k) { return cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kNgSmem); };
+    cudaError_t e = set(norm_rope_grad_kernel<uint16_t, 64>);
+    if (e == cudaSuccess) e = set(norm_rope_grad_kernel<uint16_t, 128>);
+    if (e == cudaSuccess) e = set(norm_rope_grad_kernel<float, 64>);
+    if (e == cudaSuccess) e = set(norm_rope_grad_kernel<float, 128>);
+    return e;
+}
+
 int norm_rope_grad_ctas(int sms) { return sms; }
 
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &args, bool bf16, int D, int sms, cudaStream_t s) {
@@ -343,7 +432,7 @@ cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &args, bool bf16, int D
     const long long ctas = (rows * a.split + kNgThreads / 32 - 1) / (kNgThreads / 32);
     const int most = norm_rope_grad_ctas(sms);
     const dim3 grid((unsigned)(ctas < most ? ctas : most));
-    auto go = [&](auto k) { return launch_k(k, grid, dim3(kNgThreads), 0, s, true, a); };
+    auto go = [&](auto k) { return launch_k(k, grid, dim3(kNgThreads), kNgSmem, s, true, a); };
     if (bf16) return D == 128 ? go(norm_rope_grad_kernel<uint16_t, 128>) : go(norm_rope_grad_kernel<uint16_t, 64>);
     return D == 128 ? go(norm_rope_grad_kernel<float, 128>) : go(norm_rope_grad_kernel<float, 64>);
 }
