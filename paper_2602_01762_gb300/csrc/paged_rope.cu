@@ -19,17 +19,99 @@ constexpr int kNrThreads = 128;
 constexpr int kNrRing = 8;               // head groups a warp has in flight
 constexpr int kNrStage = 1024;           // bytes of one: the lanes' low pieces, then their high ones
 
-template <typename T, int D> struct Rope {
-    static constexpr int E = Vec16<T>::E, kLanes = D / 2 / E, kHeads = 32 / kLanes;
-    float cs[E], sn[E];
-    __device__ __forceinline__ void load(const float *rope, int pos) {
-        const int j = (threadIdx.x & 31) % kLanes * E;
-        const float *p = rope + (long long)pos * D + j;
+// Two fp32 values in one 64-bit register and their packed arithmetic: half the
+// instructions, which is what the forward and the gradient were held up by (64% of
+// the issue slots at 4.7 and 4.2 TB/s with one value an instruction).
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 f2_values(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 f2_neg(F2 a) { return a ^ 0x8000000080000000ull; }
+__device__ __forceinline__ float f2_sum(F2 a) {
+    const float2 v = f2_values(a);
+    return v.x + v.y;
+}
+
+__device__ __forceinline__ F2 lds8(uint32_t addr) {
+    F2 r;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(addr));
+    return r;
+}
+
+// 16 bytes as pairs of values, and back.
+template <typename T> struct Pairs {
+    static constexpr int N = Vec16<T>::E / 2;
+    static __device__ __forceinline__ void unpack(const uint4 &u, F2 (&f)[N]) {
+        float x[2 * N];
+        Vec16<T>::unpack(u, x);
 #pragma unroll
-        for (int i = 0; i < E; i += 4) {
-            *(float4 *)(cs + i) = __ldg((const float4 *)(p + i));
-            *(float4 *)(sn + i) = __ldg((const float4 *)(p + D / 2 + i));
+        for (int i = 0; i < N; ++i) f[i] = f2(x[2 * i], x[2 * i + 1]);
+    }
+    static __device__ __forceinline__ uint4 pack(const F2 (&f)[N]) {
+        float x[2 * N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float2 v = f2_values(f[i]);
+            x[2 * i] = v.x;
+            x[2 * i + 1] = v.y;
         }
+        return Vec16<T>::pack(x);
+    }
+};
+
+// A lane's part of one row's rotation: cosines and sines of its dims.
+template <typename T, int D> struct Rope {
+    static constexpr int E = Vec16<T>::E, N = E / 2, kLanes = D / 2 / E, kHeads = 32 / kLanes;
+    F2 cs[N], sn[N];
+    __device__ __forceinline__ void set(int i, const float4 &c, const float4 &s) {
+        cs[i] = f2(c.x, c.y);
+        cs[i + 1] = f2(c.z, c.w);
+        sn[i] = f2(s.x, s.y);
+        sn[i + 1] = f2(s.z, s.w);
+    }
+    __device__ __forceinline__ void load(const float *rope, int pos) {
+        const float *p = rope + (long long)pos * D + (threadIdx.x & 31) % kLanes * E;
+#pragma unroll
+        for (int i = 0; i < N; i += 2) set(i, __ldg((const float4 *)(p + 2 * i)), __ldg((const float4 *)(p + D / 2 + 2 * i)));
+    }
+    __device__ __forceinline__ void load_shared(uint32_t at) {
+        const uint32_t p = at + (threadIdx.x & 31) % kLanes * (E * 4);
+#pragma unroll
+        for (int i = 0; i < N; i += 2) {
+            float c[4], s[4];
+            Vec16<float>::unpack(lds16(p + 8 * i), c);
+            Vec16<float>::unpack(lds16(p + D / 2 * 4 + 8 * i), s);
+            set(i, make_float4(c[0], c[1], c[2], c[3]), make_float4(s[0], s[1], s[2], s[3]));
+        }
+    }
+};
+
+// A lane's part of a gain vector.
+template <typename T, int D> struct Gain {
+    static constexpr int N = Rope<T, D>::N;
+    F2 x[N], y[N];
+    __device__ __forceinline__ void load(const void *g) {
+        if (!g) return;
+        const uint4 *p = (const uint4 *)g + (threadIdx.x & 31) % Rope<T, D>::kLanes;
+        Pairs<T>::unpack(__ldg(p), x);
+        Pairs<T>::unpack(__ldg(p + Rope<T, D>::kLanes), y);
     }
 };
 
@@ -61,25 +143,28 @@ __device__ __forceinline__ int row_count(const int32_t *n_new, int b, int max_ne
 template <typename T, int D, bool APPEND>
 __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     using R = Rope<T, D>;
-    constexpr int E = R::E;
+    constexpr int N = R::N;
     __shared__ __align__(16) unsigned char smem[kNrThreads / 32 * kNrRing * kNrStage];
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31;
     const long long w = (long long)blockIdx.x * (kNrThreads / 32) + (threadIdx.x >> 5);
-    const long long row = w / a.split;
-    const int share = (int)(w - row * a.split);
-    const int b = (int)(row / a.max_new), i = (int)(row - (long long)b * a.max_new);
+    const int row = (int)(w / a.split), share = (int)(w - (long long)row * a.split);
+    const int b = row / a.max_new, i = row - b * a.max_new;
     if (b >= a.B || i >= row_count(a.n_new, b, a.max_new, a.err)) return;
     const int sub = lane % R::kLanes, own = lane / R::kLanes;
-    const int hk = a.Hq, hv = a.Hq + a.Hkv, all = APPEND ? hv + a.Hkv : hv;
+    // head groups: the queries', the keys', with APPEND the values'
+    const int gq = (a.Hq + R::kHeads - 1) / R::kHeads, gk = (a.Hkv + R::kHeads - 1) / R::kHeads, end_k = gq + gk;
+    const int groups = APPEND ? end_k + gk : end_k;
+    const char *qi = a.q.p + b * a.q.sb + i * a.q.st + sub * 16, *ki = a.k.p + b * a.k.sb + i * a.k.st + sub * 16;
+    const char *vi = APPEND ? a.v.p + b * a.v.sb + i * a.v.st + sub * 16 : nullptr;
     // each lane copies what it reads itself, so that its own waits are enough
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.x >> 5) * (kNrRing * kNrStage) + lane * 16;
     auto copy = [&](int g, int stage) {
-        const int h = g * R::kHeads + own;
-        if (h < all) {
-            const HeadsView &x = h < hk ? a.q : h < hv ? a.k : a.v;
-            const char *p = x.p + b * x.sb + i * x.st + (h < hk ? h : h < hv ? h - hk : h - hv) * x.sh + sub * 16;
+        const bool is_q = g < gq, is_k = g < end_k;
+        const int h = (is_q ? g : is_k ? g - gq : g - end_k) * R::kHeads + own;
+        if (g < groups && h < (is_q ? a.Hq : a.Hkv)) {
+            const char *p = (is_q ? qi : is_k ? ki : vi) + h * (is_q ? a.q.sh : is_k ? a.k.sh : a.v.sh);
             cp16(ring + stage * kNrStage, p, true);
             cp16(ring + stage * kNrStage + 512, p + D / 2 * sizeof(T), true);
         }
@@ -87,80 +172,92 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     };
 #pragma unroll
     for (int u = 0; u < kNrRing - 1; ++u) copy(share + u * a.split, u);
+    Gain<T, D> gain;
+    gain.load(a.g_q);
     R rope;
     rope.load(a.rope, row_position(a.pos, b, i, a.rope_len, a.err));
-    long long at = 0, wt = 0;            // the new row's place in the pool and in the weights (KV head 0)
-    bool stored = true;
+    char *qo = a.q_out.p + b * a.q_out.sb + i * a.q_out.st + sub * 16;
+    char *ko = APPEND ? nullptr : a.k_out.p + b * a.k_out.sb + i * a.k_out.st + sub * 16, *vo = nullptr;
+    float *weight = nullptr;             // of the new row and KV head 0
     if (APPEND) {
         const long long slot = (long long)a.cache.kv_len[b] + i;
-        stored = slot >= 0 && slot < (long long)a.cache.table_pages * a.cache.page_size;
-        if (!stored) {
+        if (slot < 0 || slot >= (long long)a.cache.table_pages * a.cache.page_size) {
             set_err(a.err, kErrCache);
         } else {
             const int idx = (int)(slot / a.cache.page_size), off = (int)(slot - (long long)idx * a.cache.page_size);
             const int page = a.cache.table[(long long)b * a.cache.table_pages + idx];
-            stored = (unsigned)page < (unsigned)a.cache.n_pages;
-            if (!stored) set_err(a.err, kErrPage);
-            at = page * a.cache.page_stride + off * a.cache.row_stride;
-            wt = (long long)page * a.Hkv * a.cache.page_size + off;
+            if ((unsigned)page >= (unsigned)a.cache.n_pages) {
+                set_err(a.err, kErrPage);
+            } else {
+                const long long at = page * a.cache.page_stride + off * a.cache.row_stride + sub * 16;
+                ko = a.cache.k + at;
+                vo = a.cache.v + at;
+                if (a.cache.weights) weight = a.cache.weights + (long long)page * a.Hkv * a.cache.page_size + off;
+            }
         }
     }
+    const long long ko_sh = APPEND ? a.cache.head_stride : a.k_out.sh;
     int stage = 0;
-    for (int g = share; g * R::kHeads < all; g += a.split) {
+    // the next group's stage, with a later group requested in its place
+    auto take = [&](int g) {
         copy(g + (kNrRing - 1) * a.split, stage == 0 ? kNrRing - 1 : stage - 1);
         cp_wait_group<kNrRing - 1>();
-        const int h = g * R::kHeads + own;
-        const bool in = h < all;
-        uint4 l = make_uint4(0u, 0u, 0u, 0u), r = l;
-        if (in) {
-            l = lds16(ring + stage * kNrStage);
-            r = lds16(ring + stage * kNrStage + 512);
-        }
+        const uint32_t at = ring + stage * kNrStage;
         stage = stage + 1 == kNrRing ? 0 : stage + 1;
-        if (g * R::kHeads < hv) {        // a group with query or key heads (the same for the warp)
-            float x[E], y[E];
-            Vec16<T>::unpack(l, x);
-            Vec16<T>::unpack(r, y);
-            if (a.g_q) {
-                float s = 0.f;
+        return at;
+    };
+    auto turn = [&](int g, int h, int heads, char *to) {
+        const uint32_t at = take(g);
+        uint4 l = make_uint4(0u, 0u, 0u, 0u), r = l;
+        if (h < heads) {
+            l = lds16(at);
+            r = lds16(at + 512);
+        }
+        F2 x[N], y[N];
+        Pairs<T>::unpack(l, x);
+        Pairs<T>::unpack(r, y);
+        if (a.g_q) {
+            F2 s = f2_mul(x[0], x[0]);
 #pragma unroll
-                for (int e = 0; e < E; ++e) s = fmaf(x[e], x[e], fmaf(y[e], y[e], s));
-                const float f = rsqrtf(lanes_sum<R::kLanes>(s) * (1.f / D) + a.eps);
-                const uint4 *gain = (const uint4 *)(h < hk ? a.g_q : a.g_k) + sub;
-                float gx[E], gy[E];
-                Vec16<T>::unpack(__ldg(gain), gx);
-                Vec16<T>::unpack(__ldg(gain + R::kLanes), gy);
+            for (int e = 1; e < N; ++e) s = f2_fma(x[e], x[e], s);
 #pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    x[e] = x[e] * f * gx[e];
-                    y[e] = y[e] * f * gy[e];
-                }
-            }
-            float p[E], q[E];
+            for (int e = 0; e < N; ++e) s = f2_fma(y[e], y[e], s);
+            const float f = rsqrtf(lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + a.eps);
+            const F2 ff = f2(f, f);
 #pragma unroll
-            for (int e = 0; e < E; ++e) {
-                p[e] = x[e] * rope.cs[e] - y[e] * rope.sn[e];
-                q[e] = y[e] * rope.cs[e] + x[e] * rope.sn[e];
-            }
-            if (h < hv) {                // values stay as they are
-                l = Vec16<T>::pack(p);
-                r = Vec16<T>::pack(q);
+            for (int e = 0; e < N; ++e) {
+                x[e] = f2_mul(f2_mul(x[e], ff), gain.x[e]);
+                y[e] = f2_mul(f2_mul(y[e], ff), gain.y[e]);
             }
         }
-        char *to = nullptr;
-        if (h < hk) {
-            to = a.q_out.p + b * a.q_out.sb + i * a.q_out.st + h * a.q_out.sh;
-        } else if (!APPEND) {
-            if (in) to = a.k_out.p + b * a.k_out.sb + i * a.k_out.st + (h - hk) * a.k_out.sh;
-        } else if (in && stored) {
-            const int kh = h < hv ? h - hk : h - hv;
-            to = (h < hv ? a.cache.k : a.cache.v) + at + kh * a.cache.head_stride;
-            if (h < hv && sub == 0 && a.cache.weights) a.cache.weights[wt + (long long)kh * a.cache.page_size] = 0.f;
+        if (h >= heads || !to) return;
+        F2 p[N], q[N];
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            p[e] = f2_fma(x[e], rope.cs[e], f2_neg(f2_mul(y[e], rope.sn[e])));
+            q[e] = f2_fma(y[e], rope.cs[e], f2_mul(x[e], rope.sn[e]));
         }
-        if (to) {
-            *((uint4 *)to + sub) = l;
-            *((uint4 *)(to + D / 2 * sizeof(T)) + sub) = r;
-        }
+        *(uint4 *)to = Pairs<T>::pack(p);
+        *(uint4 *)(to + D / 2 * sizeof(T)) = Pairs<T>::pack(q);
+    };
+    int g = share;
+    for (; g < gq; g += a.split) {
+        const int h = g * R::kHeads + own;
+        turn(g, h, a.Hq, qo + h * a.q_out.sh);
+    }
+    gain.load(a.g_k);
+    for (; g < end_k; g += a.split) {
+        const int h = (g - gq) * R::kHeads + own;
+        turn(g, h, a.Hkv, ko ? ko + h * ko_sh : nullptr);
+        if (APPEND && weight && sub == 0 && h < a.Hkv) weight[(long long)h * a.cache.page_size] = 0.f;
+    }
+    for (; g < groups; g += a.split) {   // values go as they are
+        const int h = (g - end_k) * R::kHeads + own;
+        const uint32_t at = take(g);
+        if (!vo || h >= a.Hkv) continue;
+        char *to = vo + h * ko_sh;
+        *(uint4 *)to = lds16(at);
+        *(uint4 *)(to + D / 2 * sizeof(T)) = lds16(at + 512);
     }
 }
 
@@ -178,56 +275,64 @@ constexpr int kNgRing = 5;
 constexpr int kNgStage = 2048 + 512;     // x and dy, low and high pieces of each lane; the row's cosines and sines
 
 template <typename T, int D> struct GainGrad {
-    float x[Vec16<T>::E], y[Vec16<T>::E];
+    F2 x[Rope<T, D>::N], y[Rope<T, D>::N];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int e = 0; e < Rope<T, D>::N; ++e) x[e] = y[e] = 0ull;
+    }
 };
 
 // The heads of one group: x and dy from the stage, dx to `to` (null: a lane without a head).
 template <typename T, int D>
-__device__ __forceinline__ void grad_group(uint32_t stage, char *to, const void *gain, float eps, const Rope<T, D> &rope, GainGrad<T, D> &dg) {
+__device__ __forceinline__ void grad_group(uint32_t stage, char *to, bool norm, uint32_t gain, float eps, const Rope<T, D> &rope,
+                                           GainGrad<T, D> &dg) {
     using R = Rope<T, D>;
-    constexpr int E = R::E;
-    const int lane = threadIdx.x & 31, sub = lane % R::kLanes;
-    float x[E], y[E], p[E], q[E];
-    Vec16<T>::unpack(lds16(stage + lane * 16), x);
-    Vec16<T>::unpack(lds16(stage + 512 + lane * 16), y);
-    Vec16<T>::unpack(lds16(stage + 1024 + lane * 16), p);
-    Vec16<T>::unpack(lds16(stage + 1536 + lane * 16), q);
+    constexpr int N = R::N;
+    const int lane = threadIdx.x & 31;
+    F2 p[N], q[N];
+    {
+        F2 u[N], v[N];
+        Pairs<T>::unpack(lds16(stage + 1024 + lane * 16), u);
+        Pairs<T>::unpack(lds16(stage + 1536 + lane * 16), v);
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float u = p[e], v = q[e];
-        p[e] = u * rope.cs[e] + v * rope.sn[e];
-        q[e] = v * rope.cs[e] - u * rope.sn[e];
-    }
-    if (gain) {
-        float s = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) s = fmaf(x[e], x[e], fmaf(y[e], y[e], s));
-        const float r = rsqrtf(lanes_sum<R::kLanes>(s) * (1.f / D) + eps);
-        const uint4 *g = (const uint4 *)gain + sub;
-        float gx[E], gy[E];
-        Vec16<T>::unpack(__ldg(g), gx);
-        Vec16<T>::unpack(__ldg(g + R::kLanes), gy);
-        float c = 0.f;
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-            x[e] *= r;
-            y[e] *= r;
-            dg.x[e] = fmaf(p[e], x[e], dg.x[e]);
-            dg.y[e] = fmaf(q[e], y[e], dg.y[e]);
-            p[e] *= gx[e];
-            q[e] *= gy[e];
-            c = fmaf(p[e], x[e], fmaf(q[e], y[e], c));
+        for (int e = 0; e < N; ++e) {
+            p[e] = f2_fma(u[e], rope.cs[e], f2_mul(v[e], rope.sn[e]));
+            q[e] = f2_fma(v[e], rope.cs[e], f2_neg(f2_mul(u[e], rope.sn[e])));
         }
-        c = lanes_sum<R::kLanes>(c) * (1.f / D);
+    }
+    if (norm) {
+        F2 x[N], y[N];
+        Pairs<T>::unpack(lds16(stage + lane * 16), x);
+        Pairs<T>::unpack(lds16(stage + 512 + lane * 16), y);
+        F2 s = f2_mul(x[0], x[0]);
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
-            p[e] = r * (p[e] - x[e] * c);
-            q[e] = r * (q[e] - y[e] * c);
+        for (int e = 1; e < N; ++e) s = f2_fma(x[e], x[e], s);
+#pragma unroll
+        for (int e = 0; e < N; ++e) s = f2_fma(y[e], y[e], s);
+        const float r = rsqrtf(lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + eps);
+        const F2 rr = f2(r, r);
+        F2 c = 0ull;
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            x[e] = f2_mul(x[e], rr);
+            y[e] = f2_mul(y[e], rr);
+            dg.x[e] = f2_fma(p[e], x[e], dg.x[e]);
+            dg.y[e] = f2_fma(q[e], y[e], dg.y[e]);
+            p[e] = f2_mul(p[e], lds8(gain + lane % R::kLanes * (R::E * 4) + 8 * e));
+            q[e] = f2_mul(q[e], lds8(gain + (D / 2 + lane % R::kLanes * R::E) * 4 + 8 * e));
+            c = f2_fma(p[e], x[e], f2_fma(q[e], y[e], c));
+        }
+        const float m = lanes_sum<R::kLanes>(f2_sum(c)) * (-1.f / D);
+        const F2 mm = f2(m, m);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            p[e] = f2_mul(rr, f2_fma(x[e], mm, p[e]));
+            q[e] = f2_mul(rr, f2_fma(y[e], mm, q[e]));
         }
     }
     if (!to) return;
-    *((uint4 *)to + sub) = Vec16<T>::pack(p);
-    *((uint4 *)(to + D / 2 * sizeof(T)) + sub) = Vec16<T>::pack(q);
+    *(uint4 *)to = Pairs<T>::pack(p);
+    *(uint4 *)(to + D / 2 * sizeof(T)) = Pairs<T>::pack(q);
 }
 
 // A warp's walk over (row, share) items and the head groups of each.
@@ -250,38 +355,50 @@ struct RowWalk {
 template <typename T, int D>
 __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGradArgs a) {
     using R = Rope<T, D>;
-    constexpr int E = R::E, kWarps = kNgThreads / 32;
+    constexpr int kWarps = kNgThreads / 32;
     extern __shared__ __align__(16) unsigned char dyn[];
     __shared__ int last;
     pdl_wait();
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % R::kLanes, own = lane / R::kLanes;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dyn) + warp * (kNgRing * kNgStage);
+    // both gains as fp32 behind the rings
+    float *gain = (float *)(dyn + kWarps * kNgRing * kNgStage);
+    const uint32_t gains = (uint32_t)__cvta_generic_to_shared(gain);
+    if (a.g_q)
+        for (int d = threadIdx.x; d < 2 * D; d += kNgThreads)
+            gain[d] = Elem<T>::load((const T *)(d < D ? a.g_q : a.g_k), d < D ? d : d - D);
+    __syncthreads();
     GainGrad<T, D> dq, dk;
-#pragma unroll
-    for (int e = 0; e < E; ++e) dq.x[e] = dq.y[e] = dk.x[e] = dk.y[e] = 0.f;
+    dq.clear();
+    dk.clear();
     const int items = a.B * a.max_new * a.split, step = gridDim.x * kWarps;
     const int gq = (a.Hq + R::kHeads - 1) / R::kHeads, groups = gq + (a.Hkv + R::kHeads - 1) / R::kHeads;
-    auto head_at = [&](const HeadsView &v, const RowWalk &r, int h) { return v.p + r.b * v.sb + r.i * v.st + h * v.sh; };
+    auto row_at = [&](const HeadsView &v, const RowWalk &r) { return v.p + r.b * v.sb + r.i * v.st + sub * 16; };
 
     RowWalk f;                           // loads ahead: the next group to request, in rows that count
     f.at(a, blockIdx.x * kWarps + warp, items);
     while (f.live && !f.valid) f.at(a, f.w + step, items);
     bool fresh = true;                   // its row's first group: the row's table line comes with it
+    const char *x = nullptr, *y = nullptr;   // its row in q or k, and in dq_out or dk_out
     int stage_in = 0;
     auto request = [&]() {
         if (f.live) {
-            const uint32_t to = ring + stage_in * kNgStage;
+            const uint32_t to = ring + stage_in * kNgStage + lane * 16;
+            if (fresh && lane < D / 4)
+                cp16(to + 2048, a.rope + (long long)row_position(a.pos, f.b, f.i, a.rope_len, a.err) * D + lane * 4, true);
             const bool is_q = f.g < gq;
+            if (fresh || (!is_q && f.g - a.split < gq)) {
+                x = row_at(is_q ? a.q : a.k, f);
+                y = row_at(is_q ? a.dq_out : a.dk_out, f);
+            }
             const int h = (is_q ? f.g : f.g - gq) * R::kHeads + own;
             const bool ok = h < (is_q ? a.Hq : a.Hkv);
-            const char *x = ok ? head_at(is_q ? a.q : a.k, f, h) : a.q.p, *y = ok ? head_at(is_q ? a.dq_out : a.dk_out, f, h) : a.q.p;
-            cp16(to + lane * 16, x + sub * 16, ok);
-            cp16(to + 512 + lane * 16, x + D / 2 * sizeof(T) + sub * 16, ok);
-            cp16(to + 1024 + lane * 16, y + sub * 16, ok);
-            cp16(to + 1536 + lane * 16, y + D / 2 * sizeof(T) + sub * 16, ok);
-            if (fresh && lane < D / 4)
-                cp16(to + 2048 + lane * 16, a.rope + (long long)row_position(a.pos, f.b, f.i, a.rope_len, a.err) * D + lane * 4, true);
+            const char *xs = x + (ok ? h : 0) * (is_q ? a.q.sh : a.k.sh), *ys = y + (ok ? h : 0) * (is_q ? a.dq_out.sh : a.dk_out.sh);
+            cp16(to, xs, ok);
+            cp16(to + 512, xs + D / 2 * sizeof(T), ok);
+            cp16(to + 1024, ys, ok);
+            cp16(to + 1536, ys + D / 2 * sizeof(T), ok);
             f.g += a.split;
             fresh = f.g >= groups;
             if (fresh) {
@@ -303,33 +420,34 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
                 const bool is_q = r.g < gq;
                 const int h = (is_q ? r.g : r.g - gq) * R::kHeads + own;
                 if (h >= (is_q ? a.Hq : a.Hkv)) continue;
-                char *to = head_at(is_q ? a.dq : a.dk, r, h);
-                *((uint4 *)to + sub) = *((uint4 *)(to + D / 2 * sizeof(T)) + sub) = make_uint4(0u, 0u, 0u, 0u);
+                char *to = is_q ? row_at(a.dq, r) + h * a.dq.sh : row_at(a.dk, r) + h * a.dk.sh;
+                *(uint4 *)to = *(uint4 *)(to + D / 2 * sizeof(T)) = make_uint4(0u, 0u, 0u, 0u);
             }
             continue;
         }
         R rope;
-        for (bool first = true; r.g < groups; r.g += a.split, first = false) {
+        bool first = true;
+        auto take = [&]() {
             cp_wait_group<kNgRing - 2>();
             __syncwarp();
             request();                   // into the stage that was read last
             const uint32_t at = ring + stage * kNgStage;
-            if (first) {
-#pragma unroll
-                for (int e = 0; e < E; e += 4) {
-                    const uint4 c = lds16(at + 2048 + (sub * E + e) * 4), s = lds16(at + 2048 + (D / 2 + sub * E + e) * 4);
-                    Vec16<float>::unpack(c, *(float(*)[4])(rope.cs + e));
-                    Vec16<float>::unpack(s, *(float(*)[4])(rope.sn + e));
-                }
-            }
-            if (r.g < gq) {
-                const int h = r.g * R::kHeads + own;
-                grad_group<T, D>(at, h < a.Hq ? head_at(a.dq, r, h) : nullptr, a.g_q, a.eps, rope, dq);
-            } else {
-                const int h = (r.g - gq) * R::kHeads + own;
-                grad_group<T, D>(at, h < a.Hkv ? head_at(a.dk, r, h) : nullptr, a.g_k, a.eps, rope, dk);
-            }
             stage = stage + 1 == kNgRing ? 0 : stage + 1;
+            if (first) rope.load_shared(at + 2048);
+            first = false;
+            return at;
+        };
+        char *to = row_at(a.dq, r);
+        for (; r.g < gq; r.g += a.split) {
+            const uint32_t at = take();
+            const int h = r.g * R::kHeads + own;
+            grad_group<T, D>(at, h < a.Hq ? to + h * a.dq.sh : nullptr, a.g_q, gains, a.eps, rope, dq);
+        }
+        to = row_at(a.dk, r);
+        for (; r.g < groups; r.g += a.split) {
+            const uint32_t at = take();
+            const int h = (r.g - gq) * R::kHeads + own;
+            grad_group<T, D>(at, h < a.Hkv ? to + h * a.dk.sh : nullptr, a.g_k, gains + 4 * D, a.eps, rope, dk);
         }
     }
     cp_wait_group<0>();
@@ -343,11 +461,15 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
         return v;
     };
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-        const float v[4] = {fold(dq.x[e]), fold(dq.y[e]), fold(dk.x[e]), fold(dk.y[e])};
-        if (own == 0) {
+    for (int e = 0; e < R::N; ++e) {
+        const float2 v[4] = {f2_values(dq.x[e]), f2_values(dq.y[e]), f2_values(dk.x[e]), f2_values(dk.y[e])};
 #pragma unroll
-            for (int c = 0; c < 4; ++c) sum[warp][c * (D / 2) + sub * E + e] = v[c];
+        for (int c = 0; c < 4; ++c) {
+            const float x = fold(v[c].x), y = fold(v[c].y);
+            if (own == 0) {
+                sum[warp][c * (D / 2) + sub * R::E + 2 * e] = x;
+                sum[warp][c * (D / 2) + sub * R::E + 2 * e + 1] = y;
+            }
         }
     }
     __syncthreads();
@@ -393,7 +515,7 @@ int row_split(long long rows, int groups, int sms) {
     long long s = ((long long)sms * 16 + rows - 1) / rows;
     return (int)(s < 1 ? 1 : s > groups ? groups : s);
 }
-constexpr int kNgSmem = kNgThreads / 32 * kNgRing * kNgStage;
+constexpr int kNgSmem = kNgThreads / 32 * kNgRing * kNgStage + 2 * 128 * 4;
 int heads_per_warp(bool bf16, int D) { return 32 / (D / 2 / (bf16 ? 8 : 4)); }
 
 }  // namespace
