@@ -116,6 +116,41 @@ __device__ __forceinline__ uint32_t cvt_bf16x2(float lo, float hi) {
     return r;
 }
 
+// Two fp32 values in one 64-bit register and their packed arithmetic: half the
+// instructions where those, not bytes, hold a kernel up.
+typedef unsigned long long F2;
+__device__ __forceinline__ F2 f2(float x, float y) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
+    return r;
+}
+__device__ __forceinline__ float2 f2_values(F2 a) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
+    return r;
+}
+__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 f2_neg(F2 a) { return a ^ 0x8000000080000000ull; }
+__device__ __forceinline__ float f2_sum(F2 a) {
+    const float2 v = f2_values(a);
+    return v.x + v.y;
+}
+
+__device__ __forceinline__ F2 lds8(uint32_t addr) {
+    F2 r;
+    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(addr));
+    return r;
+}
+
 // E values of a 16-byte vector as floats and back (E = 8 bf16 or 4 fp32).
 template <typename T> struct Vec16;
 template <> struct Vec16<uint16_t> {

@@ -216,24 +216,25 @@ template <int D_, int MODE> struct Bf16Tile {
     }
 };
 
-// fp32 rows on the CUDA cores in full fp32: a lane holds D / 32 dims of q and of
-// the sums, a group of 8 keys x 4 heads gives 32 partial products per lane, which
-// 31 exchanges turn into one whole score per lane (lane = 4 key + head).
+// fp32 rows on the CUDA cores in full fp32, two values an instruction: a lane holds
+// D / 32 dims of q and of the sums, a group of 8 keys x 4 heads gives 32 partial
+// products per lane, which 31 exchanges turn into one whole score per lane (lane =
+// 4 key + head).
 template <int D_, int NG> struct F32Tile {
     using T = float;
-    static constexpr int D = D_, KT = kPaStage / (8 * D), V = D / 32;
+    static constexpr int D = D_, KT = kPaStage / (8 * D), V = D / 64;   // V: pairs of dims of a lane
     static constexpr int kHeads = 4 * NG;
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = 3;
-    float q[4 * NG][V], o[4 * NG][V], m[NG], l[NG];      // m, l: of head 4 ng + lane % 4
+    F2 q[4 * NG][V], o[4 * NG][V];
+    float m[NG], l[NG];                                  // of head 4 ng + lane % 4
 
     static __device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)(r * (4 * D) + (c << 4)); }
-    static __device__ __forceinline__ void row(uint32_t addr, float (&f)[V]) {
-        if (V == 4) {
-            asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];"
-                         : "=f"(f[0]), "=f"(f[1]), "=f"(f[V > 2 ? 2 : 0]), "=f"(f[V > 2 ? 3 : 1]) : "r"(addr) : "memory");
+    static __device__ __forceinline__ void row(uint32_t addr, F2 (&f)[V]) {
+        if (V == 2) {
+            asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(f[0]), "=l"(f[V - 1]) : "r"(addr) : "memory");
         } else {
-            asm volatile("ld.shared.v2.f32 {%0, %1}, [%2];" : "=f"(f[0]), "=f"(f[1]) : "r"(addr) : "memory");
+            f[0] = lds8(addr);
         }
     }
     __device__ __forceinline__ void load_q(const T *src, int heads) {
@@ -241,7 +242,7 @@ template <int D_, int NG> struct F32Tile {
 #pragma unroll
         for (int h = 0; h < 4 * NG; ++h)
 #pragma unroll
-            for (int i = 0; i < V; ++i) q[h][i] = h < heads ? src[h * D + lane * V + i] : 0.f;
+            for (int i = 0; i < V; ++i) q[h][i] = h < heads ? *(const F2 *)(src + h * D + lane * (2 * V) + 2 * i) : 0ull;
     }
     __device__ __forceinline__ void reset() {
 #pragma unroll
@@ -249,10 +250,11 @@ template <int D_, int NG> struct F32Tile {
 #pragma unroll
         for (int h = 0; h < 4 * NG; ++h)
 #pragma unroll
-            for (int i = 0; i < V; ++i) o[h][i] = 0.f;
+            for (int i = 0; i < V; ++i) o[h][i] = 0ull;
     }
     __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, float *pad, int key0, int len, float scale, float *scores, int heads) {
         const int lane = threadIdx.x & 31;
+        const uint32_t pads = (uint32_t)__cvta_generic_to_shared(pad);
 #pragma unroll 1
         for (int sub = 0; sub < KT / 8; ++sub) {
             const int base = key0 + 8 * sub;
@@ -263,14 +265,13 @@ template <int D_, int NG> struct F32Tile {
                 float x[32];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    float f[V];
-                    row(ks + (8 * sub + k) * (4 * D) + lane * (4 * V), f);
+                    F2 f[V];
+                    row(ks + (8 * sub + k) * (4 * D) + lane * (8 * V), f);
 #pragma unroll
                     for (int h = 0; h < 4; ++h) {
-                        float a = f[0] * q[4 * n + h][0];
-#pragma unroll
-                        for (int i = 1; i < V; ++i) a = fmaf(f[i], q[4 * n + h][i], a);
-                        x[4 * k + h] = a;
+                        F2 a = f2_mul(f[0], q[4 * n + h][0]);
+                        if (V == 2) a = f2_fma(f[V - 1], q[4 * n + h][V - 1], a);
+                        x[4 * k + h] = f2_sum(a);
                     }
                 }
 #pragma unroll
@@ -290,29 +291,31 @@ template <int D_, int NG> struct F32Tile {
                 mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
                 mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
                 mx = fmaxf(m[n], mx);
-                const float b = base_of(mx), alpha = exp2f(m[n] - b), p = exp2f(s - b);
-                m[n] = mx;
-                l[n] = l[n] * alpha + p;
-                pad[lane] = p;
+                const float b = base_of(mx), p = exp2f(s - b);
+                if (__any_sync(0xFFFFFFFFu, mx != m[n])) {
+                    const float alpha = exp2f(m[n] - b);
+                    m[n] = mx;
+                    l[n] *= alpha;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const float a = __shfl_sync(0xFFFFFFFFu, alpha, j);
+                    for (int j = 0; j < 4; ++j) {
+                        const float a = __shfl_sync(0xFFFFFFFFu, alpha, j);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) o[4 * n + j][i] *= a;
+                        for (int i = 0; i < V; ++i) o[4 * n + j][i] = f2_mul(o[4 * n + j][i], f2(a, a));
+                    }
                 }
+                l[n] += p;
+                *(float2 *)(pad + 2 * lane) = make_float2(p, p);   // as the pairs that the products below take
                 __syncwarp();
 #pragma unroll
                 for (int k = 0; k < 8; ++k) {
-                    const float4 w = *(const float4 *)(pad + 4 * k);
-                    float f[V];
-                    row(vs + (8 * sub + k) * (4 * D) + lane * (4 * V), f);
+                    F2 w[4], f[V];
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(w[0]), "=l"(w[1]) : "r"(pads + 32 * k) : "memory");
+                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(w[2]), "=l"(w[3]) : "r"(pads + 32 * k + 16) : "memory");
+                    row(vs + (8 * sub + k) * (4 * D) + lane * (8 * V), f);
 #pragma unroll
-                    for (int i = 0; i < V; ++i) {
-                        o[4 * n][i] = fmaf(w.x, f[i], o[4 * n][i]);
-                        o[4 * n + 1][i] = fmaf(w.y, f[i], o[4 * n + 1][i]);
-                        o[4 * n + 2][i] = fmaf(w.z, f[i], o[4 * n + 2][i]);
-                        o[4 * n + 3][i] = fmaf(w.w, f[i], o[4 * n + 3][i]);
-                    }
+                    for (int h = 0; h < 4; ++h)
+#pragma unroll
+                        for (int i = 0; i < V; ++i) o[4 * n + h][i] = f2_fma(w[h], f[i], o[4 * n + h][i]);
                 }
                 __syncwarp();
             }
@@ -334,7 +337,7 @@ template <int D_, int NG> struct F32Tile {
 #pragma unroll
         for (int h = 0; h < 4 * NG; ++h)
 #pragma unroll
-            for (int i = 0; i < V; ++i) so[h * kMergeStride + lane * V + i] = o[h][i];
+            for (int i = 0; i < V; ++i) *(F2 *)(so + h * kMergeStride + lane * (2 * V) + 2 * i) = o[h][i];
     }
 };
 
@@ -418,13 +421,13 @@ template <typename P>
 __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(AttendArgs a) {
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads;
-    constexpr int kJoin = kPaWarps * P::kMergeStride;    // pieces whose maxima the merge area holds
-    constexpr int kJoinCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;   // float4 columns of a thread
-    constexpr int kJoinEarly = 8 / kJoinCols, kJoinBatch = 12 / kJoinCols;
     constexpr int kPart = H * (D + 2);                   // floats of a piece: sums [H][D], then (maximum, sum) [H]
+    constexpr int kJoin = kPaWarps * S * kPaStage / (4 * kPart);   // pieces that the rings hold
+    constexpr int kJoinCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;   // float4 columns of a thread
     constexpr int kRow = D * (int)sizeof(T), kChunks = kRow / 16, kRowsPer = 32 / kChunks;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int last;
+    __shared__ int4 join[2];
+    int joins = 0;                                       // of thread 0
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_wait();
     pdl_trigger();
@@ -554,99 +557,74 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                 }
             }
         }
-        if (!whole) {
-            __syncthreads();                             // the piece is written; the merge area was read
-            if (tid == 0) {
+        __syncthreads();                                 // the piece is written; the merge area is free again
+        if (!whole && tid == 0) {
+            __threadfence();
+            if (atomicAdd(a.counter + seg, 1) == c1 - c0) {
                 __threadfence();
-                last = atomicAdd(a.counter + seg, 1) == c1 - c0;
-                __threadfence();
-            }
-            __syncthreads();
-            if (last) {
-                // piece i of the segment: CTA c0's second slot, the others' first
-                auto piece_part = [&](int i) { return a.part + (long long)(i == 0 ? 2 * c0 + 1 : 2 * (c0 + i)) * kPart; };
-                const int pieces = c1 - c0 + 1;
-                float4 early[kJoinCols][kJoinEarly];     // the first pieces' sums come with the maxima
-#pragma unroll
-                for (int c = 0; c < kJoinCols; ++c)
-#pragma unroll
-                    for (int i = 0; i < kJoinEarly; ++i)
-                        if (i < pieces && tid + c * kPaThreads < n * (D / 4)) early[c][i] = __ldcg((const float4 *)piece_part(i) + tid + c * kPaThreads);
-                float *top = merge;                      // [kJoin][H]: maxima of kJoin pieces at a time
-                for (int h = warp; h < n; h += kPaWarps) {
-                    float M = -INFINITY, L = 0.f;
-                    for (int i0 = lane; i0 < pieces; i0 += 64) {
-                        float2 ml[2];
-#pragma unroll
-                        for (int k = 0; k < 2; ++k)
-                            ml[k] = i0 + 32 * k < pieces ? __ldcg((const float2 *)(piece_part(i0 + 32 * k) + H * D + 2 * h)) : make_float2(-INFINITY, 0.f);
-#pragma unroll
-                        for (int k = 0; k < 2; ++k) {
-                            if (i0 + 32 * k < min(pieces, kJoin)) top[(i0 + 32 * k) * H + h] = ml[k].x;
-                            const float m = fmaxf(M, ml[k].x);
-                            L = L * exp2f(M - base_of(m)) + exp2f(ml[k].x - base_of(m)) * ml[k].y;
-                            M = m;
-                        }
-                    }
-#pragma unroll
-                    for (int o = 16; o > 0; o >>= 1) {
-                        const float m2 = __shfl_xor_sync(0xFFFFFFFFu, M, o), l2 = __shfl_xor_sync(0xFFFFFFFFu, L, o);
-                        const float m = fmaxf(M, m2);
-                        L = L * exp2f(M - base_of(m)) + l2 * exp2f(m2 - base_of(m));
-                        M = m;
-                    }
-                    if (lane == 0) sm[h] = M, sl[h] = L;
-                }
-                __syncthreads();
-                float x[kJoinCols][4] = {};
-                for (int i0 = 0; i0 < pieces; i0 += kJoin) {
-                    const int count = min(kJoin, pieces - i0);
-                    if (i0 > 0) {
-                        __syncthreads();
-                        for (int e = tid; e < count * n; e += kPaThreads)
-                            top[e / n * H + e % n] = __ldcg(piece_part(i0 + e / n) + H * D + 2 * (e % n));
-                        __syncthreads();
-                    }
-#pragma unroll
-                    for (int c = 0; c < kJoinCols; ++c) {
-                        const int e = tid + c * kPaThreads, h = e / (D / 4);
-                        if (h >= n) continue;
-                        const float base = base_of(sm[h]);
-                        auto add = [&](int i, const float4 &y) {
-                            const float k = exp2f(top[i * H + h] - base);
-                            x[c][0] = fmaf(k, y.x, x[c][0]);
-                            x[c][1] = fmaf(k, y.y, x[c][1]);
-                            x[c][2] = fmaf(k, y.z, x[c][2]);
-                            x[c][3] = fmaf(k, y.w, x[c][3]);
-                        };
-                        if (i0 == 0) {
-#pragma unroll
-                            for (int i = 0; i < kJoinEarly; ++i)
-                                if (i < count) add(i, early[c][i]);
-                        }
-                        for (int i = i0 == 0 ? kJoinEarly : 0; i < count; i += kJoinBatch) {
-                            float4 y[kJoinBatch];
-#pragma unroll
-                            for (int k = 0; k < kJoinBatch; ++k)
-                                if (i + k < count) y[k] = __ldcg((const float4 *)piece_part(i0 + i + k) + e);
-#pragma unroll
-                            for (int k = 0; k < kJoinBatch; ++k)
-                                if (i + k < count) add(i + k, y[k]);
-                        }
-                    }
-                }
-#pragma unroll
-                for (int c = 0; c < kJoinCols; ++c) {
-                    const int e = tid + c * kPaThreads, h = e / (D / 4);
-                    if (h < n) write_out<T, D>(a, hq + h, 4 * (e % (D / 4)), x[c], sm[h], sl[h]);
-                }
-                if (tid == 0) a.counter[seg] = 0;
+                a.counter[seg] = 0;
+                join[joins++] = make_int4(p.b, p.h, c0, c1);
             }
         }
-        __syncthreads();                                 // the merge area is free again
         p = after;
     }
+    // Segments of which this CTA finished the last piece (its first and its last
+    // segment at most), joined when the ring is free to take the pieces: all of them
+    // on their way at once, then added in CTA order.
     cp_wait_group<0>();
+    if (tid == 0 && joins < 2) join[joins].x = -1;
+    __syncthreads();
+    for (int k = 0; k < 2 && join[k].x >= 0; ++k) {
+        const int4 w = join[k];
+        const int h0 = w.y % tiles * H, n = min(H, G - h0), pieces = w.w - w.z + 1;
+        const long long hq = (long long)w.x * a.Hq + w.y / tiles * G + h0;
+        const uint32_t buf = (uint32_t)__cvta_generic_to_shared(smem);
+        const float *got = (const float *)smem;
+        float x[kJoinCols][4] = {}, M[kJoinCols], L[kJoinCols] = {};
+#pragma unroll
+        for (int c = 0; c < kJoinCols; ++c) M[c] = -INFINITY;
+        for (int i0 = 0; i0 < pieces; i0 += kJoin) {
+            const int count = min(kJoin, pieces - i0);
+            for (int e = tid; e < count * (kPart / 4); e += kPaThreads) {
+                const int i = e / (kPart / 4);
+                // piece i of the segment: CTA c0's second slot, the others' first
+                const int slot = i0 + i == 0 ? 2 * w.z + 1 : 2 * (w.z + i0 + i);
+                cp16(buf + e * 16, a.part + (long long)slot * kPart + (e - i * (kPart / 4)) * 4, true);
+            }
+            cp_group();
+            cp_wait_group<0>();
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < kJoinCols; ++c) {
+                const int e = tid + c * kPaThreads, h = e / (D / 4);
+                if (h >= n) continue;
+                float top = M[c];
+                for (int i = 0; i < count; ++i) top = fmaxf(top, got[i * kPart + H * D + 2 * h]);
+                const float base = base_of(top), old = exp2f(M[c] - base);
+                M[c] = top;
+                L[c] *= old;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) x[c][d] *= old;
+#pragma unroll 4
+                for (int i = 0; i < count; ++i) {
+                    const float2 ml = *(const float2 *)(got + i * kPart + H * D + 2 * h);
+                    const float4 y = *(const float4 *)(got + i * kPart + e * 4);
+                    const float f = exp2f(ml.x - base);
+                    L[c] = fmaf(f, ml.y, L[c]);
+                    x[c][0] = fmaf(f, y.x, x[c][0]);
+                    x[c][1] = fmaf(f, y.y, x[c][1]);
+                    x[c][2] = fmaf(f, y.z, x[c][2]);
+                    x[c][3] = fmaf(f, y.w, x[c][3]);
+                }
+            }
+            __syncthreads();
+        }
+#pragma unroll
+        for (int c = 0; c < kJoinCols; ++c) {
+            const int e = tid + c * kPaThreads, h = e / (D / 4);
+            if (h < n) write_out<T, D>(a, hq + h, 4 * (e % (D / 4)), x[c], M[c], L[c]);
+        }
+    }
 }
 
 // weights[j] += sum_h 2^(s_jh - M_h) / L_h from the scores the attention kernel

@@ -19,42 +19,6 @@ constexpr int kNrThreads = 128;
 constexpr int kNrRing = 8;               // head groups a warp has in flight
 constexpr int kNrStage = 1024;           // bytes of one: the lanes' low pieces, then their high ones
 
-// Two fp32 values in one 64-bit register and their packed arithmetic: half the
-// instructions, which is what the forward and the gradient were held up by (64% of
-// the issue slots at 4.7 and 4.2 TB/s with one value an instruction).
-typedef unsigned long long F2;
-__device__ __forceinline__ F2 f2(float x, float y) {
-    F2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(x), "f"(y));
-    return r;
-}
-__device__ __forceinline__ float2 f2_values(F2 a) {
-    float2 r;
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(a));
-    return r;
-}
-__device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
-    F2 r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
-    F2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ F2 f2_neg(F2 a) { return a ^ 0x8000000080000000ull; }
-__device__ __forceinline__ float f2_sum(F2 a) {
-    const float2 v = f2_values(a);
-    return v.x + v.y;
-}
-
-__device__ __forceinline__ F2 lds8(uint32_t addr) {
-    F2 r;
-    asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(addr));
-    return r;
-}
-
 // 16 bytes as pairs of values, and back.
 template <typename T> struct Pairs {
     static constexpr int N = Vec16<T>::E / 2;
