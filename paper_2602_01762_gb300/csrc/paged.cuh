@@ -73,7 +73,8 @@ struct EvictArgs {
     int *err;
 };
 
-constexpr int kAttendUnit = 128;         // keys per unit of the attention's work split
+constexpr int kAttendUnit = 64;          // keys per unit of the attention's work split
+constexpr int kAttendCost = 1;           // units that a segment costs beside its keys
 // Query heads that share one pass over a KV head's rows.
 int attend_head_tile(bool bf16, int G);
 size_t attend_part_floats(bool bf16, int D, int G, int sms);

@@ -133,7 +133,7 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
     const long long rows = (long long)c.max_pages * c.page_size;
     // work units and row numbers are 32-bit
     if (rows > (1LL << 30) || (long long)c.max_batch * c.n_q_heads > (1LL << 24) ||
-        (long long)c.max_batch * c.n_q_heads * (rows / kAttendUnit + 1) > (1LL << 30))
+        (long long)c.max_batch * c.n_q_heads * (rows / kAttendUnit + 1 + kAttendCost) > (1LL << 30))
         return fail(nullptr, PRISM_ERR_CAPACITY, "max_batch * n_q_heads * max_pages * page_size is too large");
 
     prism_paged *p = new (std::nothrow) prism_paged;

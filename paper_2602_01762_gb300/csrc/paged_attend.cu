@@ -98,16 +98,18 @@ template <int D_, int MODE> struct Bf16Tile {
         for (int sub = 0; sub < KT / 16; ++sub) {
             const int base = key0 + 16 * sub;
             if (sub > 0 && base >= len) break;
-            float s[NT][4];
+            float s[NT][4], s2[NT][4];                   // even and odd steps over D: half the chain of products
 #pragma unroll
-            for (int t = 0; t < NT; ++t) s[t][0] = s[t][1] = s[t][2] = s[t][3] = 0.f;
+            for (int t = 0; t < NT; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[t][i] = s2[t][i] = 0.f;
             const int kr = 16 * sub + (lane & 15);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 uint32_t a[4];
                 lds_x4(ks + piece(kr, 2 * k + (lane >> 4)), a);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma_bf16(s[t], a, qf[k][t][0], qf[k][t][1]);
+                for (int t = 0; t < NT; ++t) mma_bf16(k & 1 ? s2[t] : s[t], a, qf[k][t][0], qf[k][t][1]);
             }
             const bool in0 = base + g < len, in1 = base + g + 8 < len;
             float mn[NT][2];
@@ -115,7 +117,7 @@ template <int D_, int MODE> struct Bf16Tile {
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[t][i] *= scale;
+                for (int i = 0; i < 4; ++i) s[t][i] = (s[t][i] + s2[t][i]) * scale;
                 if (scores) {
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
@@ -341,13 +343,18 @@ template <int D_, int NG> struct F32Tile {
     }
 };
 
+// A segment is one (sequence, KV head, head tile): blocks of kAttendUnit keys, and
+// before them kAttendCost units without keys that stand for what a segment costs
+// beside its rows (its queries, merge and result).
 __device__ __forceinline__ int blocks_of(int len) { return max(1, (len + kAttendUnit - 1) / kAttendUnit); }
+__device__ __forceinline__ int units_of(int len) { return kAttendCost + blocks_of(len); }
 
 // Walk over the pieces of a CTA's share: the blocks [blk0, blk1) of nblk of one
-// (sequence, KV head, head tile) segment after the other.  Each lane keeps the
-// length of one of the next 32 sequences, so that a step waits for no load.
+// segment after the other; parts of a segment without blocks are passed over.  Each
+// lane keeps the length of one of the next 32 sequences, so that a step waits for
+// no load.
 struct Pieces {
-    int u, u1, b, h, heads, blk0, blk1, nblk, len;
+    int u, u1, seg, b, h, heads, blk0, blk1, nblk, len;   // seg: the segment's first unit
     int base, lens;                      // lane i: rows of sequence base + i
     __device__ __forceinline__ void fetch(const AttendArgs &a) {
         const int at = b + (int)(threadIdx.x & 31);
@@ -358,7 +365,13 @@ struct Pieces {
         len = __shfl_sync(0xFFFFFFFFu, lens, b - base);
         nblk = blocks_of(len);
     }
-    __device__ __forceinline__ void begin(const AttendArgs &a, const UnitRange &r, int n_heads) {
+    __device__ __forceinline__ bool cut() {
+        blk0 = max(u - seg - kAttendCost, 0);
+        u = min(seg + kAttendCost + nblk, u1);
+        blk1 = max(u - seg - kAttendCost, 0);
+        return blk0 < blk1;
+    }
+    __device__ __forceinline__ bool begin(const AttendArgs &a, const UnitRange &r, int n_heads) {
         u = r.u0;
         u1 = r.u1;
         b = r.b;
@@ -370,21 +383,21 @@ struct Pieces {
             fetch(a);
         }
         sequence();
-        h = (u - r.first) / nblk;
-        blk0 = (u - r.first) % nblk;
-        blk1 = min(nblk, blk0 + u1 - u);
+        h = (u - r.first) / (kAttendCost + nblk);
+        seg = r.first + h * (kAttendCost + nblk);
+        return cut() || next(a);
     }
     __device__ __forceinline__ bool next(const AttendArgs &a) {
-        u += blk1 - blk0;
-        if (u >= u1) return false;
-        blk0 = 0;
-        if (++h == heads) {
-            h = 0;
-            if (++b - base == 32) fetch(a);
-            sequence();
+        while (u < u1) {
+            seg = u;
+            if (++h == heads) {
+                h = 0;
+                if (++b - base == 32) fetch(a);
+                sequence();
+            }
+            if (cut()) return true;
         }
-        blk1 = min(nblk, u1 - u);
-        return true;
+        return false;
     }
     __device__ __forceinline__ int rows() const { return min(blk1 * kAttendUnit, len) - blk0 * kAttendUnit; }
 };
@@ -410,7 +423,7 @@ template <typename P> constexpr size_t attend_smem() {
 }
 
 // Persistent CTAs of four warps, two per SM.  The ragged (sequence, KV head,
-// block of 128 keys) units are cut into equal contiguous shares, one per CTA, so
+// block of 64 keys) units are cut into equal contiguous shares, one per CTA, so
 // that long and short sequences keep every SM equally busy; a segment cut between
 // CTAs is joined by the last of them to finish (in CTA order: the result does not
 // depend on which that is).  Within a CTA the tiles of KT keys go to the warps in
@@ -435,7 +448,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
     UnitRange r;
     if (!unit_range<kPaThreads>(r, a.B, heads, a.min_units,
-                                [&](int b) { return paged_len(a.cache, b, a.added, a.err); }, blocks_of))
+                                [&](int b) { return paged_len(a.cache, b, a.added, a.err); }, units_of))
         return;
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * kPaStage);
@@ -444,7 +457,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
 
     Pieces p;                                            // the piece being computed
-    p.begin(a, r, heads);
+    if (!p.begin(a, r, heads)) return;
 
     // Loads run ahead of the computation: their own walk, and the pool place of each
     // lane's row of the next two tiles, so that no load waits for a block-table entry.
@@ -526,8 +539,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
         const int seg = p.b * heads + p.h;
-        const int seg0 = p.u - p.blk0;                   // the segment's first unit
-        const int c0 = seg0 / r.per, c1 = (seg0 + p.nblk - 1) / r.per;
+        const int first = p.seg + kAttendCost;           // unit of the segment's first block
+        const int c0 = first / r.per, c1 = (first + p.nblk - 1) / r.per;
         const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
         float *part = a.part + (long long)slot * kPart;
         for (int e = tid; e < n * (D / 4); e += kPaThreads) {
@@ -741,7 +754,7 @@ cudaError_t prepare_attend_kernels() {
 cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s) {
     const int G = a.Hq / a.Hkv, ht = attend_head_tile(bf16, G);
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
-    const long long most = a.B * (long long)a.Hkv * ((G + ht - 1) / ht) * ((cap + kAttendUnit - 1) / kAttendUnit);
+    const long long most = a.B * (long long)a.Hkv * ((G + ht - 1) / ht) * (kAttendCost + (cap + kAttendUnit - 1) / kAttendUnit);
     const int grid = (int)(most < sms * kPaCtasPerSm ? most : sms * kPaCtasPerSm);
     cudaError_t e = with_tile(bf16, D, G, [&](auto tile) {
         using P = decltype(tile);
