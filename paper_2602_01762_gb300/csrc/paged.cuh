@@ -69,6 +69,7 @@ struct AttendArgs {
 struct EvictArgs {
     PagedView src, dst;
     int32_t *kept;                       // [B, Hkv, budget]
+    int *counter;                        // last-CTA ticket (left at zero)
     int B, Hkv, budget, sinks, recent;
     int *err;
 };

@@ -19,7 +19,7 @@ struct prism_paged {
     float *scores = nullptr;     // [max_batch, Hq, max_pages * page_size] (track_weights)
     float2 *stat = nullptr;      // [max_batch, Hq] (track_weights)
     float *grad_part = nullptr;  // [CTAs, 2, D]
-    int *counter = nullptr;      // attention tickets, then the gradient's (all left at zero)
+    int *counter = nullptr;      // attention tickets, then the gradient's and the eviction's (all left at zero)
     int counters = 0;
     int *err = nullptr;
     char error[256] = "";
@@ -160,7 +160,7 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
         bytes = (bytes + n + 255) & ~(size_t)255;
         return at;
     };
-    const size_t err = take(sizeof(int)), counter = take(sizeof(int) * ((size_t)p->counters + 1));
+    const size_t err = take(sizeof(int)), counter = take(sizeof(int) * ((size_t)p->counters + 2));
     const size_t zeroed = bytes;
     const size_t part = take(sizeof(float) * attend_part_floats(p->bf16, c.head_dim, G, p->sms));
     const size_t grad = take(sizeof(float) * 2 * c.head_dim * norm_rope_grad_ctas(p->sms));
@@ -286,7 +286,7 @@ prism_status prism_paged_evict(prism_paged *p, const prism_paged_cache *src, con
         c.need(budget <= (1 << 30), PRISM_ERR_CAPACITY, "budget above 2^30");
     }
     if (c.s != PRISM_OK) return c.s;
-    a.kept = kept, a.B = src->batch, a.Hkv = p->cfg.n_kv_heads, a.budget = budget, a.sinks = sinks, a.recent = recent, a.err = p->err;
+    a.kept = kept, a.counter = p->counter + p->counters + 1, a.B = src->batch, a.Hkv = p->cfg.n_kv_heads, a.budget = budget, a.sinks = sinks, a.recent = recent, a.err = p->err;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
     return cuda_status(p, launch_paged_evict(a, p->cfg.head_dim * c.es(), p->sms, (cudaStream_t)stream), "prism_paged_evict");

@@ -15,7 +15,7 @@ namespace {
 
 constexpr int kEvThreads = 1024;
 constexpr int kEvWarps = kEvThreads / 32;
-constexpr int kEvBatch = 8;              // rows a thread has in flight
+constexpr int kEvBatch = 4;              // rows a thread has in flight
 constexpr uint32_t kNan = 0x7FFFFFFFu;
 constexpr int kEvCached = 48 * 1024;     // rows whose keys shared memory holds
 
@@ -156,10 +156,11 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, i
     if (lane == 0) warp_gt[warp] = gt, warp_eq[warp] = eq;
     __syncthreads();
     if (warp == 0) {
-        const int g = __reduce_add_sync(0xFFFFFFFFu, warp_gt[lane]), e = __reduce_add_sync(0xFFFFFFFFu, warp_eq[lane]);
+        const int g = __reduce_add_sync(0xFFFFFFFFu, lane < kEvWarps ? warp_gt[lane] : 0);
+        const int e = __reduce_add_sync(0xFFFFFFFFu, lane < kEvWarps ? warp_eq[lane] : 0);
         if (lane < cs) dsmem_st(&share_gt[rank], lane, g), dsmem_st(&share_eq[rank], lane, e);
     }
-    static_assert(kEvWarps == 32, "one lane per warp");
+    static_assert(kEvWarps <= 32, "a lane per warp");
     cluster_sync_all();
     gt = eq = 0;
     for (int r = 0; r < rank; ++r) gt += share_gt[r], eq += share_eq[r];
@@ -180,23 +181,36 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, i
 
 // Copies the kept rows of K, V and the weights, kCpRows destination rows of one KV
 // head per warp: a lane each looks the rows up, then the warp moves them 512 bytes
-// at a time.  Also sets the destination's lengths.
-constexpr int kCpThreads = 256;
+// at a time.  Rows that are kept whatever their weights (all of a sequence within
+// its budget, the sinks, the recent ones) do not wait for the selection: the copy
+// starts beside it, the last rows first.  Also sets the destination's lengths.
+constexpr int kCpThreads = 128;
 constexpr int kCpRows = 8;
 constexpr int kCpUnroll = 4;
 __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int row_bytes) {
-    pdl_wait();
+    // Before the wait: the selection lets this kernel start once its own wait is over,
+    // so all but `kept` is final.
     pdl_trigger();
     const int lane = threadIdx.x & 31;
     const long long gid = (long long)blockIdx.x * kCpThreads + threadIdx.x;
-    for (long long b = gid; b < a.B; b += (long long)gridDim.x * kCpThreads)
-        a.dst.kv_len[b] = min(paged_len(a.src, (int)b, 0, nullptr), a.budget);
-    const int chunks = (a.budget + kCpRows - 1) / kCpRows;
+    const int chunks = (a.budget + kCpRows - 1) / kCpRows, heads = a.B * a.Hkv;
     const long long w = gid >> 5;
-    const long long bh = w / chunks;
-    if (bh >= (long long)a.B * a.Hkv) return;
-    const int b = (int)(bh / a.Hkv), h = (int)(bh - (long long)b * a.Hkv), j = (int)(w - bh * chunks) * kCpRows + lane;
-    const int slot = lane < kCpRows && j < a.budget ? a.kept[bh * a.budget + j] : -1;
+    const int chunk = chunks - 1 - (int)(w / heads), bh = (int)(w % heads);
+    const bool work = chunk >= 0;
+    const int b = bh / a.Hkv, h = bh - b * a.Hkv, j0 = chunk * kCpRows, j = j0 + lane;
+    const int len = paged_len(a.src, b, 0, nullptr);
+    // The last CTA to come here sets the lengths at its end: dst's may be src's, which
+    // every warp has read by then.
+    __syncthreads();
+    bool last = threadIdx.x == 0 && atomicAdd(a.counter, 1) == (int)gridDim.x - 1;
+    const bool early = len <= a.budget || j0 + kCpRows <= a.sinks || j0 >= a.budget - a.recent;
+    if (!(work && early)) pdl_wait();
+    last = __any_sync(0xFFFFFFFFu, last);
+    int slot = -1;
+    if (work && lane < kCpRows && j < a.budget) {
+        if (len <= a.budget) slot = j < len ? j : -1;
+        else slot = !early ? a.kept[(long long)bh * a.budget + j] : j < a.sinks ? j : len - a.budget + j;
+    }
     bool ok = slot >= 0;
     long long from = 0, to = 0;
     if (ok) {
@@ -212,8 +226,7 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
     }
     const int per = row_bytes / 16, both = 2 * per;      // 16-byte pieces of a K row, of a K and a V row
     const uint32_t rows = __ballot_sync(0xFFFFFFFFu, ok);
-    if (!rows) return;
-    for (int c0 = 0; c0 < kCpRows * both; c0 += 32 * kCpUnroll) {
+    for (int c0 = 0; rows && c0 < kCpRows * both; c0 += 32 * kCpUnroll) {
         uint4 x[kCpUnroll];
         char *dst[kCpUnroll];
 #pragma unroll
@@ -228,6 +241,10 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
         for (int u = 0; u < kCpUnroll; ++u)
             if (dst[u]) *(uint4 *)dst[u] = x[u];
     }
+    if (!last) return;
+    pdl_wait();                          // the selection reads them too
+    for (int i = lane; i < a.B; i += 32) a.dst.kv_len[i] = min(paged_len(a.src, i, 0, nullptr), a.budget);
+    if (lane == 0) *a.counter = 0;
 }
 
 }  // namespace
