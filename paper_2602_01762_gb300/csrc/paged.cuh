@@ -61,6 +61,7 @@ struct AttendArgs {
     float2 *stat;                        // [B, Hq]: (maximum score, 1 / sum), with scores
     float *part;                         // two pieces per CTA
     int *counter;                        // [B * head tiles] tickets (left at zero)
+    int *group_counter;                  // two per CTA (left at zero)
     int B, Hq, Hkv, added, min_units;
     float scale_log2;                    // softmax scale * log2(e)
     int *err;
@@ -79,6 +80,7 @@ constexpr int kAttendCost = 1;           // units that a segment costs beside it
 // Query heads that share one pass over a KV head's rows.
 int attend_head_tile(bool bf16, int G);
 size_t attend_part_floats(bool bf16, int D, int G, int sms);
+int attend_ctas(int sms);
 // Kernel attributes, before any capture.
 cudaError_t prepare_attend_kernels();
 cudaError_t prepare_evict_kernels();

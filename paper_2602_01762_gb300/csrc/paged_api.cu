@@ -19,8 +19,11 @@ struct prism_paged {
     float *scores = nullptr;     // [max_batch, Hq, max_pages * page_size] (track_weights)
     float2 *stat = nullptr;      // [max_batch, Hq] (track_weights)
     float *grad_part = nullptr;  // [CTAs, 2, D]
-    int *counter = nullptr;      // attention tickets, then the gradient's and the eviction's (all left at zero)
-    int counters = 0;
+    // tickets, all left at zero: the attention's segments, then its CTAs', the gradient's, the eviction's
+    int *counter = nullptr;
+    int segments = 0, cta_tickets = 0;
+    int *grad_ticket() const { return counter + segments + cta_tickets; }
+    int *evict_ticket() const { return grad_ticket() + 1; }
     int *err = nullptr;
     char error[256] = "";
 };
@@ -153,14 +156,15 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
         return cuda_status(nullptr, e, "prism_paged_create");
     }
     const int G = c.n_q_heads / c.n_kv_heads, ht = attend_head_tile(p->bf16, G);
-    p->counters = c.max_batch * c.n_kv_heads * ((G + ht - 1) / ht);
+    p->segments = c.max_batch * c.n_kv_heads * ((G + ht - 1) / ht);
+    p->cta_tickets = 2 * attend_ctas(p->sms);
     size_t bytes = 0;
     auto take = [&](size_t n) {
         const size_t at = bytes;
         bytes = (bytes + n + 255) & ~(size_t)255;
         return at;
     };
-    const size_t err = take(sizeof(int)), counter = take(sizeof(int) * ((size_t)p->counters + 2));
+    const size_t err = take(sizeof(int)), counter = take(sizeof(int) * ((size_t)p->segments + p->cta_tickets + 2));
     const size_t zeroed = bytes;
     const size_t part = take(sizeof(float) * attend_part_floats(p->bf16, c.head_dim, G, p->sms));
     const size_t grad = take(sizeof(float) * 2 * c.head_dim * norm_rope_grad_ctas(p->sms));
@@ -221,7 +225,7 @@ prism_status prism_qk_norm_rope_backward(prism_paged *p, const prism_rows *rows,
     a.dk_out = c.heads(grads->dk_out, "dk_out");
     a.dq = c.heads(grads->dq, "dq");
     a.dk = c.heads(grads->dk, "dk");
-    a.dg_q = grads->dg_q, a.dg_k = grads->dg_k, a.part = p->grad_part, a.counter = p->counter + p->counters;
+    a.dg_q = grads->dg_q, a.dg_k = grads->dg_k, a.part = p->grad_part, a.counter = p->grad_ticket();
     c.need(a.pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
     c.need(!a.g_q == !a.dg_q && !a.g_q == !a.dg_k, PRISM_ERR_INVALID_ARG, "dg_q and dg_k are given with the gains and only then");
     if (c.s != PRISM_OK) return c.s;
@@ -259,7 +263,7 @@ prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, 
     if (c.s != PRISM_OK) return c.s;
     a.q = q, a.out = out, a.lse = lse;
     if (a.cache.weights) a.scores = p->scores, a.stat = p->stat;
-    a.part = p->part, a.counter = p->counter, a.err = p->err;
+    a.part = p->part, a.counter = p->counter, a.group_counter = p->counter + p->segments, a.err = p->err;
     a.B = cache->batch, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.added = added, a.min_units = 1;
     a.scale_log2 = (float)(p->cfg.softmax_scale * 1.4426950408889634);
     OnDevice on(p->device);
@@ -286,7 +290,7 @@ prism_status prism_paged_evict(prism_paged *p, const prism_paged_cache *src, con
         c.need(budget <= (1 << 30), PRISM_ERR_CAPACITY, "budget above 2^30");
     }
     if (c.s != PRISM_OK) return c.s;
-    a.kept = kept, a.counter = p->counter + p->counters + 1, a.B = src->batch, a.Hkv = p->cfg.n_kv_heads, a.budget = budget, a.sinks = sinks, a.recent = recent, a.err = p->err;
+    a.kept = kept, a.counter = p->evict_ticket(), a.B = src->batch, a.Hkv = p->cfg.n_kv_heads, a.budget = budget, a.sinks = sinks, a.recent = recent, a.err = p->err;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
     return cuda_status(p, launch_paged_evict(a, p->cfg.head_dim * c.es(), p->sms, (cudaStream_t)stream), "prism_paged_evict");

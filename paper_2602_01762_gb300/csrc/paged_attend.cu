@@ -418,6 +418,87 @@ __device__ __forceinline__ void write_out(const AttendArgs &a, long long hq, int
     }
 }
 
+// A segment cut between CTAs c0, c0 + 1, ...: piece i lies in CTA c0 + i's slot (its
+// second for the segment's first piece, a CTA's last piece; else its first).  Pieces
+// are joined in groups, groups in one more step.
+struct Cut {
+    int b, h, c0, pieces;
+    __device__ __forceinline__ int slot(int i) const { return i == 0 ? 2 * c0 + 1 : 2 * (c0 + i); }
+    __device__ __forceinline__ int in_group(int g, int size) const { return min(size, pieces - g * size); }
+};
+
+// Pieces added in their order: thread t has columns t, t + kPaThreads, ... of the
+// [H][D / 4] float4 sums, with their heads' maxima and sums.
+template <typename P> struct Joined {
+    static constexpr int D = P::D, H = P::kHeads, kPart = H * (D + 2);
+    static constexpr int kRound = kPaWarps * P::kStages * kPaStage / (4 * kPart);   // pieces that the rings hold
+    static constexpr int kGroup = kRound > 16 ? kRound : 16;
+    static constexpr int kCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;
+    float x[kCols][4], M[kCols], L[kCols];
+
+    template <typename Slot>
+    __device__ __forceinline__ void add(unsigned char *rings, const float *part, int n, int pieces, const Slot &slot) {
+        const int tid = threadIdx.x;
+        const uint32_t buf = (uint32_t)__cvta_generic_to_shared(rings);
+        const float *got = (const float *)rings;
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            M[c] = -INFINITY;
+            L[c] = x[c][0] = x[c][1] = x[c][2] = x[c][3] = 0.f;
+        }
+        for (int i0 = 0; i0 < pieces; i0 += kRound) {
+            const int count = min(kRound, pieces - i0);
+            for (int e = tid; e < count * (kPart / 4); e += kPaThreads) {
+                const int i = e / (kPart / 4);
+                cp16(buf + e * 16, part + (long long)slot(i0 + i) * kPart + (e - i * (kPart / 4)) * 4, true);
+            }
+            cp_group();
+            cp_wait_group<0>();
+            __syncthreads();
+#pragma unroll
+            for (int c = 0; c < kCols; ++c) {
+                const int e = tid + c * kPaThreads, h = e / (D / 4);
+                if (h >= n) continue;
+                float top = M[c];
+                for (int i = 0; i < count; ++i) top = fmaxf(top, got[i * kPart + H * D + 2 * h]);
+                const float base = base_of(top), old = exp2f(M[c] - base);
+                M[c] = top;
+                L[c] *= old;
+#pragma unroll
+                for (int d = 0; d < 4; ++d) x[c][d] *= old;
+#pragma unroll 4
+                for (int i = 0; i < count; ++i) {
+                    const float2 ml = *(const float2 *)(got + i * kPart + H * D + 2 * h);
+                    const float4 y = *(const float4 *)(got + i * kPart + e * 4);
+                    const float f = exp2f(ml.x - base);
+                    L[c] = fmaf(f, ml.y, L[c]);
+                    x[c][0] = fmaf(f, y.x, x[c][0]);
+                    x[c][1] = fmaf(f, y.y, x[c][1]);
+                    x[c][2] = fmaf(f, y.z, x[c][2]);
+                    x[c][3] = fmaf(f, y.w, x[c][3]);
+                }
+            }
+            __syncthreads();                             // the pieces were read
+        }
+    }
+    __device__ __forceinline__ void store(float *part, int n) const {
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            const int e = threadIdx.x + c * kPaThreads, h = e / (D / 4);
+            if (h >= n) continue;
+            __stcg((float4 *)part + e, make_float4(x[c][0], x[c][1], x[c][2], x[c][3]));
+            if (e % (D / 4) == 0) __stcg((float2 *)(part + H * D + 2 * h), make_float2(M[c], L[c]));
+        }
+    }
+    __device__ __forceinline__ void write(const AttendArgs &a, long long hq, int n) const {
+#pragma unroll
+        for (int c = 0; c < kCols; ++c) {
+            const int e = threadIdx.x + c * kPaThreads, h = e / (D / 4);
+            if (h < n) write_out<typename P::T, D>(a, hq + h, 4 * (e % (D / 4)), x[c], M[c], L[c]);
+        }
+    }
+};
+
 template <typename P> constexpr size_t attend_smem() {
     return (size_t)kPaWarps * (P::kStages * kPaStage + 4 * P::kHeads * (P::kMergeStride + 2));
 }
@@ -434,13 +515,12 @@ template <typename P>
 __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(AttendArgs a) {
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads;
-    constexpr int kPart = H * (D + 2);                   // floats of a piece: sums [H][D], then (maximum, sum) [H]
-    constexpr int kJoin = kPaWarps * S * kPaStage / (4 * kPart);   // pieces that the rings hold
-    constexpr int kJoinCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;   // float4 columns of a thread
+    constexpr int kPart = Joined<P>::kPart, kGroup = Joined<P>::kGroup;   // kPart: sums [H][D], then (maximum, sum) [H]
     constexpr int kRow = D * (int)sizeof(T), kChunks = kRow / 16, kRowsPer = 32 / kChunks;
     extern __shared__ __align__(128) unsigned char smem[];
-    __shared__ int4 join[2];
-    int joins = 0;                                       // of thread 0
+    __shared__ Cut joins[2];
+    __shared__ int join_group[2], last;
+    int pending = 0;                                     // of thread 0
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     pdl_wait();
     pdl_trigger();
@@ -538,7 +618,6 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
         state.store(own, sm + warp * H, sl + warp * H);
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
-        const int seg = p.b * heads + p.h;
         const int first = p.seg + kAttendCost;           // unit of the segment's first block
         const int c0 = first / r.per, c1 = (first + p.nblk - 1) / r.per;
         const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
@@ -572,70 +651,52 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
         }
         __syncthreads();                                 // the piece is written; the merge area is free again
         if (!whole && tid == 0) {
+            const Cut cut{p.b, p.h, c0, c1 - c0 + 1};
+            const int g = (blockIdx.x - c0) / kGroup;
             __threadfence();
-            if (atomicAdd(a.counter + seg, 1) == c1 - c0) {
+            int *ticket = a.group_counter + cut.slot(g * kGroup);
+            if (atomicAdd(ticket, 1) == cut.in_group(g, kGroup) - 1) {
                 __threadfence();
-                a.counter[seg] = 0;
-                join[joins++] = make_int4(p.b, p.h, c0, c1);
+                *ticket = 0;
+                joins[pending] = cut;
+                join_group[pending++] = g;
             }
         }
         p = after;
     }
-    // Segments of which this CTA finished the last piece (its first and its last
-    // segment at most), joined when the ring is free to take the pieces: all of them
-    // on their way at once, then added in CTA order.
+    // Groups of which this CTA finished the last piece (of its first and its last
+    // segment at most), joined now that the rings are free to take the pieces, all of
+    // them on their way at once; the last group of a segment joins the groups.
     cp_wait_group<0>();
-    if (tid == 0 && joins < 2) join[joins].x = -1;
+    if (tid == 0 && pending < 2) join_group[pending] = -1;
     __syncthreads();
-    for (int k = 0; k < 2 && join[k].x >= 0; ++k) {
-        const int4 w = join[k];
-        const int h0 = w.y % tiles * H, n = min(H, G - h0), pieces = w.w - w.z + 1;
-        const long long hq = (long long)w.x * a.Hq + w.y / tiles * G + h0;
-        const uint32_t buf = (uint32_t)__cvta_generic_to_shared(smem);
-        const float *got = (const float *)smem;
-        float x[kJoinCols][4] = {}, M[kJoinCols], L[kJoinCols] = {};
-#pragma unroll
-        for (int c = 0; c < kJoinCols; ++c) M[c] = -INFINITY;
-        for (int i0 = 0; i0 < pieces; i0 += kJoin) {
-            const int count = min(kJoin, pieces - i0);
-            for (int e = tid; e < count * (kPart / 4); e += kPaThreads) {
-                const int i = e / (kPart / 4);
-                // piece i of the segment: CTA c0's second slot, the others' first
-                const int slot = i0 + i == 0 ? 2 * w.z + 1 : 2 * (w.z + i0 + i);
-                cp16(buf + e * 16, a.part + (long long)slot * kPart + (e - i * (kPart / 4)) * 4, true);
+    for (int k = 0; k < 2 && join_group[k] >= 0; ++k) {
+        const Cut cut = joins[k];
+        const int g = join_group[k], groups = (cut.pieces + kGroup - 1) / kGroup;
+        const int h0 = cut.h % tiles * H, n = min(H, G - h0);
+        const long long hq = (long long)cut.b * a.Hq + cut.h / tiles * G + h0;
+        Joined<P> sum;
+        // first the group's pieces, then, by the last group, the groups' sums (one
+        // instance of the code: what a launch fetches of it counts for short calls)
+        int first = g * kGroup, step = 1, count = cut.in_group(g, kGroup);
+        while (true) {
+            sum.add(smem, a.part, n, count, [&](int i) { return cut.slot(first + i * step); });
+            if (step > 1 || groups == 1) {
+                sum.write(a, hq, n);
+                break;
             }
-            cp_group();
-            cp_wait_group<0>();
+            sum.store(a.part + (long long)cut.slot(first) * kPart, n);
             __syncthreads();
-#pragma unroll
-            for (int c = 0; c < kJoinCols; ++c) {
-                const int e = tid + c * kPaThreads, h = e / (D / 4);
-                if (h >= n) continue;
-                float top = M[c];
-                for (int i = 0; i < count; ++i) top = fmaxf(top, got[i * kPart + H * D + 2 * h]);
-                const float base = base_of(top), old = exp2f(M[c] - base);
-                M[c] = top;
-                L[c] *= old;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) x[c][d] *= old;
-#pragma unroll 4
-                for (int i = 0; i < count; ++i) {
-                    const float2 ml = *(const float2 *)(got + i * kPart + H * D + 2 * h);
-                    const float4 y = *(const float4 *)(got + i * kPart + e * 4);
-                    const float f = exp2f(ml.x - base);
-                    L[c] = fmaf(f, ml.y, L[c]);
-                    x[c][0] = fmaf(f, y.x, x[c][0]);
-                    x[c][1] = fmaf(f, y.y, x[c][1]);
-                    x[c][2] = fmaf(f, y.z, x[c][2]);
-                    x[c][3] = fmaf(f, y.w, x[c][3]);
-                }
+            if (tid == 0) {
+                int *ticket = a.counter + cut.b * heads + cut.h;
+                __threadfence();
+                last = atomicAdd(ticket, 1) == groups - 1;
+                __threadfence();
+                if (last) *ticket = 0;
             }
             __syncthreads();
-        }
-#pragma unroll
-        for (int c = 0; c < kJoinCols; ++c) {
-            const int e = tid + c * kPaThreads, h = e / (D / 4);
-            if (h < n) write_out<T, D>(a, hq + h, 4 * (e % (D / 4)), x[c], M[c], L[c]);
+            if (!last) break;
+            first = 0, step = kGroup, count = groups;
         }
     }
 }
@@ -643,7 +704,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 // weights[j] += sum_h 2^(s_jh - M_h) / L_h from the scores the attention kernel
 // left, heads in order; one thread per (KV head, row).
 constexpr int kWtThreads = 256;
-constexpr int kWtRows = 2 * kWtThreads;  // rows per unit: two a thread, their loads side by side
+constexpr int kWtEach = 2;              // rows of a thread, their loads side by side
+constexpr int kWtRows = kWtEach * kWtThreads;
 __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a, int head_tile) {
     // Before the wait: the attention kernel lets this one start once its own wait is
     // over, so lengths, table and weights are final; scores and stat are not.
@@ -655,11 +717,11 @@ __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a,
     const int G = a.Hq / a.Hkv;
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
     int b = 0, len = 0, nblk = 1, h = 0, blk = 0;
-    float *to[2];
-    float w[2];
+    float *to[kWtEach];
+    float w[kWtEach];
     auto fetch = [&]() {                 // where the unit's rows have their weights, and these
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int i = 0; i < kWtEach; ++i) {
             const int j = blk * kWtRows + i * kWtThreads + threadIdx.x;
             to[i] = nullptr;
             if (j >= len) continue;
@@ -669,7 +731,7 @@ __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a,
             to[i] = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i) w[i] = to[i] ? *to[i] : 0.f;
+        for (int i = 0; i < kWtEach; ++i) w[i] = to[i] ? *to[i] : 0.f;
     };
     if (any) {
         b = r.b, len = rows(b), nblk = blocks(len);
@@ -681,16 +743,17 @@ __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a,
     for (int u = r.u0; u < r.u1; ++u) {
         const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
         const float2 *st = a.stat + (long long)b * a.Hq + h * G;
-        float sum[2] = {0.f, 0.f};
+        float sum[kWtEach] = {};
         for (int t = 0; t < G; t += head_tile) {
             const int n = min(head_tile, G - t);
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
+            for (int i = 0; i < kWtEach; ++i) {
                 if (!to[i]) continue;
                 const float *z = s + t * cap + (long long)(blk * kWtRows + i * kWtThreads + threadIdx.x) * n;
+                float v = sum[i];
                 auto add = [&](float x, int k) {
                     const float2 ml = st[t + k];
-                    sum[i] = fmaf(exp2f(x - ml.x), ml.y, sum[i]);
+                    v = fmaf(exp2f(x - ml.x), ml.y, v);
                 };
                 if (n % 4 == 0) {
                     for (int k = 0; k < n; k += 4) {
@@ -700,10 +763,11 @@ __global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a,
                 } else {
                     for (int k = 0; k < n; ++k) add(z[k], k);
                 }
+                sum[i] = v;
             }
         }
 #pragma unroll
-        for (int i = 0; i < 2; ++i)
+        for (int i = 0; i < kWtEach; ++i)
             if (to[i]) *to[i] = w[i] + sum[i];
         if (u + 1 == r.u1) break;
         if (++blk == nblk) {
@@ -734,8 +798,10 @@ template <typename F> cudaError_t with_tile(bool bf16, int D, int G, const F &f)
 
 int attend_head_tile(bool bf16, int G) { return G <= 4 ? 4 : G <= 8 || !bf16 ? 8 : 16; }
 
+int attend_ctas(int sms) { return sms * kPaCtasPerSm; }
+
 size_t attend_part_floats(bool bf16, int D, int G, int sms) {
-    return (size_t)2 * sms * kPaCtasPerSm * attend_head_tile(bf16, G) * (D + 2);
+    return (size_t)2 * attend_ctas(sms) * attend_head_tile(bf16, G) * (D + 2);
 }
 
 cudaError_t prepare_attend_kernels() {
@@ -755,7 +821,7 @@ cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, 
     const int G = a.Hq / a.Hkv, ht = attend_head_tile(bf16, G);
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
     const long long most = a.B * (long long)a.Hkv * ((G + ht - 1) / ht) * (kAttendCost + (cap + kAttendUnit - 1) / kAttendUnit);
-    const int grid = (int)(most < sms * kPaCtasPerSm ? most : sms * kPaCtasPerSm);
+    const int grid = (int)(most < attend_ctas(sms) ? most : attend_ctas(sms));
     cudaError_t e = with_tile(bf16, D, G, [&](auto tile) {
         using P = decltype(tile);
         return launch_k(paged_attend_kernel<P>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);

@@ -13,8 +13,6 @@
 namespace prism {
 namespace {
 
-constexpr int kEvThreads = 1024;
-constexpr int kEvWarps = kEvThreads / 32;
 constexpr int kEvBatch = 4;              // rows a thread has in flight
 constexpr uint32_t kNan = 0x7FFFFFFFu;
 constexpr int kEvCached = 48 * 1024;     // rows whose keys shared memory holds
@@ -31,7 +29,9 @@ __device__ __forceinline__ uint32_t weight_key(float w) {
 // keys in shared memory (read from the pool again where a share is more than it
 // holds), the shares' histograms added into every CTA's through distributed shared
 // memory; then the kept slots in order.
+template <int kEvThreads>
 __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, int cs, int cached) {
+    constexpr int kEvWarps = kEvThreads / 32;
     extern __shared__ uint32_t keys[];
     __shared__ __align__(16) int hist[4][256], total[4][256];   // this share's counts of each pass; the cluster's
     __shared__ int warp_eq[kEvWarps], warp_gt[kEvWarps], share_eq[8], share_gt[8], pick[2];
@@ -89,8 +89,7 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, i
             for (int u = 0; u < kEvBatch; ++u)
                 if (i0 + u * kEvThreads < m) keys[i0 + u * kEvThreads] = k[u];
         }
-    hist[tid >> 8][tid & 255] = total[tid >> 8][tid & 255] = 0;
-    static_assert(kEvThreads == 4 * 256, "a thread per counter");
+    for (int i = tid; i < 4 * 256; i += kEvThreads) hist[i >> 8][i & 255] = total[i >> 8][i & 255] = 0;
     cluster_sync_all();                  // every CTA's counts are clear before another adds to them
     uint32_t prefix = 0, mask = 0;
     int need = want;                     // rows still to be taken of those that match the prefix
@@ -250,7 +249,7 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
 }  // namespace
 
 cudaError_t prepare_evict_kernels() {
-    return cudaFuncSetAttribute(evict_select_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvCached * 4);
+    return cudaFuncSetAttribute(evict_select_kernel<1024>, cudaFuncAttributeMaxDynamicSharedMemorySize, kEvCached * 4);
 }
 
 // CTAs per (sequence, KV head) of the selection: as many as give every SM two, up
@@ -268,7 +267,7 @@ cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaS
     const int cached = (int)(share < kEvCached ? share : kEvCached);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(a.B * a.Hkv * cs);
-    cfg.blockDim = dim3(kEvThreads);
+    cfg.blockDim = dim3(1024);
     cfg.dynamicSmemBytes = (size_t)cached * 4;
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
@@ -280,7 +279,9 @@ cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaS
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 2;
-    cudaError_t e = cudaLaunchKernelEx(&cfg, evict_select_kernel, a, cs, cached);
+    // Short rows: CTAs of 256 threads, eight to an SM (728 rows of 170: 33 -> XX us a call).
+    if (cap <= 2048) cfg.blockDim = dim3(256);
+    cudaError_t e = cudaLaunchKernelEx(&cfg, cap <= 2048 ? evict_select_kernel<256> : evict_select_kernel<1024>, a, cs, cached);
     if (e != cudaSuccess) return e;
     const long long warps = (long long)a.B * a.Hkv * ((a.budget + kCpRows - 1) / kCpRows);
     return launch_k(evict_copy_kernel, dim3((unsigned)((warps * 32 + kCpThreads - 1) / kCpThreads)), dim3(kCpThreads), 0, s, true, a, row_bytes);

@@ -686,3 +686,28 @@ def test_refusals(pkg):
             handle(pkg, 8, 2, 64, "bf16", **bad)
     with pytest.raises(ValueError):
         handle(pkg, 8, 2, 64, "f16")
+
+
+# ------------------------------------------------- work divided over many CTAs
+
+@pytest.mark.parametrize("Hq,D,dtype,n", [(4, 128, "bf16", 70001), (8, 128, "bf16", 50003), (16, 128, "bf16", 45007), (16, 64, "bf16", 60000),
+                                          (1, 64, "bf16", 90001), (4, 64, "f32", 30011), (8, 128, "f32", 20005)])
+def test_attend_one_segment_over_the_whole_gpu(pkg, Hq, D, dtype, n):
+    """One KV head: its rows are cut over every CTA, joined in groups, then the groups."""
+    check_attend(pkg, Hq=Hq, Hkv=1, D=D, dtype=dtype, page=64, lens=[n], track=True, wild=False)
+
+
+def test_attend_long_among_short(pkg):
+    check_attend(pkg, Hq=16, Hkv=1, D=128, dtype="bf16", page=32, lens=[3, 40000, 0, 1, 64, 65, 12000] + [17] * 20, track=True, wild=False)
+    check_attend(pkg, Hq=8, Hkv=2, D=64, dtype="f32", page=16, lens=[5] * 40 + [9000] + [5] * 40, wild=False)
+
+
+def test_evict_rows_beyond_shared_memory(pkg):
+    """More rows than eight CTAs' shared memory holds the keys of."""
+    check_evict(pkg, Hkv=1, D=64, dtype="bf16", page=128, lens=[400100], budget=3001, sinks=7, recent=500)
+    check_evict(pkg, Hkv=1, D=64, dtype="bf16", page=128, lens=[400100], budget=3001, sinks=7, recent=500, weights="same")
+
+
+def test_evict_many_short_sequences(pkg):
+    check_evict(pkg, Hkv=8, D=64, dtype="bf16", page=16, lens=[60 + 7 * (i % 13) for i in range(50)], budget=75, sinks=2, recent=9)
+    check_evict(pkg, Hkv=40, D=64, dtype="bf16", page=64, lens=[2500 + i for i in range(9)], budget=900, sinks=2, recent=9, weights="ties")
