@@ -105,6 +105,11 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
     const int n = ok ? 16 : 0;
     asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
+// The same for data read once: its lines leave L2 first.
+__device__ __forceinline__ void cp16_once(uint32_t dst, const void *src, bool ok, uint64_t policy) {
+    const int n = ok ? 16 : 0;
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(n), "l"(policy) : "memory");
+}
 __device__ __forceinline__ void cp_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 __device__ __forceinline__ uint4 lds16(uint32_t addr) {

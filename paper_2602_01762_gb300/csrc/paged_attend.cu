@@ -119,13 +119,18 @@ template <int D_, int MODE> struct Bf16Tile {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) s[t][i] = (s[t][i] + s2[t][i]) * scale;
                 if (scores) {
+                    const int h = 8 * t + c;
+                    float *to = scores + (long long)(base + g) * heads + h;
+                    if (h + 1 < heads && h < kHeads && !(heads & 1)) {
+                        if (in0) *(float2 *)to = make_float2(s[t][0], s[t][1]);
+                        if (in1) *(float2 *)(to + 8 * heads) = make_float2(s[t][2], s[t][3]);
+                    } else {
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) {
-                        const int h = 8 * t + c + i;
-                        if (h < heads && h < kHeads) {
-                            if (in0) scores[(long long)(base + g) * heads + h] = s[t][i];
-                            if (in1) scores[(long long)(base + g + 8) * heads + h] = s[t][2 + i];
-                        }
+                        for (int i = 0; i < 2; ++i)
+                            if (h + i < heads && h < kHeads) {
+                                if (in0) to[i] = s[t][i];
+                                if (in1) to[8 * heads + i] = s[t][2 + i];
+                            }
                     }
                 }
 #pragma unroll
@@ -566,6 +571,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     };
     Place next0 = look_up(), next1 = look_up();
     int stage_in = 0;
+    // K and V leave L2 first, so that scores, weights and pieces stay for the next reader
+    const uint64_t once = l2_evict_first_policy();
     auto issue = [&]() {
         if (next0.live) {
             const bool known = (unsigned)next0.page < (unsigned)a.cache.n_pages;
@@ -579,8 +586,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                 const int row = i * kRowsPer + lane / kChunks;
                 const long long at = __shfl_sync(0xFFFFFFFFu, off, row) + 16 * c;
                 const bool in = __shfl_sync(0xFFFFFFFFu, ok, row);
-                cp16(ks + P::piece(row, c), a.cache.k + at, in);
-                cp16(vs + P::piece(row, c), a.cache.v + at, in);
+                cp16_once(ks + P::piece(row, c), a.cache.k + at, in, once);
+                cp16_once(vs + P::piece(row, c), a.cache.v + at, in, once);
             }
         }
         cp_group();
@@ -702,84 +709,64 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 }
 
 // weights[j] += sum_h 2^(s_jh - M_h) / L_h from the scores the attention kernel
-// left, heads in order; one thread per (KV head, row).
+// left, heads in order; one row of a KV head per thread.  V: float4 of scores per
+// row (0: any group).  One row a thread and eight CTAs an SM beat two or four rows
+// and fewer CTAs (16 sequences of up to 8192 rows, both kernels: 52.1, 52.3 and 53.3
+// us): what bounds it is the chain of a row's loads, not their bytes.
 constexpr int kWtThreads = 256;
-constexpr int kWtEach = 2;              // rows of a thread, their loads side by side
-constexpr int kWtRows = kWtEach * kWtThreads;
-__global__ void __launch_bounds__(kWtThreads) paged_weights_kernel(AttendArgs a, int head_tile) {
+constexpr int kWtCtasPerSm = 8;
+template <int V>
+__global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel(AttendArgs a, int head_tile) {
     // Before the wait: the attention kernel lets this one start once its own wait is
     // over, so lengths, table and weights are final; scores and stat are not.
     pdl_trigger();
     auto rows = [&](int b) { return paged_len(a.cache, b, a.added, nullptr); };
-    auto blocks = [](int n) { return max(1, (n + kWtRows - 1) / kWtRows); };
+    auto blocks = [](int n) { return max(1, (n + kWtThreads - 1) / kWtThreads); };
     UnitRange r;
-    const bool any = unit_range<kWtThreads>(r, a.B, a.Hkv, 1, rows, blocks);
+    if (!unit_range<kWtThreads>(r, a.B, a.Hkv, 1, rows, blocks)) {
+        pdl_wait();
+        return;
+    }
     const int G = a.Hq / a.Hkv;
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
-    int b = 0, len = 0, nblk = 1, h = 0, blk = 0;
-    float *to[kWtEach];
-    float w[kWtEach];
-    auto fetch = [&]() {                 // where the unit's rows have their weights, and these
-#pragma unroll
-        for (int i = 0; i < kWtEach; ++i) {
-            const int j = blk * kWtRows + i * kWtThreads + threadIdx.x;
-            to[i] = nullptr;
-            if (j >= len) continue;
-            const int slot = j / a.cache.page_size;
-            const int page = a.cache.table[(long long)b * a.cache.table_pages + slot];
-            if ((unsigned)page >= (unsigned)a.cache.n_pages) continue;   // reported by the attention
-            to[i] = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + (j - slot * a.cache.page_size);
-        }
-#pragma unroll
-        for (int i = 0; i < kWtEach; ++i) w[i] = to[i] ? *to[i] : 0.f;
-    };
-    if (any) {
-        b = r.b, len = rows(b), nblk = blocks(len);
-        h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
-        fetch();
-    }
-    pdl_wait();                          // the scores
-    if (!any) return;
+    int b = r.b, len = rows(b), nblk = blocks(len);
+    int h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
     for (int u = r.u0; u < r.u1; ++u) {
-        const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
-        const float2 *st = a.stat + (long long)b * a.Hq + h * G;
-        float sum[kWtEach] = {};
-        for (int t = 0; t < G; t += head_tile) {
-            const int n = min(head_tile, G - t);
+        const int j = blk * kWtThreads + threadIdx.x;
+        const int page = j < len ? a.cache.table[(long long)b * a.cache.table_pages + j / a.cache.page_size] : -1;
+        if (u == r.u0) pdl_wait();
+        if ((unsigned)page < (unsigned)a.cache.n_pages) {   // else past the rows, or reported by the attention
+            const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
+            const float2 *st = a.stat + (long long)b * a.Hq + h * G;
+            float *to = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + j % a.cache.page_size;
+            float w = 0.f;
+            auto add = [&](float z, const float2 &ml) { w = fmaf(exp2f(z - ml.x), ml.y, w); };
+            if (V > 0) {
+                float4 z[V > 0 ? V : 1];
 #pragma unroll
-            for (int i = 0; i < kWtEach; ++i) {
-                if (!to[i]) continue;
-                const float *z = s + t * cap + (long long)(blk * kWtRows + i * kWtThreads + threadIdx.x) * n;
-                float v = sum[i];
-                auto add = [&](float x, int k) {
-                    const float2 ml = st[t + k];
-                    v = fmaf(exp2f(x - ml.x), ml.y, v);
-                };
-                if (n % 4 == 0) {
-                    for (int k = 0; k < n; k += 4) {
-                        const float4 x = *(const float4 *)(z + k);
-                        add(x.x, k), add(x.y, k + 1), add(x.z, k + 2), add(x.w, k + 3);
-                    }
-                } else {
-                    for (int k = 0; k < n; ++k) add(z[k], k);
+                for (int k = 0; k < V; ++k) z[k] = ((const float4 *)s)[(long long)j * V + k];
+                const float was = *to;
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    add(z[k].x, st[4 * k]), add(z[k].y, st[4 * k + 1]), add(z[k].z, st[4 * k + 2]), add(z[k].w, st[4 * k + 3]);
+                *to = was + w;
+            } else {
+                for (int t = 0; t < G; t += head_tile) {
+                    const int n = min(head_tile, G - t);
+                    const float *z = s + t * cap + (long long)j * n;
+                    for (int k = 0; k < n; ++k) add(z[k], st[t + k]);
                 }
-                sum[i] = v;
+                *to += w;
             }
         }
-#pragma unroll
-        for (int i = 0; i < kWtEach; ++i)
-            if (to[i]) *to[i] = w[i] + sum[i];
-        if (u + 1 == r.u1) break;
-        if (++blk == nblk) {
+        if (++blk == nblk && u + 1 < r.u1) {
             blk = 0;
             if (++h == a.Hkv) {
                 h = 0;
-                ++b;
-                len = rows(b);
+                len = rows(++b);
                 nblk = blocks(len);
             }
         }
-        fetch();
     }
 }
 
@@ -827,9 +814,14 @@ cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, 
         return launch_k(paged_attend_kernel<P>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
     });
     if (e != cudaSuccess || !a.scores) return e;
-    const long long chunks = a.B * (long long)a.Hkv * ((cap + kWtRows - 1) / kWtRows);
-    const int wt = (int)(chunks < sms * 6 ? chunks : sms * 6);
-    return launch_k(paged_weights_kernel, dim3(wt), dim3(kWtThreads), 0, s, true, a, ht);
+    const long long chunks = a.B * (long long)a.Hkv * ((cap + kWtThreads - 1) / kWtThreads);
+    const dim3 wt((unsigned)(chunks < sms * kWtCtasPerSm ? chunks : sms * kWtCtasPerSm));
+    auto go = [&](auto k) { return launch_k(k, wt, dim3(kWtThreads), 0, s, true, a, ht); };
+    // 4, 8 or 16 heads of one tile: a row's scores are one, two or four float4
+    if (G <= ht && G == 4) return go(paged_weights_kernel<1>);
+    if (G <= ht && G == 8) return go(paged_weights_kernel<2>);
+    if (G <= ht && G == 16) return go(paged_weights_kernel<4>);
+    return go(paged_weights_kernel<0>);
 }
 
 }  // namespace prism
