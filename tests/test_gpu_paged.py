@@ -711,3 +711,22 @@ def test_evict_rows_beyond_shared_memory(pkg):
 def test_evict_many_short_sequences(pkg):
     check_evict(pkg, Hkv=8, D=64, dtype="bf16", page=16, lens=[60 + 7 * (i % 13) for i in range(50)], budget=75, sinks=2, recent=9)
     check_evict(pkg, Hkv=40, D=64, dtype="bf16", page=64, lens=[2500 + i for i in range(9)], budget=900, sinks=2, recent=9, weights="ties")
+
+
+def test_example_bounds_the_cache(pkg):
+    """The decode example: caches within budget + slack (evictions before tokens 31, 51 and 71), every kept row a row of the past, finite results."""
+    import importlib.util
+    import os
+    path = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "paged_decode.py")
+    spec = importlib.util.spec_from_file_location("paged_decode", path)
+    example = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(example)
+    layer, evictions = example.main(["--batch", "3", "--prompt", "300", "--tokens", "90", "--budget", "310", "--slack", "20", "--hidden", "256"])
+    assert evictions == 3 and int(layer.kv_len.max()) <= 330 and int(layer.pos.max()) == 390
+    assert torch.isfinite(layer.y.float()).all()
+    h, B = layer.caches[layer.at], layer.B
+    for b in range(B):                       # weights of the kept rows: each row got at most one unit per query head and step
+        n = int(layer.kv_len[b])
+        w = ref.gather(layer.weights, h.block_table[b].cpu(), n)
+        assert (w >= 0).all() and float(w.max()) <= 4 * 90 + 1e-3
+    layer.att.close()
