@@ -148,7 +148,11 @@ __device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
     return r;
 }
-__device__ __forceinline__ F2 f2_neg(F2 a) { return a ^ 0x8000000080000000ull; }
+__device__ __forceinline__ F2 f2_sub(F2 a, F2 b) {
+    F2 r;
+    asm("sub.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
 __device__ __forceinline__ float f2_sum(F2 a) {
     const float2 v = f2_values(a);
     return v.x + v.y;
@@ -158,6 +162,10 @@ __device__ __forceinline__ F2 lds8(uint32_t addr) {
     F2 r;
     asm volatile("ld.shared.b64 %0, [%1];" : "=l"(r) : "r"(addr));
     return r;
+}
+
+__device__ __forceinline__ void lds16(uint32_t addr, F2 &a, F2 &b) {
+    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(a), "=l"(b) : "r"(addr) : "memory");
 }
 
 // E values of a 16-byte vector as floats and back (E = 8 bf16 or 4 fp32).

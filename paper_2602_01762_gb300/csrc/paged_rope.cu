@@ -16,7 +16,7 @@ namespace prism {
 namespace {
 
 constexpr int kNrThreads = 128;
-constexpr int kNrRing = 8;               // head groups a warp has in flight
+constexpr int kNrRing = 6;               // head groups a warp has in flight
 constexpr int kNrStage = 1024;           // bytes of one: the lanes' low pieces, then their high ones
 
 // 16 bytes as pairs of values, and back.
@@ -120,22 +120,35 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     // head groups: the queries', the keys', with APPEND the values'
     const int gq = (a.Hq + R::kHeads - 1) / R::kHeads, gk = (a.Hkv + R::kHeads - 1) / R::kHeads, end_k = gq + gk;
     const int groups = APPEND ? end_k + gk : end_k;
-    const char *qi = a.q.p + b * a.q.sb + i * a.q.st + sub * 16, *ki = a.k.p + b * a.k.sb + i * a.k.st + sub * 16;
-    const char *vi = APPEND ? a.v.p + b * a.v.sb + i * a.v.st + sub * 16 : nullptr;
-    // each lane copies what it reads itself, so that its own waits are enough
+    // each lane copies what it reads itself, so that its own waits are enough; `from`
+    // walks over the heads of a section (queries, keys, values)
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + (threadIdx.x >> 5) * (kNrRing * kNrStage) + lane * 16;
-    auto copy = [&](int g, int stage) {
-        const bool is_q = g < gq, is_k = g < end_k;
-        const int h = (is_q ? g : is_k ? g - gq : g - end_k) * R::kHeads + own;
-        if (g < groups && h < (is_q ? a.Hq : a.Hkv)) {
-            const char *p = (is_q ? qi : is_k ? ki : vi) + h * (is_q ? a.q.sh : is_k ? a.k.sh : a.v.sh);
-            cp16(ring + stage * kNrStage, p, true);
-            cp16(ring + stage * kNrStage + 512, p + D / 2 * sizeof(T), true);
+    int lg = share, l_end = 0, l_heads = 0, lh = 0;
+    const char *from = nullptr;
+    long long l_step = 0;
+    auto copy = [&](int stage) {
+        if (lg < groups) {
+            if (lg >= l_end) {           // the section of group lg
+                const bool is_q = lg < gq, is_k = lg < end_k;
+                const HeadsView &v = is_q ? a.q : is_k ? a.k : a.v;
+                lh = (is_q ? lg : is_k ? lg - gq : lg - end_k) * R::kHeads + own;
+                l_end = is_q ? gq : is_k ? end_k : groups;
+                l_heads = is_q ? a.Hq : a.Hkv;
+                l_step = a.split * R::kHeads * v.sh;
+                from = v.p + b * v.sb + i * v.st + lh * v.sh + sub * 16;
+            }
+            if (lh < l_heads) {
+                cp16(ring + stage * kNrStage, from, true);
+                cp16(ring + stage * kNrStage + 512, from + D / 2 * sizeof(T), true);
+            }
+            lg += a.split;
+            lh += a.split * R::kHeads;
+            from += l_step;
         }
         cp_group();
     };
 #pragma unroll
-    for (int u = 0; u < kNrRing - 1; ++u) copy(share + u * a.split, u);
+    for (int u = 0; u < kNrRing - 1; ++u) copy(u);
     Gain<T, D> gain;
     gain.load(a.g_q);
     R rope;
@@ -163,15 +176,15 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     const long long ko_sh = APPEND ? a.cache.head_stride : a.k_out.sh;
     int stage = 0;
     // the next group's stage, with a later group requested in its place
-    auto take = [&](int g) {
-        copy(g + (kNrRing - 1) * a.split, stage == 0 ? kNrRing - 1 : stage - 1);
+    auto take = [&]() {
+        copy(stage == 0 ? kNrRing - 1 : stage - 1);
         cp_wait_group<kNrRing - 1>();
         const uint32_t at = ring + stage * kNrStage;
         stage = stage + 1 == kNrRing ? 0 : stage + 1;
         return at;
     };
-    auto turn = [&](int g, int h, int heads, char *to) {
-        const uint32_t at = take(g);
+    auto turn = [&](int h, int heads, char *to) {
+        const uint32_t at = take();
         uint4 l = make_uint4(0u, 0u, 0u, 0u), r = l;
         if (h < heads) {
             l = lds16(at);
@@ -198,7 +211,7 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
         F2 p[N], q[N];
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            p[e] = f2_fma(x[e], rope.cs[e], f2_neg(f2_mul(y[e], rope.sn[e])));
+            p[e] = f2_sub(f2_mul(x[e], rope.cs[e]), f2_mul(y[e], rope.sn[e]));
             q[e] = f2_fma(y[e], rope.cs[e], f2_mul(x[e], rope.sn[e]));
         }
         *(uint4 *)to = Pairs<T>::pack(p);
@@ -207,17 +220,17 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
     int g = share;
     for (; g < gq; g += a.split) {
         const int h = g * R::kHeads + own;
-        turn(g, h, a.Hq, qo + h * a.q_out.sh);
+        turn(h, a.Hq, qo + h * a.q_out.sh);
     }
     gain.load(a.g_k);
     for (; g < end_k; g += a.split) {
         const int h = (g - gq) * R::kHeads + own;
-        turn(g, h, a.Hkv, ko ? ko + h * ko_sh : nullptr);
+        turn(h, a.Hkv, ko ? ko + h * ko_sh : nullptr);
         if (APPEND && weight && sub == 0 && h < a.Hkv) weight[(long long)h * a.cache.page_size] = 0.f;
     }
     for (; g < groups; g += a.split) {   // values go as they are
         const int h = (g - end_k) * R::kHeads + own;
-        const uint32_t at = take(g);
+        const uint32_t at = take();
         if (!vo || h >= a.Hkv) continue;
         char *to = vo + h * ko_sh;
         *(uint4 *)to = lds16(at);
@@ -234,7 +247,7 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
 // depend on the order in which they ran.
 // Persistent CTAs, one per SM; each warp walks over its rows' head groups with a
 // ring of kNgRing groups requested ahead by cp.async, across rows.
-constexpr int kNgThreads = 512;
+constexpr int kNgThreads = 384;
 constexpr int kNgRing = 5;
 constexpr int kNgStage = 2048 + 512;     // x and dy, low and high pieces of each lane; the row's cosines and sines
 
@@ -261,37 +274,41 @@ __device__ __forceinline__ void grad_group(uint32_t stage, char *to, bool norm, 
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             p[e] = f2_fma(u[e], rope.cs[e], f2_mul(v[e], rope.sn[e]));
-            q[e] = f2_fma(v[e], rope.cs[e], f2_neg(f2_mul(u[e], rope.sn[e])));
+            q[e] = f2_sub(f2_mul(v[e], rope.cs[e]), f2_mul(u[e], rope.sn[e]));
         }
     }
     if (norm) {
         F2 x[N], y[N];
         Pairs<T>::unpack(lds16(stage + lane * 16), x);
         Pairs<T>::unpack(lds16(stage + 512 + lane * 16), y);
-        F2 s = f2_mul(x[0], x[0]);
+        // with v = g dz:  dx = r v - x r^3 mean(v x),  dg += dz x r; both sums go together
+        F2 s = 0ull, c = 0ull, v[N], w[N];
 #pragma unroll
-        for (int e = 1; e < N; ++e) s = f2_fma(x[e], x[e], s);
-#pragma unroll
-        for (int e = 0; e < N; ++e) s = f2_fma(y[e], y[e], s);
-        const float r = rsqrtf(lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + eps);
-        const F2 rr = f2(r, r);
-        F2 c = 0ull;
-#pragma unroll
-        for (int e = 0; e < N; ++e) {
-            x[e] = f2_mul(x[e], rr);
-            y[e] = f2_mul(y[e], rr);
-            dg.x[e] = f2_fma(p[e], x[e], dg.x[e]);
-            dg.y[e] = f2_fma(q[e], y[e], dg.y[e]);
-            p[e] = f2_mul(p[e], lds8(gain + lane % R::kLanes * (R::E * 4) + 8 * e));
-            q[e] = f2_mul(q[e], lds8(gain + (D / 2 + lane % R::kLanes * R::E) * 4 + 8 * e));
-            c = f2_fma(p[e], x[e], f2_fma(q[e], y[e], c));
+        for (int e = 0; e < N; e += 2) {
+            lds16(gain + (e / 2 * R::kLanes + lane % R::kLanes) * 16, v[e], v[e + 1]);
+            lds16(gain + ((N + e) / 2 * R::kLanes + lane % R::kLanes) * 16, w[e], w[e + 1]);
         }
-        const float m = lanes_sum<R::kLanes>(f2_sum(c)) * (-1.f / D);
-        const F2 mm = f2(m, m);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            p[e] = f2_mul(rr, f2_fma(x[e], mm, p[e]));
-            q[e] = f2_mul(rr, f2_fma(y[e], mm, q[e]));
+            v[e] = f2_mul(p[e], v[e]);
+            w[e] = f2_mul(q[e], w[e]);
+            s = f2_fma(x[e], x[e], f2_fma(y[e], y[e], s));
+            c = f2_fma(v[e], x[e], f2_fma(w[e], y[e], c));
+        }
+        float ss = f2_sum(s), cc = f2_sum(c);
+#pragma unroll
+        for (int o = R::kLanes / 2; o > 0; o >>= 1) {
+            ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
+            cc += __shfl_xor_sync(0xFFFFFFFFu, cc, o);
+        }
+        const float r = rsqrtf(ss * (1.f / D) + eps), k = -r * r * r * (cc * (1.f / D));
+        const F2 rr = f2(r, r), kk = f2(k, k);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            dg.x[e] = f2_fma(f2_mul(p[e], rr), x[e], dg.x[e]);
+            dg.y[e] = f2_fma(f2_mul(q[e], rr), y[e], dg.y[e]);
+            p[e] = f2_fma(x[e], kk, f2_mul(v[e], rr));
+            q[e] = f2_fma(y[e], kk, f2_mul(w[e], rr));
         }
     }
     if (!to) return;
@@ -326,12 +343,14 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
     pdl_trigger();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % R::kLanes, own = lane / R::kLanes;
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dyn) + warp * (kNgRing * kNgStage);
-    // both gains as fp32 behind the rings
+    // both gains as fp32 behind the rings, four values of each lane side by side
     float *gain = (float *)(dyn + kWarps * kNgRing * kNgStage);
     const uint32_t gains = (uint32_t)__cvta_generic_to_shared(gain);
     if (a.g_q)
-        for (int d = threadIdx.x; d < 2 * D; d += kNgThreads)
-            gain[d] = Elem<T>::load((const T *)(d < D ? a.g_q : a.g_k), d < D ? d : d - D);
+        for (int i = threadIdx.x; i < 2 * D; i += kNgThreads) {
+            const int d = i % D, half = d / (D / 2), l = d % (D / 2) / R::E, e = d % R::E;
+            gain[i - d + ((half * R::E + e) / 4 * R::kLanes + l) * 4 + e % 4] = Elem<T>::load((const T *)(i < D ? a.g_q : a.g_k), d);
+        }
     __syncthreads();
     GainGrad<T, D> dq, dk;
     dq.clear();
@@ -344,7 +363,9 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
     f.at(a, blockIdx.x * kWarps + warp, items);
     while (f.live && !f.valid) f.at(a, f.w + step, items);
     bool fresh = true;                   // its row's first group: the row's table line comes with it
-    const char *x = nullptr, *y = nullptr;   // its row in q or k, and in dq_out or dk_out
+    const char *x = nullptr, *y = nullptr;   // its heads in q or k, and in dq_out or dk_out
+    long long x_step = 0, y_step = 0;
+    int fh = 0;
     int stage_in = 0;
     auto request = [&]() {
         if (f.live) {
@@ -353,16 +374,22 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
                 cp16(to + 2048, a.rope + (long long)row_position(a.pos, f.b, f.i, a.rope_len, a.err) * D + lane * 4, true);
             const bool is_q = f.g < gq;
             if (fresh || (!is_q && f.g - a.split < gq)) {
-                x = row_at(is_q ? a.q : a.k, f);
-                y = row_at(is_q ? a.dq_out : a.dk_out, f);
+                const HeadsView &vx = is_q ? a.q : a.k, &vy = is_q ? a.dq_out : a.dk_out;
+                fh = (is_q ? f.g : f.g - gq) * R::kHeads + own;
+                x = row_at(vx, f) + fh * vx.sh;
+                y = row_at(vy, f) + fh * vy.sh;
+                x_step = a.split * R::kHeads * vx.sh;
+                y_step = a.split * R::kHeads * vy.sh;
             }
-            const int h = (is_q ? f.g : f.g - gq) * R::kHeads + own;
-            const bool ok = h < (is_q ? a.Hq : a.Hkv);
-            const char *xs = x + (ok ? h : 0) * (is_q ? a.q.sh : a.k.sh), *ys = y + (ok ? h : 0) * (is_q ? a.dq_out.sh : a.dk_out.sh);
+            const bool ok = fh < (is_q ? a.Hq : a.Hkv);
+            const char *xs = ok ? x : a.q.p, *ys = ok ? y : a.q.p;
             cp16(to, xs, ok);
             cp16(to + 512, xs + D / 2 * sizeof(T), ok);
             cp16(to + 1024, ys, ok);
             cp16(to + 1536, ys + D / 2 * sizeof(T), ok);
+            x += x_step;
+            y += y_step;
+            fh += a.split * R::kHeads;
             f.g += a.split;
             fresh = f.g >= groups;
             if (fresh) {
