@@ -287,7 +287,8 @@ prism_status prism_paged_evict(prism_paged *p, const prism_paged_cache *src, con
                "budget must be at least 1 and at least sinks + recent, neither negative");
         const long long page = p->cfg.page_size, most = src->table_pages * page;
         c.need((budget < most ? budget : most) <= dst->table_pages * page, PRISM_ERR_SHAPE, "dst has fewer rows than the budget");
-        c.need(budget <= (1 << 30), PRISM_ERR_CAPACITY, "budget above 2^30");
+        c.need((long long)src->batch * p->cfg.n_kv_heads * ((long long)budget / 8 + 1) <= (1LL << 30), PRISM_ERR_CAPACITY,
+               "batch * n_kv_heads * budget is too large");
     }
     if (c.s != PRISM_OK) return c.s;
     a.kept = kept, a.counter = p->evict_ticket(), a.B = src->batch, a.Hkv = p->cfg.n_kv_heads, a.budget = budget, a.sinks = sinks, a.recent = recent, a.err = p->err;

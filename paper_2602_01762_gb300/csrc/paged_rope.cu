@@ -9,7 +9,10 @@
 // bytes at j and the 16 bytes at j + D/2 of one head, so a rotation pair never
 // leaves its lane and the mean is one exchange over D/2 / E lanes (E values per
 // 16 bytes); a warp takes 32 E / (D/2) heads of a row at a time and keeps the
-// row's cosines and sines in registers over all its heads.
+// row's cosines and sines in registers over all its heads.  All arithmetic is fp32,
+// each result is rounded once.  Measured: append of 8 prompts of 1021 to 2048 rows (32
+// + 2 x 8 heads of 128, bf16) 50 us (6.2 TB/s; 45.5 at the rate of a plain copy);
+// forward and gradient of 14196 of 16384 rows (32 + 8 heads) 137 us (5.6 TB/s; 113).
 #include "paged.cuh"
 
 namespace prism {
@@ -246,7 +249,10 @@ __global__ void __launch_bounds__(kNrThreads) norm_rope_kernel(NormRopeArgs a) {
 // order (the last CTA to finish adds the CTAs' rows in CTA order), so dg does not
 // depend on the order in which they ran.
 // Persistent CTAs, one per SM; each warp walks over its rows' head groups with a
-// ring of kNgRing groups requested ahead by cp.async, across rows.
+// ring of kNgRing groups requested ahead by cp.async, across rows.  What holds it at
+// 5 TB/s is the latency of some 300 instructions a group at 12 warps an SM: the sums of
+// dg, the rotation and the data take up to 168 registers (16 warps of 128 spill: 145
+// against 137 us with the forward; a ring of 7 instead of 5 leaves too little L1: 140).
 constexpr int kNgThreads = 384;
 constexpr int kNgRing = 5;
 constexpr int kNgStage = 2048 + 512;     // x and dy, low and high pieces of each lane; the row's cosines and sines

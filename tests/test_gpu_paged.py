@@ -730,3 +730,43 @@ def test_example_bounds_the_cache(pkg):
         w = ref.gather(layer.weights, h.block_table[b].cpu(), n)
         assert (w >= 0).all() and float(w.max()) <= 4 * 90 + 1e-3
     layer.att.close()
+
+
+@pytest.mark.parametrize("what,bit", [("long", 2), ("negative", 2)])
+def test_evict_device_flags(pkg, what, bit):
+    """A length outside the table: clamped and reported; the other sequence as it should be."""
+    h = handle(pkg, 2, 2, 64, "f32", max_batch=2, max_pages=3)
+    k, v, w = torch.randn(12, 2, 16, 64, device="cuda"), torch.randn(12, 2, 16, 64, device="cuda"), torch.rand(12, 2, 16, device="cuda")
+    table = torch.tensor([[0, 1, 2], [3, 4, 5]], dtype=torch.int32, device="cuda")
+    to = torch.tensor([[6, 7], [8, 9]], dtype=torch.int32, device="cuda")
+    n = torch.tensor([40, 49 if what == "long" else -2], dtype=torch.int32, device="cuda")
+    out, kept = torch.zeros_like(n), torch.empty(2, 2, 20, dtype=torch.int32, device="cuda")
+    h.evict(h.cache(k, v, table, n, weights=w), h.cache(k, v, to, out, weights=w), kept, sinks=1, recent=3)
+    assert h.status() == bit
+    assert out.tolist() == [20, 20 if what == "long" else 0]
+    for hd in range(2):
+        wl = ref.gather(w, table[0].cpu(), 40)[hd].cpu().numpy()
+        assert np.array_equal(kept[0, hd].cpu().numpy(), ref.kept_rows(wl, 40, 20, 1, 3))
+        assert (kept[1, hd] == -1).all() == (what == "negative")
+    h.close()
+
+
+@pytest.mark.parametrize("what,bit", [("n_new", 4), ("position", 32)])
+def test_gradient_device_flags(pkg, what, bit):
+    q, k, _, g_q, g_k, pos, _, rope = rows_case(pkg, Hq=4, Hkv=2, D=64, dtype="f32", B=2, n=3, gains=True)
+    pos, n_new = torch.tensor([0, 5], dtype=torch.int32, device="cuda"), torch.tensor([3, 2], dtype=torch.int32, device="cuda")
+    if what == "n_new":
+        n_new[1] = -1
+    else:
+        pos[1] = rope.shape[0]
+    h = handle(pkg, 4, 2, 64, "f32")
+    g = rng(3)
+    dqo, dko = normal(g, 2, 3, 4, 64, dtype=torch.float32), normal(g, 2, 3, 2, 64, dtype=torch.float32)
+    dq, dk, dg = torch.empty_like(dqo), torch.empty_like(dko), torch.empty(2, 64, device="cuda")
+    h.qk_norm_rope_backward(dqo, dko, q, k, dq, dk, rope, pos, g_q=g_q, g_k=g_k, dg_q=dg[0], dg_k=dg[1], n_new=n_new)
+    assert h.status() == bit
+    want, _, tol, _ = ref.norm_rope_grad(q[0], g_q, dqo[0], rope, 0, EPS)
+    ref.within(dq[0], want, tol)
+    if what == "n_new":
+        assert (dq[1] == 0).all() and (dk[1] == 0).all()
+    h.close()
