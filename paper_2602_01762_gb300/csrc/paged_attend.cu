@@ -46,6 +46,10 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// What a warp subtracts from its scores is a maximum it has met, renewed (and its sums
+// rescaled) only when a score passes it by more than this: probabilities stay below
+// 2^8 times the largest, and most tiles need no exchange between lanes.
+constexpr float kSlack = 8.f;
 // The maximum to subtract: 0 where no score is above -inf (every exp2 is then 0).
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
@@ -119,7 +123,6 @@ template <int D_, int MODE> struct Bf16Tile {
                 for (int t = 0; t < NT; ++t) mma_bf16(k & 1 ? s2[t] : s[t], a, qf[k][t][0], qf[k][t][1]);
             }
             const bool in0 = base + g < len, in1 = base + g + 8 < len;
-            float mn[NT][2];
             bool grew = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -144,28 +147,30 @@ template <int D_, int MODE> struct Bf16Tile {
                 for (int i = 0; i < 2; ++i) {
                     if (!in0) s[t][i] = -INFINITY;
                     if (!in1) s[t][2 + i] = -INFINITY;
-                    float v = fmaxf(s[t][i], s[t][2 + i]);
-                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
-                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
-                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
-                    mn[t][i] = fmaxf(m[t][i], v);
-                    grew |= mn[t][i] != m[t][i];
+                    grew |= fmaxf(s[t][i], s[t][2 + i]) > m[t][i] + kSlack;
                 }
             }
             if (__any_sync(0xFFFFFFFFu, grew)) {
 #pragma unroll
                 for (int t = 0; t < NT; ++t) {
-                    const float a0 = exp2f(m[t][0] - base_of(mn[t][0])), a1 = exp2f(m[t][1] - base_of(mn[t][1]));
-                    m[t][0] = mn[t][0];
-                    m[t][1] = mn[t][1];
-                    l[t][0] *= a0;
-                    l[t][1] *= a1;
+                    float a[2];
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        float v = fmaxf(s[t][i], s[t][2 + i]);
+                        v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 4));
+                        v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 8));
+                        v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 16));
+                        v = fmaxf(m[t][i], v);
+                        a[i] = exp2f(m[t][i] - base_of(v));
+                        m[t][i] = v;
+                        l[t][i] *= a[i];
+                    }
 #pragma unroll
                     for (int d = 0; d < D / 16; ++d) {
-                        o[d][t][0] *= a0;
-                        o[d][t][1] *= a1;
-                        o[d][t][2] *= a0;
-                        o[d][t][3] *= a1;
+                        o[d][t][0] *= a[0];
+                        o[d][t][1] *= a[1];
+                        o[d][t][2] *= a[0];
+                        o[d][t][3] *= a[1];
                     }
                 }
             }
@@ -300,14 +305,13 @@ template <int D_, int NG> struct F32Tile {
                 const int h = 4 * n + (lane & 3);
                 if (scores && in && h < heads) scores[(long long)(base + (lane >> 2)) * heads + h] = s;
                 if (!in) s = -INFINITY;
-                float mx = s;
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                mx = fmaxf(m[n], mx);
-                const float b = base_of(mx), p = exp2f(s - b);
-                if (__any_sync(0xFFFFFFFFu, mx != m[n])) {
-                    const float alpha = exp2f(m[n] - b);
+                if (__any_sync(0xFFFFFFFFu, s > m[n] + kSlack)) {
+                    float mx = s;
+                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                    mx = fmaxf(m[n], mx);
+                    const float alpha = exp2f(m[n] - base_of(mx));
                     m[n] = mx;
                     l[n] *= alpha;
 #pragma unroll
@@ -317,6 +321,7 @@ template <int D_, int NG> struct F32Tile {
                         for (int i = 0; i < V; ++i) o[4 * n + j][i] = f2_mul(o[4 * n + j][i], f2(a, a));
                     }
                 }
+                const float p = exp2f(s - base_of(m[n]));
                 l[n] += p;
                 *(float2 *)(pad + 2 * lane) = make_float2(p, p);   // as the pairs that the products below take
                 __syncwarp();
