@@ -119,51 +119,53 @@ class PagedAttention:
         h = _vp()
         self._check(self.lib.prism_paged_create(ctypes.byref(cfg), device, ctypes.byref(h)))
         self.h = h
-        self._index = self.device.index
+        self._index, self._dims = self.device.index, (head_dim,)
         self._rows, self._grads = ctypes.create_string_buffer(_ROWS.size), ctypes.create_string_buffer(_GRADS.size)
         self._rows_at, self._grads_at = ctypes.addressof(self._rows), ctypes.addressof(self._grads)
         self._key = (self.tdtype, self.device, (n_kv_heads, page_size, head_dim))
 
     # ------------------------------------------------------------ checks
     def _check(self, status):
-        if status != 0:
+        if status:
             from . import PrismError
             raise PrismError(status, (self.lib.prism_paged_error(self.h) or b"").decode())
 
-    def _tensor(self, t, shape, dtype, name):
-        """Address of a dense tensor of this device, shape and type."""
+    def _refuse(self, t, what, name):
         if not isinstance(t, torch.Tensor):
             raise TypeError(f"{name}: expected a torch.Tensor")
-        if t.dtype is not dtype or t.shape != shape or t.get_device() != self._index or not t.is_contiguous():
-            raise ValueError(f"{name}: expected contiguous {dtype} {tuple(shape)} on {self.device}, got {t.dtype} "
-                             f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
-        return t.data_ptr()
+        raise ValueError(f"{name}: expected {what} on {self.device}, got {t.dtype} {tuple(t.shape)} on {t.device}, strides {t.stride()}")
+
+    def _tensor(self, t, shape, dtype, name):
+        """Address of a dense tensor of this device, shape and type."""
+        try:
+            if t.shape == shape and t.dtype is dtype and t.get_device() == self._index and t.is_contiguous():
+                return t.data_ptr()
+        except AttributeError:
+            pass
+        self._refuse(t, f"contiguous {dtype} {tuple(shape)}", name)
 
     def _heads(self, t, shape, name):
         """Address and strides of a [batch, rows, heads, D] tensor, D dense."""
-        if isinstance(t, torch.Tensor):
-            s = t.stride()
-            if t.shape == shape and s[3] == 1 and t.dtype is self.tdtype and t.get_device() == self._index:
-                return t.data_ptr(), s[0], s[1], s[2]
-        else:
-            raise TypeError(f"{name}: expected a torch.Tensor")
-        raise ValueError(f"{name}: expected {self.tdtype} {shape} on {self.device} with a dense head dimension, got {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device}, strides {t.stride()}")
+        try:
+            if t.shape == shape and t.dtype is self.tdtype and t.get_device() == self._index:
+                b, r, h, d = t.stride()
+                if d == 1:
+                    return t.data_ptr(), b, r, h
+        except AttributeError:
+            pass
+        self._refuse(t, f"{self.tdtype} {shape} with a dense head dimension", name)
 
     def _pack(self, shape_q, shape_k, q, k, v, q_out, k_out, rope, pos, g_q, g_k, n_new):
         """Checks a block of rows and writes its prism_rows."""
-        i32, B, D = torch.int32, shape_q[0], self.head_dim
+        heads, tensor, i32, B = self._heads, self._tensor, torch.int32, shape_q[0:1]
         n = rope.shape[0]
         _ROWS.pack_into(
-            self._rows, 0, *self._heads(q, shape_q, "q"), *self._heads(k, shape_k, "k"),
-            *(_NONE if v is None else self._heads(v, shape_k, "v")),
-            *(_NONE if q_out is None else self._heads(q_out, shape_q, "q_out")),
-            *(_NONE if k_out is None else self._heads(k_out, shape_k, "k_out")),
-            0 if g_q is None else self._tensor(g_q, (D,), self.tdtype, "g_q"),
-            0 if g_k is None else self._tensor(g_k, (D,), self.tdtype, "g_k"),
-            self._tensor(rope, (n, 2, D // 2), torch.float32, "rope"),
-            0 if pos is None else self._tensor(pos, (B,), i32, "pos"),
-            0 if n_new is None else self._tensor(n_new, (B,), i32, "n_new"), n, B, shape_q[1])
+            self._rows, 0, *heads(q, shape_q, "q"), *heads(k, shape_k, "k"), *(_NONE if v is None else heads(v, shape_k, "v")),
+            *(_NONE if q_out is None else heads(q_out, shape_q, "q_out")), *(_NONE if k_out is None else heads(k_out, shape_k, "k_out")),
+            0 if g_q is None else tensor(g_q, self._dims, self.tdtype, "g_q"),
+            0 if g_k is None else tensor(g_k, self._dims, self.tdtype, "g_k"),
+            tensor(rope, (n, 2, self.head_dim // 2), torch.float32, "rope"),
+            0 if pos is None else tensor(pos, B, i32, "pos"), 0 if n_new is None else tensor(n_new, B, i32, "n_new"), n, B[0], shape_q[1])
 
     def _stream(self, stream):
         if stream is None:
@@ -223,11 +225,10 @@ class PagedAttention:
         B, n = q.shape[:2]
         sq, sk = self._shapes(B, n)
         self._pack(sq, sk, q, k, None, None, None, rope, pos, g_q, g_k, n_new)
-        f32, D = torch.float32, self.head_dim
+        heads, tensor, f32 = self._heads, self._tensor, torch.float32
         _GRADS.pack_into(
-            self._grads, 0, *self._heads(dq_out, sq, "dq_out"), *self._heads(dk_out, sk, "dk_out"), *self._heads(dq, sq, "dq"),
-            *self._heads(dk, sk, "dk"), 0 if dg_q is None else self._tensor(dg_q, (D,), f32, "dg_q"),
-            0 if dg_k is None else self._tensor(dg_k, (D,), f32, "dg_k"))
+            self._grads, 0, *heads(dq_out, sq, "dq_out"), *heads(dk_out, sk, "dk_out"), *heads(dq, sq, "dq"), *heads(dk, sk, "dk"),
+            0 if dg_q is None else tensor(dg_q, self._dims, f32, "dg_q"), 0 if dg_k is None else tensor(dg_k, self._dims, f32, "dg_k"))
         self._check(self.lib.prism_qk_norm_rope_backward(self.h, self._rows_at, self._grads_at, self._stream(stream)))
 
     def append(self, cache, q, k, v, q_out, rope, g_q=None, g_k=None, pos=None, n_new=None, stream=None):
