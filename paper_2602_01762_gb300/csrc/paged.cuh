@@ -63,6 +63,7 @@ struct AttendArgs {
     int *counter;                        // [B * head tiles] tickets (left at zero)
     int *group_counter;                  // two per CTA (left at zero)
     int B, Hq, Hkv, added, min_units;
+    int cluster;                         // CTAs of a cluster per segment; 1: a persistent grid (set by the launch)
     float scale_log2;                    // softmax scale * log2(e)
     int *err;
 };
@@ -90,6 +91,26 @@ cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool appen
 int norm_rope_grad_ctas(int sms);
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s);
+
+// Launch in clusters of cs CTAs, with programmatic stream serialization.
+template <typename Kern, typename... Args>
+cudaError_t launch_cluster(Kern k, dim3 grid, dim3 block, size_t smem, int cs, cudaStream_t s, Args... args) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = grid;
+    cfg.blockDim = block;
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = cs;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = 2;
+    return cudaLaunchKernelEx(&cfg, k, args...);
+}
 
 #ifdef __CUDACC__
 // Rows of sequence b, held to [0, table rows] (outside: the cache-range bit).
@@ -197,11 +218,17 @@ template <> struct Vec16<float> {
     }
 };
 
-// Add to, or set, the same shared variable in another CTA of the cluster.
+// The same shared variable in another CTA of the cluster: load, add, set.
 __device__ __forceinline__ uint32_t dsmem_at(const void *local, uint32_t rank) {
     uint32_t remote;
     asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"((uint32_t)__cvta_generic_to_shared(local)), "r"(rank));
     return remote;
+}
+__device__ __forceinline__ void dsmem_ld(const float *local, uint32_t rank, float4 &v) {
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(dsmem_at(local, rank)) : "memory");
+}
+__device__ __forceinline__ void dsmem_ld(const float *local, uint32_t rank, float2 &v) {
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(dsmem_at(local, rank)) : "memory");
 }
 __device__ __forceinline__ void dsmem_add(int *local, uint32_t rank, int v) {
     asm volatile("red.relaxed.cluster.shared::cluster.add.s32 [%0], %1;" ::"r"(dsmem_at(local, rank)), "r"(v) : "memory");

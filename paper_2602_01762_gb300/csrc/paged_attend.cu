@@ -9,11 +9,11 @@
 // Bound by the bytes of K and V, read once: 4 D bytes per row and KV head in bf16
 // against 4 G D operations (G a byte: far below what the tensor cores' warp-level
 // products give at N = 8 or 16, too few columns for a 128-row tensor-memory tile).
-// Measured, bf16, D = 128: 64 sequences of 6001 to 16384 rows, G = 8, 433 us (6.8
-// TB/s, the rate of a plain copy); one of 131071 rows, G = 4, 85 us (6.3 TB/s); 8
+// Measured, bf16, D = 128: 64 sequences of 6001 to 16384 rows, G = 8, 425 us (6.9
+// TB/s, the rate of a plain copy); one of 131071 rows, G = 4, 84 us (6.4 TB/s); 8
 // multi-head ones of 2048 to 4096 rows 65 us (6.2); 16 of 1 to 8192 rows with weights
-// 52.6 us (5.2); one of 517 rows 7.1 us, a chain of length, table, row, join loads.
-// A call costs some 8 us beside its bytes: 4 until the first rows arrive, the rest the
+// 52 us (5.2); one of 517 rows 5.8 us, a chain of length, table and row loads and the
+// join.  A large call costs some 8 us beside its bytes: 4 until the first rows arrive, the rest the
 // spread of the SMs' speeds (6% by their place on the chip) and the last join.
 #include "paged.cuh"
 
@@ -71,6 +71,7 @@ template <int D_, int MODE> struct Bf16Tile {
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = MODE == kSixteen ? 2 : 3;
+    static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     uint32_t qf[D / 16][NT][2];
     float m[NT][2], l[NT][2], o[D / 16][NT][4];
 
@@ -245,6 +246,7 @@ template <int D_, int NG> struct F32Tile {
     static constexpr int kHeads = 4 * NG;
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = 3;
+    static constexpr int kClusterRows = 128 * 128 / D;
     F2 q[4 * NG][V], o[4 * NG][V];
     float m[NG], l[NG];                                  // of head 4 ng + lane % 4
 
@@ -404,6 +406,18 @@ struct Pieces {
         seg = r.first + h * (kAttendCost + nblk);
         return cut() || next(a);
     }
+    // A cluster's rank takes its run of the blocks of segment i, and no other piece.
+    __device__ __forceinline__ void only(const AttendArgs &a, int i, int rank, int n_heads) {
+        u = u1 = seg = base = lens = 0;
+        heads = n_heads;
+        b = i / heads;
+        h = i - b * heads;
+        len = paged_len(a.cache, b, a.added, a.err);
+        nblk = blocks_of(len);
+        const int share = (nblk + a.cluster - 1) / a.cluster;
+        blk0 = min(nblk, rank * share);
+        blk1 = min(nblk, blk0 + share);
+    }
     __device__ __forceinline__ bool next(const AttendArgs &a) {
         while (u < u1) {
             seg = u;
@@ -528,7 +542,11 @@ template <typename P> constexpr size_t attend_smem() {
 // turn, each with its own ring of stages filled by cp.async, its own online
 // softmax and no barrier until the segment's end; the ring runs on across
 // segments, so loads never stop.
-template <typename P>
+//
+// CLUSTER, for few short segments: a cluster of a.cluster CTAs takes one segment,
+// each an equal run of its blocks, and joins through distributed shared memory
+// instead of tickets and loads from L2.
+template <typename P, bool CLUSTER>
 __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(AttendArgs a) {
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads;
@@ -544,17 +562,21 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
     UnitRange r;
-    if (!unit_range<kPaThreads>(r, a.B, heads, a.min_units,
-                                [&](int b) { return paged_len(a.cache, b, a.added, a.err); }, units_of))
-        return;
+    Pieces p;                                            // the piece being computed
+    const int rank = CLUSTER ? (int)blockIdx.x % a.cluster : 0;
+    if (CLUSTER) {
+        p.only(a, blockIdx.x / a.cluster, rank, heads);
+    } else {
+        if (!unit_range<kPaThreads>(r, a.B, heads, a.min_units,
+                                    [&](int b) { return paged_len(a.cache, b, a.added, a.err); }, units_of))
+            return;
+        if (!p.begin(a, r, heads)) return;
+    }
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * kPaStage);
     float *merge = (float *)(smem + kPaWarps * S * kPaStage);                       // [warps][H][stride]
     float *sm = merge + kPaWarps * H * P::kMergeStride, *sl = sm + kPaWarps * H;    // [warps][H]
     float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
-
-    Pieces p;                                            // the piece being computed
-    if (!p.begin(a, r, heads)) return;
 
     // Loads run ahead of the computation: their own walk, and the pool place of each
     // lane's row of the next two tiles, so that no load waits for a block-table entry.
@@ -638,7 +660,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
         const int first = p.seg + kAttendCost;           // unit of the segment's first block
-        const int c0 = first / r.per, c1 = (first + p.nblk - 1) / r.per;
+        const int c0 = CLUSTER ? 0 : first / r.per, c1 = CLUSTER ? 0 : (first + p.nblk - 1) / r.per;
         const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
         float *part = a.part + (long long)slot * kPart;
         for (int e = tid; e < n * (D / 4); e += kPaThreads) {
@@ -658,8 +680,11 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                 x[2] = fmaf(k, y.z, x[2]);
                 x[3] = fmaf(k, y.w, x[3]);
             }
-            if (whole) {
+            if (!CLUSTER && whole) {
                 write_out<T, D>(a, hq + h, d, x, M, L);
+            } else if (CLUSTER) {                        // for the other ranks, where the rings were
+                *(float4 *)((float *)smem + h * D + d) = make_float4(x[0], x[1], x[2], x[3]);
+                if (d == 0) *(float2 *)((float *)smem + H * D + 2 * h) = make_float2(M, L);
             } else {
                 __stcg((float4 *)(part + h * D + d), make_float4(x[0], x[1], x[2], x[3]));
                 if (d == 0) {
@@ -667,6 +692,39 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                     __stcg(part + H * D + 2 * h + 1, L);
                 }
             }
+        }
+        if (CLUSTER) {
+            cluster_sync_all();
+            // each rank joins its columns, the ranks' sums in their order
+            for (int e = rank + a.cluster * tid; e < n * (D / 4); e += a.cluster * kPaThreads) {
+                const int h = e / (D / 4), d = 4 * (e % (D / 4));
+                float4 y[8];
+                float2 ml[8];
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < a.cluster) {
+                        dsmem_ld((float *)smem + h * D + d, k, y[k]);
+                        dsmem_ld((float *)smem + H * D + 2 * h, k, ml[k]);
+                    }
+                float M = -INFINITY, x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < a.cluster) M = fmaxf(M, ml[k].x);
+                const float base = base_of(M);
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+                    if (k < a.cluster) {
+                        const float f = exp2f(ml[k].x - base);
+                        L = fmaf(f, ml[k].y, L);
+                        x[0] = fmaf(f, y[k].x, x[0]);
+                        x[1] = fmaf(f, y[k].y, x[1]);
+                        x[2] = fmaf(f, y[k].z, x[2]);
+                        x[3] = fmaf(f, y[k].w, x[3]);
+                    }
+                write_out<T, D>(a, hq + h, d, x, M, L);
+            }
+            cluster_sync_all();                          // no CTA leaves while another reads its sums
+            return;
         }
         __syncthreads();                                 // the piece is written; the merge area is free again
         if (!whole && tid == 0) {
@@ -809,21 +867,40 @@ cudaError_t prepare_attend_kernels() {
             for (const int G : {4, 8, 16}) {
                 const cudaError_t e = with_tile(bf16, D, G, [](auto tile) {
                     using P = decltype(tile);
-                    return cudaFuncSetAttribute(paged_attend_kernel<P>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
+                    const cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<P, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
+                    return e != cudaSuccess ? e : cudaFuncSetAttribute(paged_attend_kernel<P, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
                 });
                 if (e != cudaSuccess) return e;
             }
     return cudaSuccess;
 }
 
-cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s) {
+// CTAs of a cluster per segment, or 1: the shares of a persistent grid.  Clusters
+// where all of them run at once and a table's rows are few for each CTA: at most
+// `rows` (bf16 at D = 128: 512, with 9 to 16 query heads 1024, fp32 128).  Measured, 8 KV
+// heads of 128 and 4 query heads each, cluster against shares: one sequence of 100
+// rows 4.7 and 6.6 us, of 1000 5.9 and 8.0, of 4000 9.8 and 9.8; four of 4000 15.0 and
+// 17.3; fp32 of 1000 rows 7.7 and 8.8, of 2000 11.1 and 9.8; 4 KV heads with 16 query
+// heads each, 4000 rows 11.7 and 19.0.
+static int attend_cluster(long long segments, long long cap, int rows, int sms) {
+    int cs = 1;
+    while (cs < 8 && cs * (long long)kAttendUnit < cap && 2 * cs * segments <= attend_ctas(sms)) cs *= 2;
+    return cap <= cs * (long long)rows ? cs : 1;
+}
+
+cudaError_t launch_paged_attend(const AttendArgs &args, bool bf16, int D, int sms, cudaStream_t s) {
+    AttendArgs a = args;
     const int G = a.Hq / a.Hkv, ht = attend_head_tile(bf16, G);
     const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
-    const long long most = a.B * (long long)a.Hkv * ((G + ht - 1) / ht) * (kAttendCost + (cap + kAttendUnit - 1) / kAttendUnit);
-    const int grid = (int)(most < attend_ctas(sms) ? most : attend_ctas(sms));
+    const long long segments = a.B * (long long)a.Hkv * ((G + ht - 1) / ht);
+    const long long most = segments * (kAttendCost + (cap + kAttendUnit - 1) / kAttendUnit);
     cudaError_t e = with_tile(bf16, D, G, [&](auto tile) {
         using P = decltype(tile);
-        return launch_k(paged_attend_kernel<P>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
+        a.cluster = attend_cluster(segments, cap, P::kClusterRows, sms);
+        if (a.cluster > 1)
+            return launch_cluster(paged_attend_kernel<P, true>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<P>(), a.cluster, s, a);
+        const int grid = (int)(most < attend_ctas(sms) ? most : attend_ctas(sms));
+        return launch_k(paged_attend_kernel<P, false>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
     });
     if (e != cudaSuccess || !a.scores) return e;
     const long long chunks = a.B * (long long)a.Hkv * ((cap + kWtThreads - 1) / kWtThreads);

@@ -271,24 +271,11 @@ cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaS
     const int cs = select_cluster(a.B * a.Hkv, cap, sms);
     const long long share = (cap + cs - 1) / cs + 32;
     const int cached = (int)(share < kEvCached ? share : kEvCached);
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(a.B * a.Hkv * cs);
-    cfg.blockDim = dim3(1024);
-    cfg.dynamicSmemBytes = (size_t)cached * 4;
-    cfg.stream = s;
-    cudaLaunchAttribute attr[2];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
-    attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = cs;
-    attr[1].val.clusterDim.y = 1;
-    attr[1].val.clusterDim.z = 1;
-    cfg.attrs = attr;
-    cfg.numAttrs = 2;
     // Short rows: CTAs of 256 threads, up to eight on an SM (728 rows of up to 170, a whole call:
     // 22 us, 33 with 1024 threads).
-    if (cap <= 2048) cfg.blockDim = dim3(256);
-    cudaError_t e = cudaLaunchKernelEx(&cfg, cap <= 2048 ? evict_select_kernel<256> : evict_select_kernel<1024>, a, cs, cached);
+    const bool small = cap <= 2048;
+    const cudaError_t e = launch_cluster(small ? evict_select_kernel<256> : evict_select_kernel<1024>, dim3(a.B * a.Hkv * cs),
+                                         dim3(small ? 256 : 1024), (size_t)cached * 4, cs, s, a, cs, cached);
     if (e != cudaSuccess) return e;
     const long long warps = (long long)a.B * a.Hkv * ((a.budget + kCpRows - 1) / kCpRows);
     return launch_k(evict_copy_kernel, dim3((unsigned)((warps * 32 + kCpThreads - 1) / kCpThreads)), dim3(kCpThreads), 0, s, true, a, row_bytes);
