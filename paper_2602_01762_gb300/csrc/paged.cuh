@@ -62,7 +62,7 @@ struct AttendArgs {
     float *part;                         // two pieces per CTA
     int *counter;                        // [B * head tiles] tickets (left at zero)
     int *group_counter;                  // two per CTA (left at zero)
-    int B, Hq, Hkv, added, min_units;
+    int B, Hq, Hkv, added;
     int cluster;                         // CTAs of a cluster per segment; 1: a persistent grid (set by the launch)
     float scale_log2;                    // softmax scale * log2(e)
     int *err;
@@ -239,15 +239,15 @@ __device__ __forceinline__ void dsmem_st(int *local, uint32_t rank, int v) {
 
 // Ragged work split into equal contiguous shares.  Sequence b of rows(b) rows has
 // blocks_of(rows) >= 1 blocks of keys, each for `heads` heads; units run over (b, head, block).
-// Every CTA takes `per` units from u0 on; begin() finds the sequence of its
-// first one.  All threads of the CTA call it.
+// Every CTA takes `per` units from u0 on, in sequence b; false: none are left for
+// it.  All threads of the CTA call it.
 struct UnitRange {
     int u0, u1, per;   // this CTA's units; units per CTA
     int b, first;      // sequence of u0 and that sequence's first unit
     int lens;          // lane i: rows of sequence i (B <= 32 alone)
 };
 template <int THREADS, typename Rows, typename Blocks>
-__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, int min_units, const Rows &rows, const Blocks &blocks_of) {
+__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, const Rows &rows, const Blocks &blocks_of) {
     const int tid = threadIdx.x, lane = tid & 31;
     const int cta = blockIdx.x, ctas = gridDim.x;
     auto blocks = [&](int b) { return blocks_of(rows(b)); };
@@ -261,7 +261,7 @@ __device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, int m
             if (lane >= o) s += t;
         }
         const int units = __shfl_sync(0xFFFFFFFFu, s, 31) * heads;
-        r.per = max(min_units, (units + ctas - 1) / ctas);
+        r.per = (units + ctas - 1) / ctas;
         if ((long long)cta * r.per >= units) return false;
         r.u0 = cta * r.per;
         r.u1 = min(r.u0 + r.per, units);
@@ -281,7 +281,7 @@ __device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, int m
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) total += warp_sum[w];
     const int units = total * heads;
-    r.per = max(min_units, (units + ctas - 1) / ctas);
+    r.per = (units + ctas - 1) / ctas;
     if ((long long)cta * r.per >= units) return false;
     r.u0 = cta * r.per;
     r.u1 = min(r.u0 + r.per, units);

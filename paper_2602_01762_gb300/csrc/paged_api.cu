@@ -264,7 +264,7 @@ prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, 
     a.q = q, a.out = out, a.lse = lse;
     if (a.cache.weights) a.scores = p->scores, a.stat = p->stat;
     a.part = p->part, a.counter = p->counter, a.group_counter = p->counter + p->segments, a.err = p->err;
-    a.B = cache->batch, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.added = added, a.min_units = 1;
+    a.B = cache->batch, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.added = added;
     a.scale_log2 = (float)(p->cfg.softmax_scale * 1.4426950408889634);
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");

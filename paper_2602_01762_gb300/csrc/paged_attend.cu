@@ -567,7 +567,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     if (CLUSTER) {
         p.only(a, blockIdx.x / a.cluster, rank, heads);
     } else {
-        if (!unit_range<kPaThreads>(r, a.B, heads, a.min_units,
+        if (!unit_range<kPaThreads>(r, a.B, heads,
                                     [&](int b) { return paged_len(a.cache, b, a.added, a.err); }, units_of))
             return;
         if (!p.begin(a, r, heads)) return;
@@ -793,7 +793,7 @@ __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel
     auto rows = [&](int b) { return paged_len(a.cache, b, a.added, nullptr); };
     auto blocks = [](int n) { return max(1, (n + kWtThreads - 1) / kWtThreads); };
     UnitRange r;
-    if (!unit_range<kWtThreads>(r, a.B, a.Hkv, 1, rows, blocks)) {
+    if (!unit_range<kWtThreads>(r, a.B, a.Hkv, rows, blocks)) {
         pdl_wait();
         return;
     }
