@@ -322,20 +322,34 @@ __device__ __forceinline__ void grad_group(uint32_t stage, char *to, bool norm, 
     *(uint4 *)(to + D / 2 * sizeof(T)) = Pairs<T>::pack(q);
 }
 
-// A warp's walk over (row, share) items and the head groups of each.
+// A warp's walk over its rows (every `rows`-th, from its own on) and, in each, its
+// share of the head groups; sequence and row are stepped without a division.
 struct RowWalk {
-    int w, b, i, g;
+    int b, i, g, share, step_b, step_i;
     bool live, valid;
-    __device__ __forceinline__ void at(const NormRopeGradArgs &a, int item, int items) {
-        w = item;
-        live = item < items;
-        valid = false;
-        if (!live) return;
-        const int row = item / a.split;
-        g = item - row * a.split;
-        b = row / a.max_new;
-        i = row - b * a.max_new;
-        valid = i < row_count(a.n_new, b, a.max_new, a.err);
+    __device__ __forceinline__ void begin(const NormRopeGradArgs &a, int warp, int warps) {
+        const int rows = warps / a.split;                // warps past rows * split have none
+        share = warp % a.split;
+        b = warp / a.split / a.max_new;
+        i = warp / a.split - b * a.max_new;
+        step_b = rows / a.max_new;
+        step_i = rows - step_b * a.max_new;
+        live = warp < rows * a.split;
+        look(a);
+    }
+    __device__ __forceinline__ void next(const NormRopeGradArgs &a) {
+        b += step_b;
+        i += step_i;
+        if (i >= a.max_new) {
+            i -= a.max_new;
+            ++b;
+        }
+        look(a);
+    }
+    __device__ __forceinline__ void look(const NormRopeGradArgs &a) {
+        g = share;
+        live = live && b < a.B;
+        valid = live && i < row_count(a.n_new, b, a.max_new, a.err);
     }
 };
 
@@ -361,13 +375,13 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
     GainGrad<T, D> dq, dk;
     dq.clear();
     dk.clear();
-    const int items = a.B * a.max_new * a.split, step = gridDim.x * kWarps;
     const int gq = (a.Hq + R::kHeads - 1) / R::kHeads, groups = gq + (a.Hkv + R::kHeads - 1) / R::kHeads;
     auto row_at = [&](const HeadsView &v, const RowWalk &r) { return v.p + r.b * v.sb + r.i * v.st + sub * 16; };
 
     RowWalk f;                           // loads ahead: the next group to request, in rows that count
-    f.at(a, blockIdx.x * kWarps + warp, items);
-    while (f.live && !f.valid) f.at(a, f.w + step, items);
+    f.begin(a, blockIdx.x * kWarps + warp, gridDim.x * kWarps);
+    RowWalk r = f;
+    while (f.live && !f.valid) f.next(a);
     bool fresh = true;                   // its row's first group: the row's table line comes with it
     const char *x = nullptr, *y = nullptr;   // its heads in q or k, and in dq_out or dk_out
     long long x_step = 0, y_step = 0;
@@ -399,8 +413,8 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
             f.g += a.split;
             fresh = f.g >= groups;
             if (fresh) {
-                f.at(a, f.w + step, items);
-                while (f.live && !f.valid) f.at(a, f.w + step, items);
+                do f.next(a);
+                while (f.live && !f.valid);
             }
         }
         cp_group();
@@ -410,8 +424,7 @@ __global__ void __launch_bounds__(kNgThreads) norm_rope_grad_kernel(NormRopeGrad
     for (int u = 0; u < kNgRing - 1; ++u) request();
 
     int stage = 0;
-    RowWalk r;
-    for (r.at(a, blockIdx.x * kWarps + warp, items); r.live; r.at(a, r.w + step, items)) {
+    for (; r.live; r.next(a)) {
         if (!r.valid) {                  // rows past n_new have zero gradients
             for (; r.g < groups; r.g += a.split) {
                 const bool is_q = r.g < gq;
@@ -548,8 +561,9 @@ cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &args, bool bf16, int D
     const int hpw = heads_per_warp(bf16, D);
     const long long rows = (long long)a.B * a.max_new;
     a.split = row_split(rows, (a.Hq + hpw - 1) / hpw + (a.Hkv + hpw - 1) / hpw, sms);
-    const long long ctas = (rows * a.split + kNgThreads / 32 - 1) / (kNgThreads / 32);
     const int most = norm_rope_grad_ctas(sms);
+    if (a.split > most * (kNgThreads / 32)) a.split = most * (kNgThreads / 32);   // a row's shares fit the grid
+    const long long ctas = (rows * a.split + kNgThreads / 32 - 1) / (kNgThreads / 32);
     const dim3 grid((unsigned)(ctas < most ? ctas : most));
     auto go = [&](auto k) { return launch_k(k, grid, dim3(kNgThreads), kNgSmem, s, true, a); };
     if (bf16) return D == 128 ? go(norm_rope_grad_kernel<uint16_t, 128>) : go(norm_rope_grad_kernel<uint16_t, 64>);
