@@ -526,7 +526,8 @@ typedef struct {
 /* A wtype [batch, max_new, heads, D] tensor, D dense, the other strides (in
  * elements) any multiples of 16 bytes, so that the queries, keys and values of
  * one fused projection, or [batch, heads, max_new, D] tensors, are taken as they
- * are.  An output may be its own input (same strides). */
+ * are.  An output may be its own input (same strides).  Inputs may repeat rows
+ * (stride 0; their gradients are given row by row), outputs may not. */
 typedef struct {
     void *data;
     int64_t batch_stride, row_stride, head_stride;

@@ -79,6 +79,13 @@ struct Check {
             s = fail(p, PRISM_ERR_INVALID_ARG, "%s: base and strides must be multiples of 16 bytes", name);
         return v;
     }
+    // An output: rows and heads of their own (a stride of 0 would have them written over each other).
+    HeadsView out(const prism_heads &h, const prism_rows &r, int n_heads, const char *name) {
+        const HeadsView v = heads(h, name);
+        if (s == PRISM_OK && ((v.sb == 0 && r.batch > 1) || (v.st == 0 && r.max_new > 1) || (v.sh == 0 && n_heads > 1)))
+            s = fail(p, PRISM_ERR_INVALID_ARG, "%s: an output stride is 0", name);
+        return v;
+    }
     PagedView cache(const prism_paged_cache *c, const char *name) {
         PagedView v{};
         if (!c || !c->k_pages || !c->v_pages || !c->block_table || !c->kv_len) {
@@ -90,6 +97,8 @@ struct Check {
         if (s != PRISM_OK) return v;
         if (misaligned(c->k_pages) || misaligned(c->v_pages) || ((v.page_stride | v.head_stride | v.row_stride) & 15))
             s = fail(p, PRISM_ERR_INVALID_ARG, "%s: bases and strides must be multiples of 16 bytes", name);
+        else if ((v.page_stride == 0 && c->n_pages > 1) || (v.head_stride == 0 && p->cfg.n_kv_heads > 1) || (v.row_stride == 0 && v.page_size > 1))
+            s = fail(p, PRISM_ERR_INVALID_ARG, "%s: a stride is 0", name);
         else if (c->n_pages < 1 || c->table_pages < 1)
             s = fail(p, PRISM_ERR_SHAPE, "%s: no pages", name);
         else if (c->batch < 1)
@@ -208,8 +217,8 @@ prism_status prism_qk_norm_rope(prism_paged *p, const prism_rows *rows, void *st
     if (!p || !rows) return fail(p, PRISM_ERR_INVALID_ARG, "prism_qk_norm_rope: null argument");
     Check c{p};
     NormRopeArgs a = c.rows<NormRopeArgs>(*rows);
-    a.q_out = c.heads(rows->q_out, "q_out");
-    a.k_out = c.heads(rows->k_out, "k_out");
+    a.q_out = c.out(rows->q_out, *rows, p->cfg.n_q_heads, "q_out");
+    a.k_out = c.out(rows->k_out, *rows, p->cfg.n_kv_heads, "k_out");
     c.need(a.pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
     if (c.s != PRISM_OK) return c.s;
     OnDevice on(p->device);
@@ -223,8 +232,8 @@ prism_status prism_qk_norm_rope_backward(prism_paged *p, const prism_rows *rows,
     NormRopeGradArgs a = c.rows<NormRopeGradArgs>(*rows);
     a.dq_out = c.heads(grads->dq_out, "dq_out");
     a.dk_out = c.heads(grads->dk_out, "dk_out");
-    a.dq = c.heads(grads->dq, "dq");
-    a.dk = c.heads(grads->dk, "dk");
+    a.dq = c.out(grads->dq, *rows, p->cfg.n_q_heads, "dq");
+    a.dk = c.out(grads->dk, *rows, p->cfg.n_kv_heads, "dk");
     a.dg_q = grads->dg_q, a.dg_k = grads->dg_k, a.part = p->grad_part, a.counter = p->grad_ticket();
     c.need(a.pos != nullptr, PRISM_ERR_INVALID_ARG, "pos is null");
     c.need(!a.g_q == !a.dg_q && !a.g_q == !a.dg_k, PRISM_ERR_INVALID_ARG, "dg_q and dg_k are given with the gains and only then");
@@ -240,7 +249,7 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
     NormRopeArgs a = c.rows<NormRopeArgs>(*rows);
     a.cache = c.cache(cache, "cache");
     a.v = c.heads(rows->v, "v");
-    a.q_out = c.heads(rows->q_out, "q_out");
+    a.q_out = c.out(rows->q_out, *rows, p->cfg.n_q_heads, "q_out");
     if (c.s != PRISM_OK) return c.s;
     c.need(rows->batch == cache->batch, PRISM_ERR_SHAPE, "the rows and the cache differ in batch");
     if (c.s != PRISM_OK) return c.s;

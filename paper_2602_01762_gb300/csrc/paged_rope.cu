@@ -287,7 +287,7 @@ __device__ __forceinline__ void grad_group(uint32_t stage, char *to, bool norm, 
         F2 x[N], y[N];
         Pairs<T>::unpack(lds16(stage + lane * 16), x);
         Pairs<T>::unpack(lds16(stage + 512 + lane * 16), y);
-        // with v = g dz:  dx = r v - x r^3 mean(v x),  dg += dz x r; both sums go together
+        // with v = g dz:  dx = r v - (x r) r^2 mean(v x),  dg += dz (x r); both sums go together
         F2 s = 0ull, c = 0ull, v[N], w[N];
 #pragma unroll
         for (int e = 0; e < N; e += 2) {
@@ -307,12 +307,16 @@ __device__ __forceinline__ void grad_group(uint32_t stage, char *to, bool norm, 
             ss += __shfl_xor_sync(0xFFFFFFFFu, ss, o);
             cc += __shfl_xor_sync(0xFFFFFFFFu, cc, o);
         }
-        const float r = rsqrtf(ss * (1.f / D) + eps), k = -r * r * r * (cc * (1.f / D));
+        // each factor r beside a factor x: no power of r that overflows where the result does not
+        // (a lane without a head adds nothing to dg, also where eps is 0)
+        const float r = to ? rsqrtf(ss * (1.f / D) + eps) : 0.f, k = -(cc * (1.f / D) * r) * r;
         const F2 rr = f2(r, r), kk = f2(k, k);
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            dg.x[e] = f2_fma(f2_mul(p[e], rr), x[e], dg.x[e]);
-            dg.y[e] = f2_fma(f2_mul(q[e], rr), y[e], dg.y[e]);
+            x[e] = f2_mul(x[e], rr);
+            y[e] = f2_mul(y[e], rr);
+            dg.x[e] = f2_fma(p[e], x[e], dg.x[e]);
+            dg.y[e] = f2_fma(q[e], y[e], dg.y[e]);
             p[e] = f2_fma(x[e], kk, f2_mul(v[e], rr));
             q[e] = f2_fma(y[e], kk, f2_mul(w[e], rr));
         }

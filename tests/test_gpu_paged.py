@@ -770,3 +770,49 @@ def test_gradient_device_flags(pkg, what, bit):
     if what == "n_new":
         assert (dq[1] == 0).all() and (dk[1] == 0).all()
     h.close()
+
+
+def test_broadcast_inputs_and_overlapping_outputs(pkg):
+    """One row for every sequence, one key head for every KV head (strides of 0) as inputs: as their copies.  As outputs: refused."""
+    B, n, Hq, Hkv, D = 3, 4, 8, 2, 64
+    g = rng(8)
+    q1, k1 = normal(g, 1, n, Hq, D, dtype=torch.bfloat16), normal(g, B, n, 1, D, dtype=torch.bfloat16)
+    q, k = q1.expand(B, n, Hq, D), k1.expand(B, n, Hkv, D)
+    dy, dk_out = normal(g, B, n, Hq, D, dtype=torch.bfloat16), normal(g, 1, 1, Hkv, D, dtype=torch.bfloat16).expand(B, n, Hkv, D)
+    pos, rope = torch.tensor([0, 3, 9], dtype=torch.int32, device="cuda"), pkg.rope_table(20, D)
+    gains = [normal(g, D, dtype=torch.bfloat16) for _ in range(2)]
+    h = handle(pkg, Hq, Hkv, D, "bf16")
+    got = []
+    for a, b, c, d in ((q, k, dy, dk_out), (q.contiguous(), k.contiguous(), dy, dk_out.contiguous())):
+        o = [torch.empty(B, n, H, D, dtype=torch.bfloat16, device="cuda") for H in (Hq, Hkv, Hq, Hkv)] + [torch.empty(2, D, device="cuda")]
+        h.qk_norm_rope(a, b, o[0], o[1], rope, pos, g_q=gains[0], g_k=gains[1])
+        h.qk_norm_rope_backward(c, d, a, b, o[2], o[3], rope, pos, g_q=gains[0], g_k=gains[1], dg_q=o[4][0], dg_k=o[4][1])
+        got.append(o)
+    assert all(torch.equal(x, y) for x, y in zip(*got))
+    wide = torch.empty(1, n, Hq, D, dtype=torch.bfloat16, device="cuda").expand(B, n, Hq, D)
+    with pytest.raises(pkg.PrismError, match="stride is 0"):
+        h.qk_norm_rope(q, k, wide, got[0][1], rope, pos)
+    with pytest.raises(pkg.PrismError, match="stride is 0"):
+        h.qk_norm_rope_backward(dy, dk_out, q, k, wide, got[0][3], rope, pos)
+    one = torch.empty(1, Hkv, 16, D, dtype=torch.bfloat16, device="cuda").expand(4, Hkv, 16, D)
+    with pytest.raises(pkg.PrismError, match="stride is 0"):
+        h.attend(h.cache(one, one, torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")),
+                 got[0][0][:1, 0].contiguous(), got[0][2][:1, 0].contiguous())
+    h.close()
+
+
+def test_gradient_of_tiny_rows(pkg):
+    """Rows of 1e-18 without an epsilon: r is 1e18 and its powers are not, the gradient is."""
+    Hq, Hkv, D = 4, 2, 64
+    q, k, _, g_q, g_k, pos, _, rope = rows_case(pkg, Hq=Hq, Hkv=Hkv, D=D, dtype="f32", B=1, n=3, gains=True)
+    q, k = q * 1e-18, k * 1e-18
+    h = handle(pkg, Hq, Hkv, D, "f32", rms_eps=0.0)
+    g = rng(3)
+    dqo, dko = normal(g, 1, 3, Hq, D, dtype=torch.float32), normal(g, 1, 3, Hkv, D, dtype=torch.float32)
+    dq, dk, dg = torch.empty_like(dqo), torch.empty_like(dko), torch.empty(2, D, device="cuda")
+    h.qk_norm_rope_backward(dqo, dko, q, k, dq, dk, rope, pos, g_q=g_q, g_k=g_k, dg_q=dg[0], dg_k=dg[1])
+    for x, gain, dy, dx, dgain in ((q, g_q, dqo, dq, dg[0]), (k, g_k, dko, dk, dg[1])):
+        want, dgw, tol, dgt = ref.norm_rope_grad(x[0], gain, dy[0], rope, int(pos[0]), 0.0)
+        ref.within(dx[0], want, tol, "dx")
+        ref.within(dgain, dgw, dgt, "dg")
+    h.close()
