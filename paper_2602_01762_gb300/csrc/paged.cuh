@@ -78,9 +78,9 @@ struct EvictArgs {
 
 constexpr int kAttendUnit = 64;          // keys per unit of the attention's work split
 constexpr int kAttendCost = 1;           // units that a segment costs beside its keys
-// Query heads that share one pass over a KV head's rows.
-int attend_head_tile(bool bf16, int G);
-size_t attend_part_floats(bool bf16, int D, int G, int sms);
+// The most passes over a KV head's rows that its G query heads take.
+int attend_head_tiles(int G);
+size_t attend_part_floats(int D, int G, int sms);
 int attend_ctas(int sms);
 // Kernel attributes, before any capture.
 cudaError_t prepare_attend_kernels();
@@ -167,6 +167,11 @@ __device__ __forceinline__ F2 f2_mul(F2 a, F2 b) {
 __device__ __forceinline__ F2 f2_fma(F2 a, F2 b, F2 c) {
     F2 r;
     asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ F2 f2_add(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
 __device__ __forceinline__ F2 f2_sub(F2 a, F2 b) {

@@ -164,8 +164,8 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
         delete p;
         return cuda_status(nullptr, e, "prism_paged_create");
     }
-    const int G = c.n_q_heads / c.n_kv_heads, ht = attend_head_tile(p->bf16, G);
-    p->segments = c.max_batch * c.n_kv_heads * ((G + ht - 1) / ht);
+    const int G = c.n_q_heads / c.n_kv_heads;
+    p->segments = c.max_batch * c.n_kv_heads * attend_head_tiles(G);
     p->cta_tickets = 2 * attend_ctas(p->sms);
     size_t bytes = 0;
     auto take = [&](size_t n) {
@@ -175,7 +175,7 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
     };
     const size_t err = take(sizeof(int)), counter = take(sizeof(int) * ((size_t)p->segments + p->cta_tickets + 2));
     const size_t zeroed = bytes;
-    const size_t part = take(sizeof(float) * attend_part_floats(p->bf16, c.head_dim, G, p->sms));
+    const size_t part = take(sizeof(float) * attend_part_floats(c.head_dim, G, p->sms));
     const size_t grad = take(sizeof(float) * 2 * c.head_dim * norm_rope_grad_ctas(p->sms));
     const size_t stat = take(c.track_weights ? sizeof(float2) * (size_t)c.max_batch * c.n_q_heads : 0);
     const size_t scores = take(c.track_weights ? sizeof(float) * (size_t)c.max_batch * c.n_q_heads * rows : 0);

@@ -236,19 +236,19 @@ template <int D_, int MODE> struct Bf16Tile {
     }
 };
 
-// fp32 rows on the CUDA cores in full fp32, two values an instruction: a lane holds
+// fp32 rows with up to 4 query heads on the CUDA cores, two values an instruction: a lane holds
 // D / 32 dims of q and of the sums, a group of 8 keys x 4 heads gives 32 partial
 // products per lane, which 31 exchanges turn into one whole score per lane (lane =
 // 4 key + head).
-template <int D_, int NG> struct F32Tile {
+template <int D_> struct F32Tile {
     using T = float;
     static constexpr int D = D_, KT = kPaStage / (8 * D), V = D / 64;   // V: pairs of dims of a lane
-    static constexpr int kHeads = 4 * NG;
+    static constexpr int kHeads = 4;
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = 3;
     static constexpr int kClusterRows = 128 * 128 / D;
-    F2 q[4 * NG][V], o[4 * NG][V];
-    float m[NG], l[NG];                                  // of head 4 ng + lane % 4
+    F2 q[4][V], o[4][V];
+    float m, l;                                          // of head lane % 4
 
     static __device__ __forceinline__ uint32_t piece(int r, int c) { return (uint32_t)(r * (4 * D) + (c << 4)); }
     static __device__ __forceinline__ void row(uint32_t addr, F2 (&f)[V]) {
@@ -261,15 +261,14 @@ template <int D_, int NG> struct F32Tile {
     __device__ __forceinline__ void load_q(const T *src, int heads) {
         const int lane = threadIdx.x & 31;
 #pragma unroll
-        for (int h = 0; h < 4 * NG; ++h)
+        for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int i = 0; i < V; ++i) q[h][i] = h < heads ? *(const F2 *)(src + h * D + lane * (2 * V) + 2 * i) : 0ull;
     }
     __device__ __forceinline__ void reset() {
+        m = -INFINITY, l = 0.f;
 #pragma unroll
-        for (int n = 0; n < NG; ++n) m[n] = -INFINITY, l[n] = 0.f;
-#pragma unroll
-        for (int h = 0; h < 4 * NG; ++h)
+        for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int i = 0; i < V; ++i) o[h][i] = 0ull;
     }
@@ -281,84 +280,318 @@ template <int D_, int NG> struct F32Tile {
             const int base = key0 + 8 * sub;
             if (base >= len) break;
             const bool in = base + (lane >> 2) < len;
+            float x[32];
 #pragma unroll
-            for (int n = 0; n < NG; ++n) {
-                float x[32];
+            for (int k = 0; k < 8; ++k) {
+                F2 f[V];
+                row(ks + (8 * sub + k) * (4 * D) + lane * (8 * V), f);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    F2 f[V];
-                    row(ks + (8 * sub + k) * (4 * D) + lane * (8 * V), f);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h) {
-                        F2 a = f2_mul(f[0], q[4 * n + h][0]);
-                        if (V == 2) a = f2_fma(f[V - 1], q[4 * n + h][V - 1], a);
-                        x[4 * k + h] = f2_sum(a);
-                    }
+                for (int h = 0; h < 4; ++h) {
+                    F2 a = f2_mul(f[0], q[h][0]);
+                    if (V == 2) a = f2_fma(f[V - 1], q[h][V - 1], a);
+                    x[4 * k + h] = f2_sum(a);
                 }
-#pragma unroll
-                for (int off = 16; off > 0; off >>= 1)
-#pragma unroll
-                    for (int i = 0; i < off; ++i) {
-                        const bool up = lane & off;
-                        const float give = up ? x[i] : x[i + off];
-                        x[i] = (up ? x[i + off] : x[i]) + __shfl_xor_sync(0xFFFFFFFFu, give, off);
-                    }
-                float s = x[0] * scale;
-                const int h = 4 * n + (lane & 3);
-                if (scores && in && h < heads) scores[(long long)(base + (lane >> 2)) * heads + h] = s;
-                if (!in) s = -INFINITY;
-                if (__any_sync(0xFFFFFFFFu, s > m[n] + kSlack)) {
-                    float mx = s;
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
-                    mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
-                    mx = fmaxf(m[n], mx);
-                    const float alpha = exp2f(m[n] - base_of(mx));
-                    m[n] = mx;
-                    l[n] *= alpha;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float a = __shfl_sync(0xFFFFFFFFu, alpha, j);
-#pragma unroll
-                        for (int i = 0; i < V; ++i) o[4 * n + j][i] = f2_mul(o[4 * n + j][i], f2(a, a));
-                    }
-                }
-                const float p = exp2f(s - base_of(m[n]));
-                l[n] += p;
-                *(float2 *)(pad + 2 * lane) = make_float2(p, p);   // as the pairs that the products below take
-                __syncwarp();
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    F2 w[4], f[V];
-                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(w[0]), "=l"(w[1]) : "r"(pads + 32 * k) : "memory");
-                    asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(w[2]), "=l"(w[3]) : "r"(pads + 32 * k + 16) : "memory");
-                    row(vs + (8 * sub + k) * (4 * D) + lane * (8 * V), f);
-#pragma unroll
-                    for (int h = 0; h < 4; ++h)
-#pragma unroll
-                        for (int i = 0; i < V; ++i) o[4 * n + h][i] = f2_fma(w[h], f[i], o[4 * n + h][i]);
-                }
-                __syncwarp();
             }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1)
+#pragma unroll
+                for (int i = 0; i < off; ++i) {
+                    const bool up = lane & off;
+                    const float give = up ? x[i] : x[i + off];
+                    x[i] = (up ? x[i + off] : x[i]) + __shfl_xor_sync(0xFFFFFFFFu, give, off);
+                }
+            float s = x[0] * scale;
+            const int h = lane & 3;
+            if (scores && in && h < heads) scores[(long long)(base + (lane >> 2)) * heads + h] = s;
+            if (!in) s = -INFINITY;
+            if (__any_sync(0xFFFFFFFFu, s > m + kSlack)) {
+                float mx = s;
+                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 4));
+                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 8));
+                mx = fmaxf(mx, __shfl_xor_sync(0xFFFFFFFFu, mx, 16));
+                mx = fmaxf(m, mx);
+                const float alpha = exp2f(m - base_of(mx));
+                m = mx;
+                l *= alpha;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float a = __shfl_sync(0xFFFFFFFFu, alpha, j);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[j][i] = f2_mul(o[j][i], f2(a, a));
+                }
+            }
+            const float p = exp2f(s - base_of(m));
+            l += p;
+            *(float2 *)(pad + 2 * lane) = make_float2(p, p);   // as the pairs that the products below take
+            __syncwarp();
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                F2 w[4], f[V];
+                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(w[0]), "=l"(w[1]) : "r"(pads + 32 * k) : "memory");
+                asm volatile("ld.shared.v2.b64 {%0, %1}, [%2];" : "=l"(w[2]), "=l"(w[3]) : "r"(pads + 32 * k + 16) : "memory");
+                row(vs + (8 * sub + k) * (4 * D) + lane * (8 * V), f);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < V; ++i) o[j][i] = f2_fma(w[j], f[i], o[j][i]);
+            }
+            __syncwarp();
         }
     }
     __device__ __forceinline__ void store(float *so, float *sm, float *sl) {
         const int lane = threadIdx.x & 31;
-#pragma unroll
-        for (int n = 0; n < NG; ++n) {
-            float v = l[n];
-            v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
-            v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
-            v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
-            if (lane < 4) {
-                sm[4 * n + lane] = m[n];
-                sl[4 * n + lane] = v;
-            }
+        float v = l;
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 4);
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
+        v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
+        if (lane < 4) {
+            sm[lane] = m;
+            sl[lane] = v;
         }
 #pragma unroll
-        for (int h = 0; h < 4 * NG; ++h)
+        for (int h = 0; h < 4; ++h)
 #pragma unroll
             for (int i = 0; i < V; ++i) *(F2 *)(so + h * kMergeStride + lane * (2 * V) + 2 * i) = o[h][i];
+    }
+};
+
+// fp32 rows with 5 to 16 query heads on the tensor cores: every value is the sum of
+// three bf16 parts (24 bits), a product the six products of parts above 2^-24 of it.
+//   S[h][key]   = q[h][:] . K[key][:]        A = q in registers, B = 8 rows of K
+//   O^T[d][h]  += V^T[d][keys] P^T[keys][h]  A = V^T, B = P^T: what S leaves in a lane
+// K and V are cut, which is exact, takes no conversion and cannot overflow; q and P
+// are rounded, so that what the products leave out has no common sign.  Up to 8 heads
+// leave half of S's 16 rows to the queries' second part.  The tensor cores drop bits
+// below their accumulator, so the large products go to four short chains and each
+// tile's O is added by the CUDA cores.  Which dim is which k (and which row of O^T)
+// is free: a lane's 16 bytes of a row are four of them, and no value is moved.
+// Measured, D = 128, 16 sequences of one KV head: 8 query heads, 40000 to 60000 rows,
+// 143 us (5.7 TB/s; on the CUDA cores 170); 16 query heads, 56800 rows, 224 us (4.2
+// TB/s; in two passes of 8 heads 304, on the CUDA cores 374).  What bounds the latter is
+// a warp's chain of some 1000 instructions to 8 rows with 8 warps an SM, which its 250
+// registers allow, not the tensor pipe (33%).
+template <int D_, int NT> struct F32Mma {
+    using T = float;
+    static constexpr int D = D_, KT = kPaStage / (8 * D);
+    static constexpr int kHeads = 8 * NT;
+    static constexpr int kMergeStride = D + 4;
+    static constexpr int kStages = NT == 2 ? 2 : 3;
+    static constexpr int kClusterRows = NT == 2 ? 256 * 128 / D : 256;
+    const T *q;                                          // this tile's, for scores recomputed
+    uint32_t qf[D / 16][3][NT][2];                       // part, heads g + 8 u, two pairs of dims
+    F2 o[D / 16][NT][2];
+    float m[NT], l[NT];                                  // of heads g + 8 u; l: of this lane's keys
+
+    // Eight lanes read two neighbouring rows of K, or four rows of V of one parity.
+    static __device__ __forceinline__ uint32_t piece(int r, int c) {
+        return (uint32_t)(r * (4 * D) + ((c ^ ((((r >> 2) ^ r) & 1) << 2 | (r & 2))) << 4));
+    }
+    static __device__ __forceinline__ float4 lds(uint32_t addr) {
+        float4 f;
+        asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(addr) : "memory");
+        return f;
+    }
+    static __device__ __forceinline__ void rounded(float x, float y, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
+        p0 = cvt_bf16x2(x, y);
+        x -= bf16lo(p0), y -= bf16hi(p0);
+        p1 = cvt_bf16x2(x, y);
+        p2 = cvt_bf16x2(x - bf16lo(p1), y - bf16hi(p1));
+    }
+    // The first bf16 parts of two values as a pair, and what a cut leaves of two values.
+    static __device__ __forceinline__ uint32_t heads_of(float x, float y) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632); }
+    static __device__ __forceinline__ F2 rest(F2 v) { return f2_sub(v, v & 0xFFFF0000FFFF0000ull); }
+    // c += a b, or a b on its own.
+    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool fresh) {
+        if (fresh)
+            asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+        else
+            asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+    }
+    // Two products of 8 keys as one of 16: part i of V with p, part j with r.
+    static __device__ __forceinline__ void pair(float (&c)[4], const uint32_t (&v)[3], const uint32_t (&w)[3], int i, uint32_t p, int j, uint32_t r, bool fresh) {
+        const uint32_t a[4] = {v[i], w[i], v[j], w[j]};
+        mma(c, a, p, r, fresh);
+    }
+    __device__ __forceinline__ void load_q(const T *src, int heads) {
+        const int lane = threadIdx.x & 31, g = lane >> 2;
+        q = src;
+#pragma unroll
+        for (int u = 0; u < NT; ++u)
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const float4 x = g + 8 * u < heads ? *(const float4 *)(src + (g + 8 * u) * D + 16 * k + 4 * (lane & 3)) : make_float4(0.f, 0.f, 0.f, 0.f);
+                rounded(x.x, x.y, qf[k][0][u][0], qf[k][1][u][0], qf[k][2][u][0]);
+                rounded(x.z, x.w, qf[k][0][u][1], qf[k][1][u][1], qf[k][2][u][1]);
+            }
+    }
+    __device__ __forceinline__ void reset() {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            m[u] = -INFINITY;
+            l[u] = 0.f;
+#pragma unroll
+            for (int d = 0; d < D / 16; ++d) o[d][u][0] = o[d][u][1] = 0ull;
+        }
+    }
+    __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, float *, int key0, int len, float scale, float *scores, int heads) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll 1
+        for (int sub = 0; sub < KT / 8; ++sub) {
+            const int base = key0 + 8 * sub;
+            if (base >= len) break;
+            float x[4][4], y[3][4];                      // q's and K's first parts; the rest
+#pragma unroll
+            for (int k = 0; k < D / 16; ++k) {
+                const float4 f = lds(ks + piece(8 * sub + g, 4 * k + t));
+                F2 v = f2(f.x, f.y), w = f2(f.z, f.w);
+                uint32_t a[3], b[3];
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    a[i] = heads_of(f2_values(v).x, f2_values(v).y);
+                    b[i] = heads_of(f2_values(w).x, f2_values(w).y);
+                    if (i < 2) v = rest(v), w = rest(w);
+                }
+                const auto &p = qf[k];
+                if (NT == 1) {
+                    const uint32_t two[4] = {p[0][0][0], p[1][0][0], p[0][0][1], p[1][0][1]}, third[4] = {p[2][0][0], 0u, p[2][0][1], 0u};
+                    mma(x[k & 3], two, a[0], b[0], k < 4);
+                    mma(y[0], two, a[1], b[1], k == 0);
+                    mma(y[1], two, a[2], b[2], k == 0);
+                    mma(y[1], third, a[0], b[0], false);
+                } else {
+                    const uint32_t q0[4] = {p[0][0][0], p[0][NT - 1][0], p[0][0][1], p[0][NT - 1][1]};
+                    const uint32_t q1[4] = {p[1][0][0], p[1][NT - 1][0], p[1][0][1], p[1][NT - 1][1]};
+                    const uint32_t q2[4] = {p[2][0][0], p[2][NT - 1][0], p[2][0][1], p[2][NT - 1][1]};
+                    mma(x[k & 3], q0, a[0], b[0], k < 4);
+                    mma(y[0], q1, a[0], b[0], k == 0);
+                    mma(y[1], q2, a[0], b[0], k == 0);
+                    mma(y[2], q0, a[1], b[1], k == 0);
+                    mma(y[0], q1, a[1], b[1], false);
+                    mma(y[1], q0, a[2], b[2], false);
+                }
+            }
+            float s[NT][2];
+            bool nan = false;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const bool in = base + 2 * t + i < len;
+                if (NT == 1) y[0][i] += (x[0][2 + i] + x[1][2 + i]) + (x[2][2 + i] + x[3][2 + i]) + (y[0][2 + i] + y[1][2 + i]);
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    const int c = 2 * u + i;
+                    s[u][i] = (((x[0][c] + x[1][c]) + (x[2][c] + x[3][c])) + (y[0][c] + y[1][c]) + (NT == 2 ? y[2][c] : 0.f)) * scale;
+                    nan |= in && g + 8 * u < heads && s[u][i] != s[u][i];
+                }
+            }
+            if (__any_sync(0xFFFFFFFFu, nan)) {          // infinities have no parts: the score as it is defined
+#pragma unroll
+                for (int u = 0; u < NT; ++u)
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        if (g + 8 * u >= heads) continue;
+                        float z = 0.f;
+#pragma unroll 1
+                        for (int c = 0; c < D / 4; ++c) {
+                            const float4 f = lds(ks + piece(8 * sub + 2 * t + i, c)), w = *(const float4 *)(q + (g + 8 * u) * D + 4 * c);
+                            z = fmaf(f.x, w.x, fmaf(f.y, w.y, fmaf(f.z, w.z, fmaf(f.w, w.w, z))));
+                        }
+                        s[u][i] = z * scale;
+                    }
+            }
+            bool grew = false;
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) {
+                    const int key = base + 2 * t + i;
+                    if (scores && key < len && g + 8 * u < heads) scores[(long long)key * heads + g + 8 * u] = s[u][i];
+                    if (key >= len) s[u][i] = -INFINITY;
+                }
+                grew |= fmaxf(s[u][0], s[u][1]) > m[u] + kSlack;
+            }
+            if (__any_sync(0xFFFFFFFFu, grew)) {
+#pragma unroll
+                for (int u = 0; u < NT; ++u) {
+                    float v = fmaxf(s[u][0], s[u][1]);
+                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 1));
+                    v = fmaxf(v, __shfl_xor_sync(0xFFFFFFFFu, v, 2));
+                    v = fmaxf(m[u], v);
+                    const float alpha = exp2f(m[u] - base_of(v));
+                    m[u] = v;
+                    l[u] *= alpha;
+                    const F2 both = f2(__shfl_sync(0xFFFFFFFFu, alpha, 8 * t), __shfl_sync(0xFFFFFFFFu, alpha, 8 * t + 4));
+#pragma unroll
+                    for (int d = 0; d < D / 16; ++d) {
+                        o[d][u][0] = f2_mul(o[d][u][0], both);
+                        o[d][u][1] = f2_mul(o[d][u][1], both);
+                    }
+                }
+            }
+            uint32_t p[NT][3];
+#pragma unroll
+            for (int u = 0; u < NT; ++u) {
+                const float b = base_of(m[u]), p0 = exp2f(s[u][0] - b), p1 = exp2f(s[u][1] - b);
+                l[u] += p0 + p1;
+                rounded(p0, p1, p[u][0], p[u][1], p[u][2]);
+            }
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                const float4 f0 = lds(vs + piece(8 * sub + 2 * t, 8 * k + g)), f1 = lds(vs + piece(8 * sub + 2 * t + 1, 8 * k + g));
+                F2 lo[2] = {f2(f0.x, f0.y), f2(f1.x, f1.y)}, hi[2] = {f2(f0.z, f0.w), f2(f1.z, f1.w)};
+                uint32_t v[4][3];
+#pragma unroll
+                for (int i = 0; i < 3; ++i) {
+                    v[0][i] = heads_of(f2_values(lo[0]).x, f2_values(lo[1]).x);
+                    v[1][i] = heads_of(f2_values(lo[0]).y, f2_values(lo[1]).y);
+                    v[2][i] = heads_of(f2_values(hi[0]).x, f2_values(hi[1]).x);
+                    v[3][i] = heads_of(f2_values(hi[0]).y, f2_values(hi[1]).y);
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        if (i < 2) lo[r] = rest(lo[r]), hi[r] = rest(hi[r]);
+                }
+                float c[2][NT][4];
+#pragma unroll
+                for (int i = 0; i < 3; ++i)
+#pragma unroll
+                    for (int d = 0; d < 2; ++d)
+#pragma unroll
+                        for (int u = 0; u < NT; ++u)
+                            if (i == 0)
+                                pair(c[d][u], v[2 * d], v[2 * d + 1], 2, p[u][0], 0, p[u][2], true);
+                            else
+                                pair(c[d][u], v[2 * d], v[2 * d + 1], 0, p[u][2 - i], 1, p[u][2 - i], false);
+#pragma unroll
+                for (int d = 0; d < 2; ++d)
+#pragma unroll
+                    for (int u = 0; u < NT; ++u) {
+                        o[2 * k + d][u][0] = f2_add(o[2 * k + d][u][0], f2(c[d][u][0], c[d][u][1]));
+                        o[2 * k + d][u][1] = f2_add(o[2 * k + d][u][1], f2(c[d][u][2], c[d][u][3]));
+                    }
+            }
+        }
+    }
+    __device__ __forceinline__ void store(float *so, float *sm, float *sl) {
+        const int lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            float v = l[u];
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 1);
+            v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
+            if (t == 0) {
+                sm[g + 8 * u] = m[u];
+                sl[g + 8 * u] = v;
+            }
+#pragma unroll
+            for (int k = 0; k < D / 32; ++k) {
+                const float2 a = f2_values(o[2 * k][u][0]), b = f2_values(o[2 * k][u][1]);
+                const float2 c = f2_values(o[2 * k + 1][u][0]), d = f2_values(o[2 * k + 1][u][1]);
+                float *to = so + (8 * u + 2 * t) * kMergeStride + 32 * k + 4 * g;
+                *(float4 *)to = make_float4(a.x, b.x, c.x, d.x);
+                *(float4 *)(to + kMergeStride) = make_float4(a.y, b.y, c.y, d.y);
+            }
+        }
     }
 };
 
@@ -840,32 +1073,34 @@ __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel
     }
 }
 
-// The tile form of a type, head dimension and group: 4, 8 or 16 heads of bf16, 4
-// or 8 of fp32 share a pass over the rows; more heads take more passes.
-template <typename F> cudaError_t with_tile(bool bf16, int D, int G, const F &f) {
+// The tile form of a type, head dimension and heads that share a pass over the rows
+// (4, 8 or 16; more heads take more passes).
+template <typename F> cudaError_t with_tile(bool bf16, int D, int heads, const F &f) {
     if (bf16) {
-        if (D == 128) return G <= 4 ? f(Bf16Tile<128, kPacked>()) : G <= 8 ? f(Bf16Tile<128, kEight>()) : f(Bf16Tile<128, kSixteen>());
-        return G <= 4 ? f(Bf16Tile<64, kPacked>()) : G <= 8 ? f(Bf16Tile<64, kEight>()) : f(Bf16Tile<64, kSixteen>());
+        if (D == 128) return heads == 4 ? f(Bf16Tile<128, kPacked>()) : heads == 8 ? f(Bf16Tile<128, kEight>()) : f(Bf16Tile<128, kSixteen>());
+        return heads == 4 ? f(Bf16Tile<64, kPacked>()) : heads == 8 ? f(Bf16Tile<64, kEight>()) : f(Bf16Tile<64, kSixteen>());
     }
-    if (D == 128) return G <= 4 ? f(F32Tile<128, 1>()) : f(F32Tile<128, 2>());
-    return G <= 4 ? f(F32Tile<64, 1>()) : f(F32Tile<64, 2>());
+    if (D == 128) return heads == 4 ? f(F32Tile<128>()) : heads == 8 ? f(F32Mma<128, 1>()) : f(F32Mma<128, 2>());
+    return heads == 4 ? f(F32Tile<64>()) : heads == 8 ? f(F32Mma<64, 1>()) : f(F32Mma<64, 2>());
 }
 
 }  // namespace
 
-int attend_head_tile(bool bf16, int G) { return G <= 4 ? 4 : G <= 8 || !bf16 ? 8 : 16; }
+static int attend_head_tile(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
+
+int attend_head_tiles(int G) { return (G + 7) / 8; }
 
 int attend_ctas(int sms) { return sms * kPaCtasPerSm; }
 
-size_t attend_part_floats(bool bf16, int D, int G, int sms) {
-    return (size_t)2 * attend_ctas(sms) * attend_head_tile(bf16, G) * (D + 2);
+size_t attend_part_floats(int D, int G, int sms) {
+    return (size_t)2 * attend_ctas(sms) * attend_head_tile(G) * (D + 2);
 }
 
 cudaError_t prepare_attend_kernels() {
     for (const bool bf16 : {false, true})
         for (const int D : {64, 128})
-            for (const int G : {4, 8, 16}) {
-                const cudaError_t e = with_tile(bf16, D, G, [](auto tile) {
+            for (const int heads : {4, 8, 16}) {
+                const cudaError_t e = with_tile(bf16, D, heads, [](auto tile) {
                     using P = decltype(tile);
                     const cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<P, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
                     return e != cudaSuccess ? e : cudaFuncSetAttribute(paged_attend_kernel<P, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
@@ -877,7 +1112,8 @@ cudaError_t prepare_attend_kernels() {
 
 // CTAs of a cluster per segment, or 1: the shares of a persistent grid.  Clusters
 // where all of them run at once and a table's rows are few for each CTA: at most
-// `rows` (bf16 at D = 128: 512, with 9 to 16 query heads 1024, fp32 128).  Measured, 8 KV
+// `rows` (bf16 at D = 128: 512, with 9 to 16 query heads 1024; fp32 128,
+// with 5 to 16 query heads 256).  Measured, 8 KV
 // heads of 128 and 4 query heads each, cluster against shares: one sequence of 100
 // rows 4.7 and 6.6 us, of 1000 5.9 and 8.0, of 4000 9.8 and 9.8; four of 4000 15.0 and
 // 17.3; fp32 of 1000 rows 7.7 and 8.8, of 2000 11.1 and 9.8; 4 KV heads with 16 query
@@ -890,11 +1126,17 @@ static int attend_cluster(long long segments, long long cap, int rows, int sms) 
 
 cudaError_t launch_paged_attend(const AttendArgs &args, bool bf16, int D, int sms, cudaStream_t s) {
     AttendArgs a = args;
-    const int G = a.Hq / a.Hkv, ht = attend_head_tile(bf16, G);
-    const long long cap = (long long)a.cache.table_pages * a.cache.page_size;
-    const long long segments = a.B * (long long)a.Hkv * ((G + ht - 1) / ht);
+    const int G = a.Hq / a.Hkv;
+    const long long cap = (long long)a.cache.table_pages * a.cache.page_size, groups = a.B * (long long)a.Hkv;
+    int ht = attend_head_tile(G);
+    // fp32 tables of few rows: a tile of 16 heads takes longer than the second pass of
+    // two of 8.  Measured, D = 128, 8 against 16: 4 KV heads of 1000 rows 9.6 and 12.3
+    // us, of 8000 24 and 26, of 16000 35 and 36; 32 sequences of 500 rows 34 and 24;
+    // D = 64: 4000 rows 11.7 and 17.1, 8 sequences of 1000 rows 11.9 and 10.5.
+    if (!bf16 && ht == 16 && groups * ((G + 15) / 16) * cap <= 256 * D) ht = 8;
+    const long long segments = groups * ((G + ht - 1) / ht);
     const long long most = segments * (kAttendCost + (cap + kAttendUnit - 1) / kAttendUnit);
-    cudaError_t e = with_tile(bf16, D, G, [&](auto tile) {
+    cudaError_t e = with_tile(bf16, D, ht, [&](auto tile) {
         using P = decltype(tile);
         a.cluster = attend_cluster(segments, cap, P::kClusterRows, sms);
         if (a.cluster > 1)

@@ -168,6 +168,67 @@ def test_attend_infinite_and_nan_values(pkg, dtype):
     h.close()
 
 
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("Hq,Hkv", [(9, 1), (16, 1), (13, 1), (40, 2)])
+def test_attend_fp32_many_heads_over_many_rows(pkg, D, Hq, Hkv):
+    """16 heads of fp32 to a pass, in shares of the grid, with and without weights."""
+    check_attend(pkg, Hq=Hq, Hkv=Hkv, D=D, dtype="f32", page=24, lens=[17, 0, 9001, 1, 8191, 33], track=Hq != 13, seed=Hq)
+
+
+@pytest.mark.parametrize("D,Hq", [(64, 16), (128, 16), (64, 7), (128, 10)])
+def test_attend_fp32_many_heads_short_rows(pkg, D, Hq):
+    """The same in clusters: many short sequences."""
+    check_attend(pkg, Hq=Hq, Hkv=1, D=D, dtype="f32", page=16, lens=[480] + [(37 * i) % 481 for i in range(69)], track=True)
+
+
+@pytest.mark.parametrize("G", [8, 16])
+@pytest.mark.parametrize("qscale", [0.0, 1e-3, 30.0, 1e-30])
+def test_attend_fp32_parts(pkg, G, qscale):
+    """Flat, peaked and vanishing scores of values in three parts."""
+    check_attend(pkg, Hq=G, Hkv=1, D=128, dtype="f32", page=64, lens=[33001, 77], qscale=qscale, wild=False)
+    check_attend(pkg, Hq=2 * G, Hkv=2, D=64, dtype="f32", page=8, lens=[300, 77], qscale=qscale, scale=0.31)
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [5, 8, 12, 16])
+@pytest.mark.parametrize("rows", [50, 33000])
+def test_attend_fp32_many_heads_infinite_and_nan_values(pkg, D, G, rows):
+    """Infinities have no finite parts; scores are what their definition says all the same."""
+    h, cache, q, out, lse, _ = attend_case(pkg, Hq=2 * G, Hkv=2, D=D, dtype="f32", page=16, lens=[50, 50, rows], wild=False)
+    lowest = torch.finfo(torch.float32).min
+    k, t = cache.k_pages, cache.block_table
+    q.fill_(0)
+    q[..., 0] = 1.0
+    q[:, 1, 0] = 0.0                       # head 1: 0 times infinity
+    q[:, 2, 1] = -1.0                      # head 2: minus the second dim as well
+    for j in range(50):
+        at = lambda b, hd: k[int(t[b, j // 16]), hd, j % 16]  # noqa: B023,E731
+        at(0, 0)[0] = -math.inf if j != 33 else 0.5
+        at(0, 0)[1] = 0.25
+        at(0, 1)[0] = -math.inf
+        at(0, 1)[1] = 0.0
+        at(1, 0)[0] = lowest
+        at(1, 0)[1] = 0.0
+        at(1, 1)[0] = math.nan if j == 20 else 1.0
+    h.attend(cache, q, out, lse=lse, added=0)
+    assert h.status() == 0
+    v_at = lambda b, hd, j: cache.v_pages[int(t[b, j // 16]), hd, j % 16]  # noqa: E731
+    for head in range(G):
+        if head == 1:
+            assert torch.isnan(out[0, head]).all() and torch.isnan(lse[0, head])
+        else:
+            assert torch.equal(out[0, head], v_at(0, 0, 33))
+    assert (out[0, G:] == 0).all() and (lse[0, G:] == -math.inf).all()
+    mean = torch.stack([v_at(1, 0, j).double() for j in range(50)]).mean(0)
+    spread = torch.stack([v_at(1, 0, j).double().abs() for j in range(50)]).mean(0)
+    ref.within(out[1, :G], mean.expand(G, D), 2.0 ** -19 * spread.expand(G, D), "average")
+    assert torch.isnan(out[1, G:]).all() and torch.isfinite(out[1, :G]).all()
+    o, l, _, to, tl, _ = ref.attend(q[2:], k, cache.v_pages, t[2:], [rows], D ** -0.5)
+    ref.within(out[2:], o, to)
+    ref.within(lse[2:], l, tl)
+    h.close()
+
+
 def test_attend_added_rows_and_other_stream(pkg):
     h, cache, q, out, lse, scale = attend_case(pkg, Hq=8, Hkv=2, D=128, dtype="bf16", page=16, lens=[40, 129], wild=False)
     cache.kv_len.sub_(1)
