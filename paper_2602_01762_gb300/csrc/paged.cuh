@@ -34,7 +34,7 @@ struct NormRopeArgs {
     const void *g_q, *g_k;               // [D] wtype, or both null: no norm
     const float *rope;                   // [rope_len, 2, D/2]: cosines, then sines
     const int32_t *pos, *n_new;          // [B]; n_new null: max_new rows each
-    int rope_len, B, max_new, Hq, Hkv, split;
+    int rope_len, B, max_new, Hq, Hkv, split, heads;   // heads: of a row that a warp takes at a time
     float eps;
     int *err;
 };
@@ -47,7 +47,7 @@ struct NormRopeGradArgs {
     float *dg_q, *dg_k;                  // [D] fp32 (null without gains)
     float *part;                         // [CTAs, 2, D]
     int *counter;                        // last-CTA ticket (left at zero)
-    int rope_len, B, max_new, Hq, Hkv, split;
+    int rope_len, B, max_new, Hq, Hkv, split, heads;
     float eps;
     int *err;
 };

@@ -458,6 +458,23 @@ def test_append(pkg, dtype, Hq, Hkv, D, page, layout, B, n, gains):
     h.close()
 
 
+FEW = [(2, 1, 64), (4, 4, 64), (1, 1, 64), (3, 1, 64), (6, 2, 64), (8, 2, 128), (1, 1, 128), (5, 1, 128), (7, 7, 128)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", FEW)
+@pytest.mark.parametrize("B,n,order", [(37, 701, "fused"), (300, 37, "heads")])
+def test_norm_rope_and_gradient_of_few_heads(pkg, dtype, Hq, Hkv, D, B, n, order):
+    """Rows enough that a warp takes several at a time, of one sequence or of two, some past n_new."""
+    test_norm_rope_and_gradient(pkg, dtype, Hq, Hkv, D, order == "fused", B, n, order)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("Hq,Hkv,D", FEW)
+def test_append_few_heads(pkg, dtype, Hq, Hkv, D):
+    test_append(pkg, dtype, Hq, Hkv, D, 24, "rows_first", 19, 301, True)
+
+
 def test_append_positions_default_to_slots(pkg):
     q, k, v, _, _, _, _, rope = rows_case(pkg, Hq=4, Hkv=4, D=64, dtype="f32", B=2, n=3, gains=False)
     h = handle(pkg, 4, 4, 64, "f32", max_batch=2, max_pages=2)
