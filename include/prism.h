@@ -590,8 +590,9 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
  * sequence without rows gives zeros and -inf.  If the cache has weights, each
  * row's grows by the sum of its probabilities over the KV head's query heads
  * (needs track_weights).  Scores, probabilities and sums are fp32; the result
- * does not depend on the order in which CTAs run.  Errors: INVALID_ARG, SHAPE,
- * CAPACITY, CUDA. */
+ * does not depend on the order in which CTAs run.  A score of -inf drops its row, NaN
+ * or +inf makes its head NaN; an infinite value in V makes that dim of its KV head's
+ * outputs infinite or NaN.  Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
 prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,
                                 float *lse, void *stream);
 
