@@ -46,6 +46,14 @@ __device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], 
                  : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
 
+// Two values as three bf16 parts each, rounded: their sum is the value.
+__device__ __forceinline__ void three_parts(float x, float y, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
+    p0 = cvt_bf16x2(x, y);
+    x -= bf16lo(p0), y -= bf16hi(p0);
+    p1 = cvt_bf16x2(x, y);
+    p2 = cvt_bf16x2(x - bf16lo(p1), y - bf16hi(p1));
+}
+
 // What a warp subtracts from its scores is a maximum it has met, renewed (and its sums
 // rescaled) only when a score passes it by more than this: probabilities stay below
 // 2^8 times the largest, and most tiles need no exchange between lanes.
@@ -58,17 +66,18 @@ __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f 
 // tile:
 //   S^T[key][h] = K[key][:] . q[h][:]        A = 16 rows of K, B = q^T in registers
 //   O^T[d][h]  += V^T[d][keys] P^T[keys][h]  A = V^T (transposing load), B = P^T
-// q and K enter exactly.  P is split into two bf16 parts, P = hi + lo to 2^-17,
-// so that what the result loses is its own rounding: kPacked (G <= 4) holds the
-// four heads' hi in columns 0-3 and lo in columns 4-7 of one product, the wider
-// forms take two products.  Per warp and tile of 16 keys: 8 + 8 products of
-// 16x8x16 at D = 128 (kPacked), far below the tensor pipe's rate at the speed
-// rows arrive.
+// q and K enter exactly.  P is the sum of three bf16 parts (its 24 bits), so that
+// what the result loses is its own rounding: kPacked (G <= 4) holds the four heads'
+// first parts in columns 0-3 and second parts in columns 4-7 of one product, the
+// third parts in another; the wider forms take three products.  Per warp and tile of
+// 16 keys: 8 + 16 products of 16x8x16 at D = 128 (kPacked), far below the tensor
+// pipe's rate at the speed rows arrive.
 enum HeadMode : int { kPacked = 0, kEight = 1, kSixteen = 2 };
 template <int D_, int MODE> struct Bf16Tile {
     using T = uint16_t;
     static constexpr int D = D_, KT = kPaStage / (4 * D), NT = MODE == kSixteen ? 2 : 1;
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
+    static constexpr int kParts = MODE == kPacked ? 2 : 3;   // products of P and V
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = MODE == kSixteen ? 2 : 3;
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
@@ -175,7 +184,7 @@ template <int D_, int MODE> struct Bf16Tile {
                     }
                 }
             }
-            uint32_t hi[NT][2], lo[NT][2];
+            uint32_t part[kParts][NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
                 const float b0 = base_of(m[t][0]), b1 = base_of(m[t][1]);
@@ -184,13 +193,15 @@ template <int D_, int MODE> struct Bf16Tile {
                     const float p0 = exp2f(s[t][2 * u] - b0), p1 = exp2f(s[t][2 * u + 1] - b1);
                     l[t][0] += p0;
                     l[t][1] += p1;
-                    const uint32_t h = cvt_bf16x2(p0, p1);
-                    const uint32_t r = cvt_bf16x2(p0 - bf16lo(h), p1 - bf16hi(h));
+                    uint32_t x, y, z;
+                    three_parts(p0, p1, x, y, z);
                     if (MODE == kPacked) {
-                        hi[t][u] = transpose8((lane & 2) ? r : h);
+                        part[0][t][u] = transpose8((lane & 2) ? y : x);
+                        part[1][t][u] = transpose8((lane & 2) ? 0u : z);
                     } else {
-                        hi[t][u] = transpose8(h);
-                        lo[t][u] = transpose8(r);
+                        part[0][t][u] = transpose8(x);
+                        part[1][t][u] = transpose8(y);
+                        part[kParts - 1][t][u] = transpose8(z);
                     }
                 }
             }
@@ -200,10 +211,9 @@ template <int D_, int MODE> struct Bf16Tile {
                 uint32_t a[4];
                 lds_x4_t(vs + piece(vr, 2 * d + ((lane >> 3) & 1)), a);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) {
-                    mma_bf16(o[d][t], a, hi[t][0], hi[t][1]);
-                    if (MODE != kPacked) mma_bf16(o[d][t], a, lo[t][0], lo[t][1]);
-                }
+                for (int t = 0; t < NT; ++t)
+#pragma unroll
+                    for (int i = kParts - 1; i >= 0; --i) mma_bf16(o[d][t], a, part[i][t][0], part[i][t][1]);
             }
         }
     }
@@ -391,12 +401,6 @@ template <int D_, int NT> struct F32Mma {
         asm volatile("ld.shared.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(f.x), "=f"(f.y), "=f"(f.z), "=f"(f.w) : "r"(addr) : "memory");
         return f;
     }
-    static __device__ __forceinline__ void rounded(float x, float y, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
-        p0 = cvt_bf16x2(x, y);
-        x -= bf16lo(p0), y -= bf16hi(p0);
-        p1 = cvt_bf16x2(x, y);
-        p2 = cvt_bf16x2(x - bf16lo(p1), y - bf16hi(p1));
-    }
     // The first bf16 parts of two values as a pair, and what a cut leaves of two values.
     static __device__ __forceinline__ uint32_t heads_of(float x, float y) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632); }
     static __device__ __forceinline__ F2 rest(F2 v) { return f2_sub(v, v & 0xFFFF0000FFFF0000ull); }
@@ -422,8 +426,8 @@ template <int D_, int NT> struct F32Mma {
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 const float4 x = g + 8 * u < heads ? *(const float4 *)(src + (g + 8 * u) * D + 16 * k + 4 * (lane & 3)) : make_float4(0.f, 0.f, 0.f, 0.f);
-                rounded(x.x, x.y, qf[k][0][u][0], qf[k][1][u][0], qf[k][2][u][0]);
-                rounded(x.z, x.w, qf[k][0][u][1], qf[k][1][u][1], qf[k][2][u][1]);
+                three_parts(x.x, x.y, qf[k][0][u][0], qf[k][1][u][0], qf[k][2][u][0]);
+                three_parts(x.z, x.w, qf[k][0][u][1], qf[k][1][u][1], qf[k][2][u][1]);
             }
     }
     __device__ __forceinline__ void reset() {
@@ -534,7 +538,7 @@ template <int D_, int NT> struct F32Mma {
             for (int u = 0; u < NT; ++u) {
                 const float b = base_of(m[u]), p0 = exp2f(s[u][0] - b), p1 = exp2f(s[u][1] - b);
                 l[u] += p0 + p1;
-                rounded(p0, p1, p[u][0], p[u][1], p[u][2]);
+                three_parts(p0, p1, p[u][0], p[u][1], p[u][2]);
             }
 #pragma unroll
             for (int k = 0; k < D / 32; ++k) {
