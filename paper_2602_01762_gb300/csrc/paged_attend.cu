@@ -39,13 +39,15 @@ __device__ __forceinline__ uint32_t transpose8(uint32_t x) {
     asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
     return y;
 }
-__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, "
-                 "{%8, %9}, {%0, %1, %2, %3};"
-                 : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
-                 : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+// c += a b, or a b on its own.
+__device__ __forceinline__ void mma_bf16(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool fresh) {
+    if (fresh)
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+            : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+    else
+        asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+            : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-
 // Two values as three bf16 parts each, rounded: their sum is the value.
 __device__ __forceinline__ void three_parts(float x, float y, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
     p0 = cvt_bf16x2(x, y);
@@ -71,7 +73,9 @@ __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f 
 // first parts in columns 0-3 and second parts in columns 4-7 of one product, the
 // third parts in another; the wider forms take three products.  Per warp and tile of
 // 16 keys: 8 + 16 products of 16x8x16 at D = 128 (kPacked), far below the tensor
-// pipe's rate at the speed rows arrive.
+// pipe's rate at the speed rows arrive.  The tensor cores drop bits below their
+// accumulator, so each tile's O is added by the CUDA cores: sums over many rows
+// would drift towards 0.
 enum HeadMode : int { kPacked = 0, kEight = 1, kSixteen = 2 };
 template <int D_, int MODE> struct Bf16Tile {
     using T = uint16_t;
@@ -82,7 +86,8 @@ template <int D_, int MODE> struct Bf16Tile {
     static constexpr int kStages = MODE == kSixteen ? 2 : 3;
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     uint32_t qf[D / 16][NT][2];
-    float m[NT][2], l[NT][2], o[D / 16][NT][4];
+    float m[NT][2], l[NT][2];
+    F2 o[D / 16][NT][2];                                 // rows g and g + 8 of a head pair
 
     // Shared address of 16-byte piece c of row r: pieces exchanged by row, so that
     // eight rows of one piece lie in different banks.
@@ -107,9 +112,7 @@ template <int D_, int MODE> struct Bf16Tile {
             m[t][0] = m[t][1] = -INFINITY;
             l[t][0] = l[t][1] = 0.f;
 #pragma unroll
-            for (int d = 0; d < D / 16; ++d)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) o[d][t][i] = 0.f;
+            for (int d = 0; d < D / 16; ++d) o[d][t][0] = o[d][t][1] = 0ull;
         }
     }
     // One stage: rows key0 .. key0 + KT - 1, of which those below len count.
@@ -120,17 +123,13 @@ template <int D_, int MODE> struct Bf16Tile {
             const int base = key0 + 16 * sub;
             if (sub > 0 && base >= len) break;
             float s[NT][4], s2[NT][4];                   // even and odd steps over D: half the chain of products
-#pragma unroll
-            for (int t = 0; t < NT; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) s[t][i] = s2[t][i] = 0.f;
             const int kr = 16 * sub + (lane & 15);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
                 uint32_t a[4];
                 lds_x4(ks + piece(kr, 2 * k + (lane >> 4)), a);
 #pragma unroll
-                for (int t = 0; t < NT; ++t) mma_bf16(k & 1 ? s2[t] : s[t], a, qf[k][t][0], qf[k][t][1]);
+                for (int t = 0; t < NT; ++t) mma_bf16(k & 1 ? s2[t] : s[t], a, qf[k][t][0], qf[k][t][1], k < 2);
             }
             const bool in0 = base + g < len, in1 = base + g + 8 < len;
             bool grew = false;
@@ -175,12 +174,11 @@ template <int D_, int MODE> struct Bf16Tile {
                         m[t][i] = v;
                         l[t][i] *= a[i];
                     }
+                    const F2 both = f2(a[0], a[1]);
 #pragma unroll
                     for (int d = 0; d < D / 16; ++d) {
-                        o[d][t][0] *= a[0];
-                        o[d][t][1] *= a[1];
-                        o[d][t][2] *= a[0];
-                        o[d][t][3] *= a[1];
+                        o[d][t][0] = f2_mul(o[d][t][0], both);
+                        o[d][t][1] = f2_mul(o[d][t][1], both);
                     }
                 }
             }
@@ -211,9 +209,13 @@ template <int D_, int MODE> struct Bf16Tile {
                 uint32_t a[4];
                 lds_x4_t(vs + piece(vr, 2 * d + ((lane >> 3) & 1)), a);
 #pragma unroll
-                for (int t = 0; t < NT; ++t)
+                for (int t = 0; t < NT; ++t) {
+                    float x[4];
 #pragma unroll
-                    for (int i = kParts - 1; i >= 0; --i) mma_bf16(o[d][t], a, part[i][t][0], part[i][t][1]);
+                    for (int i = kParts - 1; i >= 0; --i) mma_bf16(x, a, part[i][t][0], part[i][t][1], i == kParts - 1);
+                    o[d][t][0] = f2_add(o[d][t][0], f2(x[0], x[1]));
+                    o[d][t][1] = f2_add(o[d][t][1], f2(x[2], x[3]));
+                }
             }
         }
     }
@@ -235,9 +237,10 @@ template <int D_, int MODE> struct Bf16Tile {
             }
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
+                const float2 x[2] = {f2_values(o[d][t][0]), f2_values(o[d][t][1])};
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float v = o[d][t][i];
+                    float v = i & 1 ? x[i >> 1].y : x[i >> 1].x;
                     if (MODE == kPacked) v += __shfl_xor_sync(0xFFFFFFFFu, v, 2);
                     if (8 * t + c < kHeads) so[(8 * t + c + (i & 1)) * kMergeStride + 16 * d + g + 8 * (i >> 1)] = v;
                 }
@@ -404,19 +407,10 @@ template <int D_, int NT> struct F32Mma {
     // The first bf16 parts of two values as a pair, and what a cut leaves of two values.
     static __device__ __forceinline__ uint32_t heads_of(float x, float y) { return __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632); }
     static __device__ __forceinline__ F2 rest(F2 v) { return f2_sub(v, v & 0xFFFF0000FFFF0000ull); }
-    // c += a b, or a b on its own.
-    static __device__ __forceinline__ void mma(float (&c)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, bool fresh) {
-        if (fresh)
-            asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
-                : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-        else
-            asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
-                : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-    }
     // Two products of 8 keys as one of 16: part i of V with p, part j with r.
     static __device__ __forceinline__ void pair(float (&c)[4], const uint32_t (&v)[3], const uint32_t (&w)[3], int i, uint32_t p, int j, uint32_t r, bool fresh) {
         const uint32_t a[4] = {v[i], w[i], v[j], w[j]};
-        mma(c, a, p, r, fresh);
+        mma_bf16(c, a, p, r, fresh);
     }
     __device__ __forceinline__ void load_q(const T *src, int heads) {
         const int lane = threadIdx.x & 31, g = lane >> 2;
@@ -460,20 +454,20 @@ template <int D_, int NT> struct F32Mma {
                 const auto &p = qf[k];
                 if (NT == 1) {
                     const uint32_t two[4] = {p[0][0][0], p[1][0][0], p[0][0][1], p[1][0][1]}, third[4] = {p[2][0][0], 0u, p[2][0][1], 0u};
-                    mma(x[k & 3], two, a[0], b[0], k < 4);
-                    mma(y[0], two, a[1], b[1], k == 0);
-                    mma(y[1], two, a[2], b[2], k == 0);
-                    mma(y[1], third, a[0], b[0], false);
+                    mma_bf16(x[k & 3], two, a[0], b[0], k < 4);
+                    mma_bf16(y[0], two, a[1], b[1], k == 0);
+                    mma_bf16(y[1], two, a[2], b[2], k == 0);
+                    mma_bf16(y[1], third, a[0], b[0], false);
                 } else {
                     const uint32_t q0[4] = {p[0][0][0], p[0][NT - 1][0], p[0][0][1], p[0][NT - 1][1]};
                     const uint32_t q1[4] = {p[1][0][0], p[1][NT - 1][0], p[1][0][1], p[1][NT - 1][1]};
                     const uint32_t q2[4] = {p[2][0][0], p[2][NT - 1][0], p[2][0][1], p[2][NT - 1][1]};
-                    mma(x[k & 3], q0, a[0], b[0], k < 4);
-                    mma(y[0], q1, a[0], b[0], k == 0);
-                    mma(y[1], q2, a[0], b[0], k == 0);
-                    mma(y[2], q0, a[1], b[1], k == 0);
-                    mma(y[0], q1, a[1], b[1], false);
-                    mma(y[1], q0, a[2], b[2], false);
+                    mma_bf16(x[k & 3], q0, a[0], b[0], k < 4);
+                    mma_bf16(y[0], q1, a[0], b[0], k == 0);
+                    mma_bf16(y[1], q2, a[0], b[0], k == 0);
+                    mma_bf16(y[2], q0, a[1], b[1], k == 0);
+                    mma_bf16(y[0], q1, a[1], b[1], false);
+                    mma_bf16(y[1], q0, a[2], b[2], false);
                 }
             }
             float s[NT][2];

@@ -60,3 +60,32 @@ def test_probabilities_keep_their_bits(dtype, D, G):
         tol = tol + 2.0 ** -8 * want.abs()
     worst = float(((got - want).abs() / tol).max())
     assert worst <= 1, worst
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [4, 8, 16])
+def test_long_sums_do_not_drift(D, G):
+    """bf16: 2^14 enters every warp's sums at its first tile and leaves at its last, small values in between.
+
+    All keys are 0: every p is 1.  A tile of r rows is added at an ulp of 2^-9: N / r roundings to nearest of deviation
+    2^-9 / sqrt(12), six of these (1e-9 of all results beyond), one whole ulp for each of the eight tiles with 2^14 in
+    them, and half an ulp of the bf16 result.  Sums that drop the low bits of each tile instead lose half an ulp every time,
+    N / r 2^-10.
+    """
+    ctas = 2 * torch.cuda.get_device_properties(0).multi_processor_count
+    Hkv, n = 8, 4096
+    B = max(1, ctas // Hkv)                                # about a segment to every CTA
+    rows = 16 if D == 128 else 32
+    g = torch.Generator(device="cuda").manual_seed(G)
+    k = torch.zeros(1, Hkv, n, D, dtype=torch.bfloat16, device="cuda")
+    v = ((torch.rand(1, Hkv, n, D, generator=g, device="cuda") + 1) * 2.0 ** -11).bfloat16()
+    for t in range(4):
+        v[:, :, t * rows] = 2.0 ** 14
+        v[:, :, n - (t + 1) * rows] = -2.0 ** 14
+    q = torch.randn(B, Hkv * G, D, generator=g, device="cuda").bfloat16()
+    out, _ = attend(Hkv, D, q, k, v, n, None, batch_table=torch.zeros(B, 1, dtype=torch.int32, device="cuda"))
+    want = v[0].double().mean(1)[None, :, None].expand(B, Hkv, G, D).reshape(B, Hkv * G, D)
+    tol = (6 * (n / rows / 12) ** 0.5 * 2.0 ** -9 + 8 * 2.0 ** -9) / n + 2.0 ** -8 * want.abs()
+    worst = float(((out.double() - want).abs() / tol).max())
+    assert worst <= 1, worst
+    assert n / rows * 2.0 ** -10 / n > float(tol.max())     # what a drift would add is more than is allowed
