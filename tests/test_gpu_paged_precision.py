@@ -89,3 +89,65 @@ def test_long_sums_do_not_drift(D, G):
     worst = float(((out.double() - want).abs() / tol).max())
     assert worst <= 1, worst
     assert n / rows * 2.0 ** -10 / n > float(tol.max())     # what a drift would add is more than is allowed
+
+
+U = 2.0 ** -24
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 4, 5, 8, 12, 16])
+@pytest.mark.parametrize("what", ["keys", "queries", "both"])
+def test_fp32_scores_keep_their_bits(what, D, G):
+    """fp32 scores of which 2^-15 and less is left when their large products cancel; lse of one row is that row's score.
+
+    keys: a (1 + g + e) - a (1 + g + e'), queries the same with the sides exchanged, e below 2^-15 in steps of 2^-23; both: (a + f) (c + g)
+    - (a + f) c - a (c + g) + a c = f g.  Products up to 1.1 in size, four at most: rounded or cut at 8 places, 8 * 4.4 u.
+    """
+    B, Hkv = 64, 2
+    g = torch.Generator(device="cuda").manual_seed(G)
+    rand = lambda *s: torch.rand(*s, generator=g, device="cuda", dtype=torch.float64)  # noqa: E731
+    bits = lambda x, n: torch.round(x * 2.0 ** n) * 2.0 ** -n  # noqa: E731
+    q = torch.zeros(B, Hkv, G, D, dtype=torch.float64, device="cuda")
+    k = torch.zeros(B, Hkv, 1, D, dtype=torch.float64, device="cuda")
+    at = int(torch.randint(0, D // 4, (1,), generator=g, device="cuda")) * 4
+    if what == "both":
+        f, s = bits(2.0 ** -9 * (1 + rand(B, Hkv, G) * 0.9), 16), bits(2.0 ** -8 * (1 + rand(B, Hkv, 1) * 0.9), 15)
+        for d, (x, y) in enumerate(((1 + f, 1 + s), (1 + f, -torch.ones_like(s)), (torch.ones_like(f), -1 - s), (torch.ones_like(f), torch.ones_like(s)))):
+            q[..., at + d], k[..., at + d] = x, y
+    else:
+        a, b = (q, k) if what == "keys" else (k, q)
+        a[..., at] = bits(0.9 + 0.2 * rand(*a.shape[:3]), 20)
+        a[..., at + 1] = -a[..., at]
+        b[..., at] = 1 + bits(2.0 ** -8 * (1 + rand(*b.shape[:3]) * 0.9), 15)
+        b[..., at + 1] = b[..., at]
+        b[..., at] += bits(2.0 ** -15 * rand(*b.shape[:3]), 23)
+        b[..., at + 1] += bits(2.0 ** -15 * rand(*b.shape[:3]), 23)
+    assert torch.equal(q.float().double(), q) and torch.equal(k.float().double(), k)
+    scale = 2.0 ** 15
+    v = torch.ones(B, Hkv, 8, D, device="cuda")
+    page = torch.zeros(B, Hkv, 8, D, device="cuda")
+    page[:, :, :1] = k.float()
+    _, lse = attend(Hkv, D, q.view(B, Hkv * G, D).float(), page, v, 1, scale)
+    want = ((q @ k.transpose(2, 3))[..., 0] * scale).view(B, Hkv * G)
+    tol = 8 * 4.4 * U * scale + 8 * U * want.abs()
+    worst = float(((lse.double() - want).abs() / tol).max())
+    assert worst <= 1, worst
+    assert float(want.abs().max()) > 4 * tol.max()          # what the parts below hold is well above the bound
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("G", [1, 4, 5, 8, 12, 16])
+def test_fp32_values_keep_their_bits(D, G):
+    """Two rows of equal scores whose values differ in their last bits alone: half that difference, to 8 u."""
+    B, Hkv, page = 16, 2, 8
+    g = torch.Generator(device="cuda").manual_seed(G)
+    k = torch.zeros(B, Hkv, page, D, device="cuda")
+    v = torch.zeros(B, Hkv, page, D, device="cuda")
+    v[:, :, :2] = 1 + torch.round(torch.rand(B, Hkv, 1, D, generator=g, device="cuda") * 2 ** 7) * 2.0 ** -15
+    v[:, :, :2] += torch.round(torch.rand(B, Hkv, 2, D, generator=g, device="cuda") * 2 ** 8) * 2.0 ** -23
+    v[:, :, 1].neg_()
+    q = torch.randn(B, Hkv * G, D, generator=g, device="cuda")
+    out, _ = attend(Hkv, D, q, k, v, 2, None)
+    want = (v[:, :, :2].double().sum(2) / 2)[:, :, None].expand(B, Hkv, G, D).reshape(B, Hkv * G, D)
+    assert float((out.double() - want).abs().max()) <= 8 * U
+    assert float(want.abs().max()) > 64 * U
