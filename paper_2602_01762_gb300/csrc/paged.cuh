@@ -57,7 +57,7 @@ struct AttendArgs {
     const void *q;                       // [B, Hq, D]
     void *out;                           // [B, Hq, D]
     float *lse;                          // [B, Hq] or null
-    float *scores;                       // [B, Hkv, table rows, G] base-2 scores, or null
+    float *scores;                       // base-2 scores (paged_scores.h), or null
     float2 *stat;                        // [B, Hq]: (maximum score, 1 / sum), with scores
     float *part;                         // two pieces per CTA
     int *counter;                        // [B * head tiles] tickets (left at zero)

@@ -16,6 +16,7 @@
 // join.  A large call costs some 8 us beside its bytes: 4 until the first rows arrive, the rest the
 // spread of the SMs' speeds (6% by their place on the chip) and the last join.
 #include "paged.cuh"
+#include "paged_scores.h"
 
 namespace prism {
 namespace {
@@ -140,7 +141,7 @@ template <int D_, int MODE> struct Bf16Tile {
                 if (scores) {
                     const int h = 8 * t + c;
                     float *to = scores + (long long)(base + g) * heads + h;
-                    if (h + 1 < heads && h < kHeads && !(heads & 1)) {
+                    if (h + 1 < heads && h < kHeads && score_pairs(scores, heads)) {
                         if (in0) *(float2 *)to = make_float2(s[t][0], s[t][1]);
                         if (in1) *(float2 *)(to + 8 * heads) = make_float2(s[t][2], s[t][3]);
                     } else {
@@ -873,8 +874,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
         const int kvh = p.h / tiles, h0 = (p.h % tiles) * H, n = head_count(p);
         const long long hq = first_head(p);
         state.reset();
-        float *scores = a.scores ? a.scores + ((long long)p.b * a.Hkv + kvh) * G * a.cache.table_pages * a.cache.page_size +
-                                       (long long)h0 * a.cache.table_pages * a.cache.page_size : nullptr;
+        float *scores = a.scores ? a.scores + score_place(p.b, kvh, h0, a.Hkv, G, (long long)a.cache.table_pages * a.cache.page_size) : nullptr;
         const int rows = p.rows();
         for (int t = warp; t * KT < rows; t += kPaWarps) {
             cp_wait_group<S - 2>();
@@ -1037,7 +1037,7 @@ __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel
         const int page = j < len ? a.cache.table[(long long)b * a.cache.table_pages + j / a.cache.page_size] : -1;
         if (u == r.u0) pdl_wait();
         if ((unsigned)page < (unsigned)a.cache.n_pages) {   // else past the rows, or reported by the attention
-            const float *s = a.scores + ((long long)b * a.Hkv + h) * G * cap;
+            const float *s = a.scores + score_place(b, h, 0, a.Hkv, G, cap);
             const float2 *st = a.stat + (long long)b * a.Hq + h * G;
             float *to = a.cache.weights + ((long long)page * a.Hkv + h) * a.cache.page_size + j % a.cache.page_size;
             float w = 0.f;
