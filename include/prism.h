@@ -483,10 +483,11 @@ prism_status prism_profile_tree(prism_ctx *ctx, int32_t batch, const int32_t *to
  * wait for nothing and can be captured into a CUDA graph.  Errors are returned
  * as above; prism_paged_error gives the message.  Device-only conditions set
  * the handle's own error word (prism_paged_status): a length outside the block
- * table or a row that does not fit it (cache bit; the length is clamped, the
- * row skipped), n_new outside [0, max_new] (clamped), a position outside the
- * rotation table (clamped), a block-table entry outside the pool (its rows
- * read as zeros, are not written, and the results are not to be used). */
+ * table (cache bit; attention and eviction clamp it, prism_paged_append stores no
+ * row of that sequence) or a new row that does not fit it (cache bit; not stored),
+ * n_new outside [0, max_new] (clamped), a position outside the rotation table
+ * (clamped), a block-table entry outside the pool (its rows read as zeros, are not
+ * written, and the results are not to be used). */
 
 /* n_q_heads = Hq, n_kv_heads = Hkv (Hq % Hkv == 0), head_dim = D (64 or 128),
  * dtype PRISM_BF16 or PRISM_F32 ("wtype": queries, keys, values, gains, cache).

@@ -184,8 +184,9 @@ __global__ void __launch_bounds__(kNrThreads, 5) norm_rope_kernel(NormRopeArgs a
     char *ko = APPEND ? nullptr : a.k_out.p + b * a.k_out.sb + i * a.k_out.st + sub * 16, *vo = nullptr;
     float *weight = nullptr;             // of the new row and KV head 0
     if (APPEND && live) {
-        const long long slot = (long long)a.cache.kv_len[b] + i;
-        if (slot < 0 || slot >= (long long)a.cache.table_pages * a.cache.page_size) {
+        const int len = a.cache.kv_len[b];
+        const long long slot = (long long)len + i;
+        if (len < 0 || slot >= (long long)a.cache.table_pages * a.cache.page_size) {   // no slot of a negative length is the row's
             set_err(a.err, kErrCache);
         } else {
             const int idx = (int)(slot / a.cache.page_size), off = (int)(slot - (long long)idx * a.cache.page_size);
