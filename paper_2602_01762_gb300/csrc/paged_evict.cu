@@ -184,6 +184,12 @@ __global__ void __launch_bounds__(kEvThreads) evict_select_kernel(EvictArgs a, i
     for (int j = rank * kEvThreads + tid; j < a.recent; j += cs * kEvThreads) kept[first + want + j] = len - a.recent + j;
 }
 
+__device__ __forceinline__ int ticket_release(int *counter) {
+    int n;
+    asm volatile("atom.add.release.gpu.global.s32 %0, [%1], 1;" : "=r"(n) : "l"(counter) : "memory");
+    return n;
+}
+
 // Copies the kept rows of K, V and the weights, kCpRows destination rows of one KV
 // head per warp: a lane each looks the rows up, then the warp moves them 512 bytes
 // at a time.  Rows that are kept whatever their weights (all of a sequence within
@@ -205,9 +211,11 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
     const int b = bh / a.Hkv, h = bh - b * a.Hkv, j0 = chunk * kCpRows, j = j0 + lane;
     const int len = paged_len(a.src, b, 0, nullptr);
     // The last CTA to come here sets the lengths at its end: dst's may be src's, which
-    // every warp has read by then.
+    // every warp has read by then.  The release orders those reads, the CTA's by the
+    // barrier, before its ticket; the fence at the end the tickets before the lengths.
     __syncthreads();
-    bool last = threadIdx.x == 0 && atomicAdd(a.counter, 1) == (int)gridDim.x - 1;
+    bool last = false;
+    if (threadIdx.x == 0) last = ticket_release(a.counter) == (int)gridDim.x - 1;
     const bool early = len <= a.budget || j0 + kCpRows <= a.sinks || j0 >= a.budget - a.recent;
     if (!(work && early)) pdl_wait();
     last = __any_sync(0xFFFFFFFFu, last);
@@ -248,6 +256,8 @@ __global__ void __launch_bounds__(kCpThreads) evict_copy_kernel(EvictArgs a, int
     }
     if (!last) return;
     pdl_wait();                          // the selection reads them too
+    __threadfence();
+    __syncwarp();                        // lane 0 has the ticket, every lane writes
     for (int i = lane; i < a.B; i += 32) a.dst.kv_len[i] = min(paged_len(a.src, i, 0, nullptr), a.budget);
     if (lane == 0) *a.counter = 0;
 }
