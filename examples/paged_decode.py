@@ -77,19 +77,15 @@ class Layer:
 
     def step(self):
         """One token of every sequence: x in, y out."""
-        if self.at not in self.graphs:                   # captured once per half of the pool
-            stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
-            stream.wait_stream(torch.cuda.current_stream())
-            lens = (self.kv_len.clone(), self.pos.clone())
-            with torch.cuda.stream(stream):              # warm-up: its row is written again by the first replay
-                self._step()
-                self.kv_len.copy_(lens[0])
-                self.pos.copy_(lens[1])
-            torch.cuda.current_stream().wait_stream(stream)
-            with torch.cuda.graph(graph, stream=stream):
-                self._step()
-            self.graphs[self.at] = graph
-        self.graphs[self.at].replay()
+        if self.at in self.graphs:
+            self.graphs[self.at].replay()
+            return self.y
+        self._step()                                     # a half's first token; the next ones replay what is captured here
+        stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+        stream.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.graph(graph, stream=stream):
+            self._step()
+        self.graphs[self.at] = graph
         return self.y
 
     def evict(self):
