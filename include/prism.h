@@ -507,7 +507,8 @@ typedef struct prism_paged prism_paged;
  * page * page_stride + h * head_stride + (slot % page_size) * row_stride of
  * k_pages and of v_pages, page = block_table[b, slot / page_size], followed by
  * the head's other dims.  Strides in elements, the same for K and V; bases and
- * strides multiples of 16 bytes.
+ * strides multiples of 16 bytes (that of a dimension of one element is not used,
+ * here and below).
  *   weights      fp32 [n_pages, Hkv, page_size], dense, or NULL: each row's
  *                accumulated attention weight
  *   block_table  int32 [batch, table_pages]; entries past a sequence's rows

@@ -71,8 +71,10 @@ struct Check {
         if (!ok && s == PRISM_OK) s = fail(p, st, "%s", what);
     }
     int es() const { return p->bf16 ? 2 : 4; }
-    HeadsView heads(const prism_heads &h, const char *name) {
-        const HeadsView v = {(char *)h.data, h.batch_stride * es(), h.row_stride * es(), h.head_stride * es()};
+    // The stride of a dimension of one element is not used, whatever it is.
+    long long stride(long long elements, int n) const { return n > 1 ? elements * es() : 0; }
+    HeadsView heads(const prism_heads &h, const prism_rows &r, int n_heads, const char *name) {
+        const HeadsView v = {(char *)h.data, stride(h.batch_stride, r.batch), stride(h.row_stride, r.max_new), stride(h.head_stride, n_heads)};
         if (s != PRISM_OK) return v;
         if (!v.p) s = fail(p, PRISM_ERR_INVALID_ARG, "%s is null", name);
         else if (misaligned(v.p) || ((v.sb | v.st | v.sh) & 15))
@@ -81,7 +83,7 @@ struct Check {
     }
     // An output: rows and heads of their own (a stride of 0 would have them written over each other).
     HeadsView out(const prism_heads &h, const prism_rows &r, int n_heads, const char *name) {
-        const HeadsView v = heads(h, name);
+        const HeadsView v = heads(h, r, n_heads, name);
         if (s == PRISM_OK && ((v.sb == 0 && r.batch > 1) || (v.st == 0 && r.max_new > 1) || (v.sh == 0 && n_heads > 1)))
             s = fail(p, PRISM_ERR_INVALID_ARG, "%s: an output stride is 0", name);
         return v;
@@ -92,8 +94,8 @@ struct Check {
             if (s == PRISM_OK) s = fail(p, PRISM_ERR_INVALID_ARG, "%s: null cache, pages, block table or kv_len", name);
             return v;
         }
-        v = {(char *)c->k_pages, (char *)c->v_pages, c->page_stride * es(), c->head_stride * es(), c->row_stride * es(),
-             c->weights, c->block_table, c->kv_len, c->n_pages, c->table_pages, p->cfg.page_size};
+        v = {(char *)c->k_pages, (char *)c->v_pages, stride(c->page_stride, c->n_pages), stride(c->head_stride, p->cfg.n_kv_heads),
+             stride(c->row_stride, p->cfg.page_size), c->weights, c->block_table, c->kv_len, c->n_pages, c->table_pages, p->cfg.page_size};
         if (s != PRISM_OK) return v;
         if (misaligned(c->k_pages) || misaligned(c->v_pages) || ((v.page_stride | v.head_stride | v.row_stride) & 15))
             s = fail(p, PRISM_ERR_INVALID_ARG, "%s: bases and strides must be multiples of 16 bytes", name);
@@ -111,8 +113,8 @@ struct Check {
     // What the forward, the append and the gradient have in common.
     template <typename A> A rows(const prism_rows &r) {
         A a{};
-        a.q = heads(r.q, "q");
-        a.k = heads(r.k, "k");
+        a.q = heads(r.q, r, p->cfg.n_q_heads, "q");
+        a.k = heads(r.k, r, p->cfg.n_kv_heads, "k");
         a.g_q = r.g_q, a.g_k = r.g_k, a.rope = r.rope, a.pos = r.pos, a.n_new = r.n_new, a.rope_len = r.rope_len;
         a.B = r.batch, a.max_new = r.max_new, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.eps = p->cfg.rms_eps, a.err = p->err;
         need(r.batch >= 1 && r.max_new >= 1, PRISM_ERR_SHAPE, "batch and max_new must be at least 1");
@@ -230,8 +232,8 @@ prism_status prism_qk_norm_rope_backward(prism_paged *p, const prism_rows *rows,
     if (!p || !rows || !grads) return fail(p, PRISM_ERR_INVALID_ARG, "prism_qk_norm_rope_backward: null argument");
     Check c{p};
     NormRopeGradArgs a = c.rows<NormRopeGradArgs>(*rows);
-    a.dq_out = c.heads(grads->dq_out, "dq_out");
-    a.dk_out = c.heads(grads->dk_out, "dk_out");
+    a.dq_out = c.heads(grads->dq_out, *rows, p->cfg.n_q_heads, "dq_out");
+    a.dk_out = c.heads(grads->dk_out, *rows, p->cfg.n_kv_heads, "dk_out");
     a.dq = c.out(grads->dq, *rows, p->cfg.n_q_heads, "dq");
     a.dk = c.out(grads->dk, *rows, p->cfg.n_kv_heads, "dk");
     a.dg_q = grads->dg_q, a.dg_k = grads->dg_k, a.part = p->grad_part, a.counter = p->grad_ticket();
@@ -248,7 +250,7 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
     Check c{p};
     NormRopeArgs a = c.rows<NormRopeArgs>(*rows);
     a.cache = c.cache(cache, "cache");
-    a.v = c.heads(rows->v, "v");
+    a.v = c.heads(rows->v, *rows, p->cfg.n_kv_heads, "v");
     a.q_out = c.out(rows->q_out, *rows, p->cfg.n_q_heads, "q_out");
     if (c.s != PRISM_OK) return c.s;
     c.need(rows->batch == cache->batch, PRISM_ERR_SHAPE, "the rows and the cache differ in batch");

@@ -182,16 +182,17 @@ class PagedAttention:
     # ------------------------------------------------------------ calls
     def cache(self, k_pages, v_pages, block_table, kv_len, weights=None) -> PagedCache:
         """Bind a paged cache.  ``k_pages``, ``v_pages`` [n_pages, Hkv, page_size,
-        D], with any equal strides but a dense D (a permuted view of [n_pages,
-        page_size, Hkv, D] storage will do); ``block_table`` int32 [batch, pages];
-        ``kv_len`` int32 [batch]; ``weights`` fp32 [n_pages, Hkv, page_size]."""
+        D], dense in D, with the same strides otherwise (a permuted view of [n_pages,
+        page_size, Hkv, D] storage will do; dimensions of one element do not count);
+        ``block_table`` int32 [batch, pages]; ``kv_len`` int32 [batch]; ``weights``
+        fp32 [n_pages, Hkv, page_size]."""
         n_pages = k_pages.shape[0]
         shape = (n_pages, self.n_kv_heads, self.page_size, self.head_dim)
         for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
             if t.dtype is not self.tdtype or t.shape != shape or t.device != self.device:
                 raise ValueError(f"{name}: expected {self.tdtype} {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} "
                                  f"on {t.device}")
-            if t.stride() != k_pages.stride() or t.stride(3) != 1:
+            if t.stride(3) != 1 or any(a != b for n, a, b in zip(shape, t.stride(), k_pages.stride()) if n > 1):
                 raise ValueError(f"{name}: K and V need the same strides and a dense head dimension")
         if block_table.dim() != 2:
             raise ValueError("block_table: expected two dimensions")
