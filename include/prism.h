@@ -580,7 +580,8 @@ prism_status prism_qk_norm_rope_backward(prism_paged *p, const prism_rows *rows,
 
 /* The same norm and rotation with the keys, and the values as they are, stored
  * into the cache: row i < n_new[b] of sequence b goes to slot kv_len[b] + i, its
- * weight (if the cache has weights) starts at 0.  kv_len is read, not advanced.
+ * weight (if the cache has weights) starts at 0 and grows with prism_paged_attend
+ * alone: a prompt's rows weigh the same until then.  kv_len is read, not advanced.
  * pos NULL: rows stand at their slots (after an eviction they no longer do).
  * Errors: as prism_qk_norm_rope, CAPACITY (batch or table beyond the handle). */
 prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, const prism_rows *rows, void *stream);
@@ -591,10 +592,14 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
  * given lse fp32 [batch, Hq], the natural log of the sum of exponentials.  A
  * sequence without rows gives zeros and -inf.  If the cache has weights, each
  * row's grows by the sum of its probabilities over the KV head's query heads
- * (needs track_weights).  Scores, probabilities and sums are fp32; the result
+ * (needs track_weights).  Scores, probabilities and sums keep fp32's 24 bits: bf16
+ * products are exact and probabilities enter the product with V as three bf16 parts;
+ * in fp32 with 5 query heads to a KV head or more every value does, products of
+ * parts below 2^-24 of a whole one left out.  The result
  * does not depend on the order in which CTAs run.  A score of -inf drops its row, NaN
- * or +inf makes its head NaN; an infinite value in V makes that dim of its KV head's
- * outputs infinite or NaN.  Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
+ * or +inf makes its head NaN, and with it the weights of the sequence's rows of that
+ * KV head, for good (no error bit tells); an infinite value in V makes that dim of its
+ * KV head's outputs infinite or NaN.  Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
 prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,
                                 float *lse, void *stream);
 

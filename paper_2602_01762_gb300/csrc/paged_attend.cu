@@ -6,15 +6,18 @@
 // heads h of each KV head; optionally lse_h = log sum_j exp(z_j), and the
 // accumulated weights w_j += sum_h p_j that eviction ranks by.
 //
-// Bound by the bytes of K and V, read once: 4 D bytes per row and KV head in bf16
-// against 4 G D operations (G a byte: far below what the tensor cores' warp-level
-// products give at N = 8 or 16, too few columns for a 128-row tensor-memory tile).
-// Measured, bf16, D = 128: 64 sequences of 6001 to 16384 rows, G = 8, 425 us (6.9
-// TB/s, the rate of a plain copy); one of 131071 rows, G = 4, 84 us (6.4 TB/s); 8
-// multi-head ones of 2048 to 4096 rows 65 us (6.2); 16 of 1 to 8192 rows with weights
-// 52 us (5.2); one of 517 rows 5.8 us, a chain of length, table and row loads and the
-// join.  A large call costs some 8 us beside its bytes: 4 until the first rows arrive, the rest the
-// spread of the SMs' speeds (6% by their place on the chip) and the last join.
+// Bound by the bytes of K and V, read once up to G = 16 (more query heads read them
+// once for every 16, fp32 tables of few rows once for every 8): 4 D bytes per row and
+// KV head in bf16 against 4 G D operations (G a byte: far below what the tensor cores'
+// warp-level products give at N = 8 or 16, too few columns for a 128-row tensor-memory
+// tile).  Measured, bf16, D = 128: 64 sequences of 6001 to 16384 rows, G = 8, 427 to 433
+// us (6.8 TB/s, the rate of a plain copy); one of 131071 rows, G = 4, 85 us (6.3 TB/s);
+// 8 multi-head ones of 2048 to 4096 rows 65 us (6.2); 16 of 1 to 8192 rows with weights
+// 53 us (5.2); one of 517 rows 5.9 us, a chain of length, table and row loads and the
+// join; 16 of 56800 rows with one KV head, G = 16, 90 us (5.2); the same of D = 64, G = 32,
+// 95 us (4.9 TB/s of rows read twice).  fp32: one of 131071 rows, G = 4, 160 us (6.7
+// TB/s).  A large call costs some 8 us beside its bytes: 4 until the first rows arrive,
+// the rest the spread of the SMs' speeds (6% by their place on the chip) and the last join.
 #include "paged.cuh"
 #include "paged_scores.h"
 
@@ -380,10 +383,10 @@ template <int D_> struct F32Tile {
 // tile's O is added by the CUDA cores.  Which dim is which k (and which row of O^T)
 // is free: a lane's 16 bytes of a row are four of them, and no value is moved.
 // Measured, D = 128, 16 sequences of one KV head: 8 query heads, 40000 to 60000 rows,
-// 143 us (5.7 TB/s; on the CUDA cores 170); 16 query heads, 56800 rows, 224 us (4.2
+// 146 us (5.6 TB/s; on the CUDA cores 170); 16 query heads, 56800 rows, 226 us (4.1
 // TB/s; in two passes of 8 heads 304, on the CUDA cores 374).  What bounds the latter is
-// a warp's chain of some 1000 instructions to 8 rows with 8 warps an SM, which its 250
-// registers allow, not the tensor pipe (33%).
+// a warp's chain of some 1000 instructions to 8 rows with 8 warps an SM, which its 255
+// registers (and 52 bytes of spills) allow, not the tensor pipe (33%).
 template <int D_, int NT> struct F32Mma {
     using T = float;
     static constexpr int D = D_, KT = kPaStage / (8 * D);
@@ -838,6 +841,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     Place next0 = look_up(), next1 = look_up();
     int stage_in = 0;
     // K and V leave L2 first, so that scores, weights and pieces stay for the next reader
+    // (up to 16 query heads a KV head read them once; the next head tile of more reads them again)
     const uint64_t once = l2_evict_first_policy();
     auto issue = [&]() {
         if (next0.live) {
@@ -1012,8 +1016,8 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 // weights[j] += sum_h 2^(s_jh - M_h) / L_h from the scores the attention kernel
 // left, heads in order; one row of a KV head per thread.  V: float4 of scores per
 // row (0: any group).  One row a thread and eight CTAs an SM beat two or four rows
-// and fewer CTAs (16 sequences of up to 8192 rows, both kernels: 52.1, 52.3 and 53.3
-// us): what bounds it is the chain of a row's loads, not their bytes.
+// and fewer CTAs (16 sequences of up to 8192 rows, both kernels, before the attention
+// kept P in three parts: 52.1, 52.3 and 53.3 us): what bounds it is the chain of a row's loads, not their bytes.
 constexpr int kWtThreads = 256;
 constexpr int kWtCtasPerSm = 8;
 template <int V>
@@ -1111,11 +1115,12 @@ cudaError_t prepare_attend_kernels() {
 // CTAs of a cluster per segment, or 1: the shares of a persistent grid.  Clusters
 // where all of them run at once and a table's rows are few for each CTA: at most
 // `rows` (bf16 at D = 128: 512, with 9 to 16 query heads 1024; fp32 128,
-// with 5 to 16 query heads 256).  Measured, 8 KV
+// with 5 to 16 query heads 256).  The rows are the table's, all that a launch knows: a
+// table far wider than its sequences takes the shares.  Measured, 8 KV
 // heads of 128 and 4 query heads each, cluster against shares: one sequence of 100
-// rows 4.7 and 6.6 us, of 1000 5.9 and 8.0, of 4000 9.8 and 9.8; four of 4000 15.0 and
-// 17.3; fp32 of 1000 rows 7.7 and 8.8, of 2000 11.1 and 9.8; 4 KV heads with 16 query
-// heads each, 4000 rows 11.7 and 19.0.
+// rows 4.8 and 6.6 us, of 1000 5.9 and 8.0, of 4000 10.1 and 10.1; four of 4000 14.8 and
+// 17.3; fp32 of 1000 rows 7.8 and 8.7, of 2000 11.2 and 9.7; 4 KV heads with 16 query
+// heads each, 1000 rows 7.6 and 14.3, 4000 rows 13.0 and 18.9.
 static int attend_cluster(long long segments, long long cap, int rows, int sms) {
     int cs = 1;
     while (cs < 8 && cs * (long long)kAttendUnit < cap && 2 * cs * segments <= attend_ctas(sms)) cs *= 2;

@@ -9,7 +9,7 @@
 // Bound by the kept rows' bytes, read once and written once: the selection reads 4
 // bytes a row and KV head, the copy moves 8 D in bf16.  Two kernels, since the copy
 // wants every SM whatever the number of (sequence, KV head) pairs.  Measured: 16
-// sequences of 3900 to 4351 rows and 8 KV heads cut to 4096, 86 us (6.3 TB/s; 79.5 at
+// sequences of 3900 to 4351 rows and 8 KV heads cut to 4096, 87 us (6.2 TB/s; 79.5 at
 // the rate of a plain copy); one of 65537 rows cut to 4096, 23 us, of which 15 are the
 // selection's chain of loads, four passes and cluster barriers.
 #include "paged.cuh"

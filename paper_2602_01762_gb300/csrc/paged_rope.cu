@@ -276,7 +276,7 @@ __global__ void __launch_bounds__(kNrThreads, 5) norm_rope_kernel(NormRopeArgs a
 // Persistent CTAs, one per SM; each warp walks over its rows' head groups with a
 // ring of kNgRing groups requested ahead by cp.async, across rows.  What holds it at
 // 5 TB/s is the latency of some 300 instructions a group at 12 warps an SM: the sums of
-// dg, the rotation and the data take up to 168 registers (16 warps of 128 spill: 145
+// dg, the rotation and the data take up to 142 registers (16 warps of 128 spill: 145
 // against 137 us with the forward; a ring of 7 instead of 5 leaves too little L1: 140).
 constexpr int kNgThreads = 384;
 constexpr int kNgRing = 5;

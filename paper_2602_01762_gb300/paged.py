@@ -22,7 +22,9 @@ and, when the cache has grown past its budget,
 
 As in the rest of the package the binding only checks and marshals: every
 result is computed by the library's kernels on the current CUDA stream, and a
-missing library raises.  Tensors belong to the caller; a call that uses a tensor
+missing library raises.  Autograd records none of them: outputs carry no history,
+also of inputs that require a gradient, and the norm's gradient is the call named
+above.  Tensors belong to the caller; a call that uses a tensor
 on another stream than the one it was allocated on needs the caller's
 ``record_stream``, as with any asynchronous torch operation.
 """
