@@ -474,8 +474,9 @@ prism_status prism_profile_tree(prism_ctx *ctx, int32_t batch, const int32_t *to
 /* ------------------------------------------------------------------------
  * Operators over a paged key-value cache: the per-head norm of queries and
  * keys with the position rotation (stored into the cache, or dense with its
- * gradient), the attention of one new token, and eviction by accumulated
- * attention weight.  They need no prism_ctx.
+ * gradient), the attention of one new token, to every row or to a sliding window,
+ * and eviction by accumulated attention weight; and over a cache held in 8 bits.
+ * They need no prism_ctx.
  *
  * A handle fixes the head layout, the type and the page size, and owns the
  * workspace.  One handle's calls share that workspace: keep them on one stream
@@ -602,6 +603,67 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
  * KV head's outputs infinite or NaN.  Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
 prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,
                                 float *lse, void *stream);
+
+/* The same over the rows j < sinks and j >= L - window of the L = kv_len[b] + added
+ * (window >= 0, sinks >= 0; window < 0: every row, as prism_paged_attend): a sliding
+ * window and a few first rows that stay visible.  Rows that are not seen are not
+ * read, their weights stay as they are, and the block-table entries of pages without
+ * a seen row are not read: those pages may belong to another sequence.  No seen row
+ * gives zeros and -inf.  Errors: as prism_paged_attend. */
+prism_status prism_paged_attend_window(prism_paged *p, const prism_paged_cache *cache, int32_t added, int32_t window, int32_t sinks,
+                                       const void *q, void *out, float *lse, void *stream);
+
+/* A cache held in 8 bits: k_pages and v_pages hold codes, one byte each (strides in
+ * bytes, multiples of 16), and each block of scale_rows rows of a page and KV head
+ * has an fp32 scale for K and one for V: a row's value is its code times its block's
+ * scale.  scale_rows divides page_size: 1 (a scale a row) to page_size (a scale a
+ * page and head).  Scales are 0 or normal positive numbers (any, if the rows were
+ * written by another program), or NaN, which makes the block's rows NaN.  Such a cache
+ * has no weights.
+ *   k_scales, v_scales   fp32 [n_pages, Hkv, page_size / scale_rows], dense
+ *   format               PRISM_E4M3 (finite values up to 448, and NaN) or PRISM_INT8
+ *                        (-127 .. 127)
+ * A handle serves such caches beside those of its own type; q, k, v and results stay
+ * wtype. */
+typedef enum { PRISM_E4M3 = 0, PRISM_INT8 = 1 } prism_code_format;
+typedef struct {
+    float *k_scales, *v_scales;
+    int32_t format, scale_rows;
+} prism_paged_scales;
+
+/* prism_paged_append to a cache held in 8 bits: queries are normed and rotated as
+ * there; keys, normed and rotated, and values are quantised from fp32 in one rounding
+ * (ties to even).  A block's scale becomes the smallest power of two, not below
+ * 2^-126, that keeps the new rows' largest magnitude within the codes' range (0 for
+ * rows of zeros), or stays what the block's earlier rows have if that is larger; where
+ * it grows the earlier rows' codes are rounded again in the new scale, at most half a
+ * step of it.  A block whose first row is new starts afresh.  NaN and infinities do
+ * not count for the scale: in e4m3 they are stored as NaN, in int8, which has no code
+ * for them, they make the scale, and so the block's rows, NaN until it starts afresh.
+ * Blocks that receive rows belong to one sequence.  Errors: as prism_paged_append. */
+prism_status prism_paged_append_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales,
+                                      const prism_rows *rows, void *stream);
+
+/* Rows of such a cache read back: row start[b] + i, i < n_rows[b], of sequence b goes
+ * to row i of k_out and v_out, wtype [batch, max_rows, Hkv, D] (code times scale,
+ * rounded once); rows past n_rows[b] are left as they are.  Rows beyond kv_len are
+ * read as any other.  A row outside the block table is written as zeros (cache bit),
+ * as is one of a page outside the pool.
+ *   start    int32 [batch], or NULL: 0
+ *   n_rows   int32 [batch] in [0, max_rows] (n_new bit outside; clamped), or NULL:
+ *            max_rows each
+ * Errors: INVALID_ARG, SHAPE, CAPACITY (more than 2^24 rows), CUDA. */
+prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales,
+                                    const int32_t *start, const int32_t *n_rows, int32_t max_rows, const prism_heads *k_out,
+                                    const prism_heads *v_out, void *stream);
+
+/* prism_paged_attend_window over such a cache.  Codes enter their products exactly,
+ * the scales outside of them in fp32; bf16 queries keep their 8 bits, fp32 queries,
+ * and probabilities times V's scale, 22 bits (two fp16 parts), sums 24.  A key that is
+ * NaN makes its KV head's results NaN; a value, that dim of them.  Errors: as
+ * prism_paged_attend. */
+prism_status prism_paged_attend_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales, int32_t added,
+                                      int32_t window, int32_t sinks, const void *q, void *out, float *lse, void *stream);
 
 /* Eviction: of the L = kv_len[b] rows of every sequence and KV head, the
  * min(L, budget) rows to keep go, in order, to slots 0, 1, ... of dst: the first

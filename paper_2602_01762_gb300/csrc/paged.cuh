@@ -11,6 +11,8 @@ enum PagedErr : int {
     kErrPosition = 32,  // a rotary position outside the table
 };
 
+enum CodeFormat : int { kE4m3 = 0, kInt8 = 1 };
+
 // A paged cache on the device.  Strides in bytes; row `slot` of sequence b and
 // KV head h lies in page table[b, slot / page_size] at row slot % page_size.
 struct PagedView {
@@ -65,6 +67,34 @@ struct AttendArgs {
     int B, Hq, Hkv, added;
     int cluster;                         // CTAs of a cluster per segment; 1: a persistent grid (set by the launch)
     float scale_log2;                    // softmax scale * log2(e)
+    int window, sinks;                   // window < 0: every row is seen
+    const float *k_scales, *v_scales;    // 8-bit caches: [n_pages, Hkv, scale_blocks]
+    int scale_rows, scale_blocks;        // rows of a block; blocks of a page
+    int *err;
+};
+
+// Rows quantised into a cache of codes; the first and last row of a cache read back.
+struct StoreCodesArgs {
+    HeadsView k, v;
+    PagedView cache;
+    float *k_scales, *v_scales;          // [n_pages, Hkv, scale_blocks]
+    int scale_rows, scale_blocks;
+    const void *g_k;                     // [D] wtype, or null: no norm
+    const float *rope;
+    const int32_t *pos, *n_new;
+    int rope_len, B, max_new, Hkv;
+    int team, per, tasks;                // see store_codes_kernel
+    float eps;
+    int *err;
+};
+
+struct ReadCodesArgs {
+    HeadsView k_out, v_out;
+    PagedView cache;
+    const float *k_scales, *v_scales;
+    int scale_rows, scale_blocks;
+    const int32_t *start, *n_rows;       // [B]; null: 0, max_rows
+    int B, max_rows, Hkv;
     int *err;
 };
 
@@ -78,18 +108,31 @@ struct EvictArgs {
 
 constexpr int kAttendUnit = 64;          // keys per unit of the attention's work split
 constexpr int kAttendCost = 1;           // units that a segment costs beside its keys
-// The most passes over a KV head's rows that its G query heads take.
+// Query heads that share a pass over the rows; the most passes over a KV head's rows
+// that its G query heads take.
+inline int attend_head_tile(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
 int attend_head_tiles(int G);
 size_t attend_part_floats(int D, int G, int sms);
 int attend_ctas(int sms);
 // Kernel attributes, before any capture.
-cudaError_t prepare_attend_kernels();
+cudaError_t prepare_attend_kernels(bool bf16, int D, int G);
+cudaError_t prepare_window_attend_kernels(bool bf16, int D, int G);
+cudaError_t prepare_code_attend_kernels(bool bf16, int D, int G);
 cudaError_t prepare_evict_kernels();
 cudaError_t prepare_rope_kernels();
 cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+// The attention's first kernel: over a window (ht: heads of a tile), over codes.
+cudaError_t start_window_attend(const AttendArgs &a, bool bf16, int D, int ht, int sms, cudaStream_t s);
+cudaError_t prepare_e4m3_attend(bool bf16, int D, int G);
+cudaError_t prepare_int8_attend(bool bf16, int D, int G);
+cudaError_t start_e4m3_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t start_int8_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t launch_code_attend(const AttendArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
 int norm_rope_grad_ctas(int sms);
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t launch_store_codes(const StoreCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, cudaStream_t s);
 cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s);
 
 // Launch in clusters of cs CTAs, with programmatic stream serialization.
@@ -130,6 +173,11 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
 __device__ __forceinline__ void cp16_once(uint32_t dst, const void *src, bool ok, uint64_t policy) {
     const int n = ok ? 16 : 0;
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(n), "l"(policy) : "memory");
+}
+// 4 bytes.
+__device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool ok) {
+    const int n = ok ? 4 : 0;
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
 }
 __device__ __forceinline__ void cp_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void cp_wait_group() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }

@@ -88,7 +88,9 @@ struct Check {
             s = fail(p, PRISM_ERR_INVALID_ARG, "%s: an output stride is 0", name);
         return v;
     }
-    PagedView cache(const prism_paged_cache *c, const char *name) {
+    PagedView cache(const prism_paged_cache *c, const char *name, bool codes = false) {
+        const int es = codes ? 1 : this->es();
+        auto stride = [&](long long elements, int n) { return n > 1 ? elements * es : 0; };
         PagedView v{};
         if (!c || !c->k_pages || !c->v_pages || !c->block_table || !c->kv_len) {
             if (s == PRISM_OK) s = fail(p, PRISM_ERR_INVALID_ARG, "%s: null cache, pages, block table or kv_len", name);
@@ -109,6 +111,33 @@ struct Check {
             s = fail(p, PRISM_ERR_CAPACITY, "%s: batch %d and %d pages a sequence exceed the handle's %d and %d", name, c->batch,
                      c->table_pages, p->cfg.max_batch, p->cfg.max_pages);
         return v;
+    }
+    // A cache held in 8 bits, its scales to `a`.
+    template <typename A> void codes(A &a, const prism_paged_cache *c, const prism_paged_scales *q) {
+        a.cache = cache(c, "cache", true);
+        need(q && q->k_scales && q->v_scales, PRISM_ERR_INVALID_ARG, "scales: null");
+        if (s != PRISM_OK) return;
+        need(q->format == PRISM_E4M3 || q->format == PRISM_INT8, PRISM_ERR_INVALID_ARG, "scales: format must be PRISM_E4M3 or PRISM_INT8");
+        need(q->scale_rows >= 1 && q->scale_rows <= p->cfg.page_size && p->cfg.page_size % q->scale_rows == 0, PRISM_ERR_SHAPE,
+             "scales: scale_rows must divide page_size");
+        need(!c->weights, PRISM_ERR_INVALID_ARG, "a cache held in 8 bits has no weights");
+        if (s != PRISM_OK) return;
+        a.k_scales = q->k_scales, a.v_scales = q->v_scales, a.scale_rows = q->scale_rows;
+        a.scale_blocks = p->cfg.page_size / q->scale_rows;
+    }
+    // An attention's arguments but its cache.
+    void attend(AttendArgs &a, const prism_paged_cache *c, int added, int window, int sinks, const void *q, void *out, float *lse) {
+        need(q && out, PRISM_ERR_INVALID_ARG, "q or out is null");
+        need(!misaligned(q) && !misaligned(out), PRISM_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
+        need(added >= 0, PRISM_ERR_INVALID_ARG, "added is negative");
+        need(sinks >= 0, PRISM_ERR_INVALID_ARG, "sinks is negative");
+        need(!a.cache.weights || p->scores, PRISM_ERR_INVALID_ARG, "the cache has weights: the handle needs track_weights");
+        if (s != PRISM_OK) return;
+        a.q = q, a.out = out, a.lse = lse;
+        if (a.cache.weights) a.scores = p->scores, a.stat = p->stat;
+        a.part = p->part, a.counter = p->counter, a.group_counter = p->counter + p->segments, a.err = p->err;
+        a.B = c->batch, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.added = added, a.window = window, a.sinks = sinks;
+        a.scale_log2 = (float)(p->cfg.softmax_scale * 1.4426950408889634);
     }
     // What the forward, the append and the gradient have in common.
     template <typename A> A rows(const prism_rows &r) {
@@ -159,14 +188,16 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
     OnDevice on(device);
     cudaError_t e = on.e;
     if (e == cudaSuccess) e = cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, device);
-    if (e == cudaSuccess) e = prepare_attend_kernels();
+    const int G = c.n_q_heads / c.n_kv_heads;
+    if (e == cudaSuccess) e = prepare_attend_kernels(p->bf16, c.head_dim, G);
+    if (e == cudaSuccess) e = prepare_window_attend_kernels(p->bf16, c.head_dim, G);
+    if (e == cudaSuccess) e = prepare_code_attend_kernels(p->bf16, c.head_dim, G);
     if (e == cudaSuccess) e = prepare_evict_kernels();
     if (e == cudaSuccess) e = prepare_rope_kernels();
     if (e != cudaSuccess) {
         delete p;
         return cuda_status(nullptr, e, "prism_paged_create");
     }
-    const int G = c.n_q_heads / c.n_kv_heads;
     p->segments = c.max_batch * c.n_kv_heads * attend_head_tiles(G);
     p->cta_tickets = 2 * attend_ctas(p->sms);
     size_t bytes = 0;
@@ -261,25 +292,83 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
     return cuda_status(p, launch_norm_rope(a, p->bf16, p->cfg.head_dim, true, p->sms, (cudaStream_t)stream), "prism_paged_append");
 }
 
+prism_status prism_paged_append_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales,
+                                      const prism_rows *rows, void *stream) {
+    if (!p || !rows) return fail(p, PRISM_ERR_INVALID_ARG, "prism_paged_append_codes: null argument");
+    Check c{p};
+    NormRopeArgs q = c.rows<NormRopeArgs>(*rows);
+    StoreCodesArgs a{};
+    c.codes(a, cache, scales);
+    a.k = q.k;
+    a.v = c.heads(rows->v, *rows, p->cfg.n_kv_heads, "v");
+    q.q_out = c.out(rows->q_out, *rows, p->cfg.n_q_heads, "q_out");
+    if (c.s != PRISM_OK) return c.s;
+    c.need(rows->batch == cache->batch, PRISM_ERR_SHAPE, "the rows and the cache differ in batch");
+    c.need(rows->batch * (((long long)rows->max_new + 2 * a.scale_rows) / a.scale_rows) * p->cfg.n_kv_heads <= (1LL << 28), PRISM_ERR_CAPACITY,
+           "batch * max_new * n_kv_heads is too large");
+    if (c.s != PRISM_OK) return c.s;
+    if (!q.pos) q.pos = cache->kv_len;
+    a.g_k = q.g_k, a.rope = q.rope, a.pos = q.pos, a.n_new = q.n_new, a.rope_len = q.rope_len, a.B = q.B, a.max_new = q.max_new, a.Hkv = q.Hkv;
+    a.eps = q.eps, a.err = p->err;
+    q.Hkv = 0;                                   // the queries alone
+    OnDevice on(p->device);
+    if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
+    cudaError_t e = launch_norm_rope(q, p->bf16, p->cfg.head_dim, false, p->sms, (cudaStream_t)stream);
+    if (e == cudaSuccess) e = launch_store_codes(a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream);
+    return cuda_status(p, e, "prism_paged_append_codes");
+}
+
+prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales,
+                                    const int32_t *start, const int32_t *n_rows, int32_t max_rows, const prism_heads *k_out,
+                                    const prism_heads *v_out, void *stream) {
+    if (!p || !k_out || !v_out) return fail(p, PRISM_ERR_INVALID_ARG, "prism_paged_read_codes: null argument");
+    Check c{p};
+    ReadCodesArgs a{};
+    c.codes(a, cache, scales);
+    c.need(max_rows >= 1, PRISM_ERR_SHAPE, "max_rows must be at least 1");
+    if (c.s != PRISM_OK) return c.s;
+    c.need((long long)cache->batch * max_rows <= (1LL << 24), PRISM_ERR_CAPACITY, "batch * max_rows exceeds 2^24 rows");
+    prism_rows shape{};
+    shape.batch = cache->batch, shape.max_new = max_rows;
+    a.k_out = c.out(*k_out, shape, p->cfg.n_kv_heads, "k_out");
+    a.v_out = c.out(*v_out, shape, p->cfg.n_kv_heads, "v_out");
+    if (c.s != PRISM_OK) return c.s;
+    a.start = start, a.n_rows = n_rows, a.B = cache->batch, a.max_rows = max_rows, a.Hkv = p->cfg.n_kv_heads, a.err = p->err;
+    OnDevice on(p->device);
+    if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
+    return cuda_status(p, launch_read_codes(a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, (cudaStream_t)stream), "prism_paged_read_codes");
+}
+
 prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,
                                 float *lse, void *stream) {
+    return prism_paged_attend_window(p, cache, added, -1, 0, q, out, lse, stream);
+}
+
+prism_status prism_paged_attend_window(prism_paged *p, const prism_paged_cache *cache, int32_t added, int32_t window, int32_t sinks,
+                                       const void *q, void *out, float *lse, void *stream) {
     if (!p) return fail(nullptr, PRISM_ERR_INVALID_ARG, "prism_paged_attend: null handle");
     Check c{p};
     AttendArgs a{};
     a.cache = c.cache(cache, "cache");
-    c.need(q && out, PRISM_ERR_INVALID_ARG, "q or out is null");
-    c.need(!misaligned(q) && !misaligned(out), PRISM_ERR_INVALID_ARG, "q and out must be 16-byte aligned");
-    c.need(added >= 0, PRISM_ERR_INVALID_ARG, "added is negative");
-    c.need(!a.cache.weights || p->scores, PRISM_ERR_INVALID_ARG, "the cache has weights: the handle needs track_weights");
+    c.attend(a, cache, added, window, sinks, q, out, lse);
     if (c.s != PRISM_OK) return c.s;
-    a.q = q, a.out = out, a.lse = lse;
-    if (a.cache.weights) a.scores = p->scores, a.stat = p->stat;
-    a.part = p->part, a.counter = p->counter, a.group_counter = p->counter + p->segments, a.err = p->err;
-    a.B = cache->batch, a.Hq = p->cfg.n_q_heads, a.Hkv = p->cfg.n_kv_heads, a.added = added;
-    a.scale_log2 = (float)(p->cfg.softmax_scale * 1.4426950408889634);
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
     return cuda_status(p, launch_paged_attend(a, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream), "prism_paged_attend");
+}
+
+prism_status prism_paged_attend_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales, int32_t added,
+                                      int32_t window, int32_t sinks, const void *q, void *out, float *lse, void *stream) {
+    if (!p) return fail(nullptr, PRISM_ERR_INVALID_ARG, "prism_paged_attend_codes: null handle");
+    Check c{p};
+    AttendArgs a{};
+    c.codes(a, cache, scales);
+    c.attend(a, cache, added, window, sinks, q, out, lse);
+    if (c.s != PRISM_OK) return c.s;
+    OnDevice on(p->device);
+    if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
+    return cuda_status(p, launch_code_attend(a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream),
+                       "prism_paged_attend_codes");
 }
 
 prism_status prism_paged_evict(prism_paged *p, const prism_paged_cache *src, const prism_paged_cache *dst, int32_t budget,

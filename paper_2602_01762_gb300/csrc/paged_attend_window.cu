@@ -1,0 +1,29 @@
+// The paged attention (paged_attend.cu) over a sliding window and a few first rows.
+//
+// Row j of L is seen where j < sinks or j >= L - window.  The blocks of 64 rows without
+// a seen row are not part of the work that is split, so that the cost goes by the
+// window, not by the sequence: rows that are not seen are not read, and neither are the
+// block-table entries of pages without a seen row, whose pages can be given back.
+#include "paged_attend_tiles.cuh"
+
+namespace prism {
+
+cudaError_t prepare_window_attend_kernels(bool bf16, int D, int G) { return prepare_attend_tiles<WindowRows>(bf16, D, G); }
+
+cudaError_t start_window_attend(const AttendArgs &a, bool bf16, int D, int ht, int sms, cudaStream_t s) {
+    return start_attend_tiles<WindowRows>(a, bf16, D, ht, sms, s);
+}
+
+cudaError_t prepare_code_attend_kernels(bool bf16, int D, int G) {
+    const cudaError_t e = prepare_e4m3_attend(bf16, D, G);
+    return e != cudaSuccess ? e : prepare_int8_attend(bf16, D, G);
+}
+
+// Codes have one form for both: without a window the window is every row.
+cudaError_t launch_code_attend(const AttendArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
+    AttendArgs a = args;
+    if (a.window < 0) a.window = 0x7FFFFFFF;
+    return format == kE4m3 ? start_e4m3_attend(a, bf16, D, sms, s) : start_int8_attend(a, bf16, D, sms, s);
+}
+
+}  // namespace prism

@@ -3,8 +3,9 @@
 rotation, stored into the cache (:meth:`PagedAttention.append`) or dense with
 its gradient (:meth:`PagedAttention.qk_norm_rope`,
 :meth:`PagedAttention.qk_norm_rope_backward`), the attention of one new token
-(:meth:`PagedAttention.attend`) and eviction by accumulated attention weight
-(:meth:`PagedAttention.evict`).
+(:meth:`PagedAttention.attend`), to every row or to a sliding window, eviction by
+accumulated attention weight (:meth:`PagedAttention.evict`), and rows of a cache held
+in 8 bits read back (:meth:`PagedAttention.read`).
 
 A decode step of one layer::
 
@@ -18,7 +19,13 @@ A decode step of one layer::
     kv_len += 1; pos += 1
 
 and, when the cache has grown past its budget,
-``att.evict(cache, other_cache, kept, sinks=4, recent=512)``.
+``att.evict(cache, other_cache, kept, sinks=4, recent=512)``.  Attention to the last
+rows and a few first ones alone is ``att.attend(..., window=1024, sinks=4)``.
+
+A cache held in 8 bits has pages of ``torch.float8_e4m3fn`` or ``torch.int8`` codes
+and a scale for each block of rows, ``att.cache(k_pages, v_pages, block_table, kv_len,
+k_scales=ks, v_scales=vs)``; ``append`` quantises into it, ``attend`` reads it as it is,
+``read`` gives rows back in the handle's type.
 
 As in the rest of the package the binding only checks and marshals: every
 result is computed by the library's kernels on the current CUDA stream, and a
@@ -52,9 +59,16 @@ class _Cache(ctypes.Structure):
                 ("batch", _i32)]
 
 
+class _Scales(ctypes.Structure):
+    _fields_ = [("k_scales", _vp), ("v_scales", _vp), ("format", _i32), ("scale_rows", _i32)]
+
+
+_CODES = {torch.float8_e4m3fn: 0, torch.int8: 1}
+
 # prism_rows (five strided tensors of four words, five addresses, three sizes) and
 # prism_row_grads (four strided tensors, two addresses)
 _ROWS, _GRADS = struct.Struct("=20q5Q3i4x"), struct.Struct("=16q2Q")
+_HEADS = struct.Struct("=4q")        # prism_heads
 _NONE = (0, 0, 0, 0)
 
 
@@ -69,11 +83,17 @@ def bind(lib: ctypes.CDLL) -> None:
     lib.prism_paged_append.argtypes = [_vp, C, _vp, _vp]
     lib.prism_paged_attend.argtypes = [_vp, C, _i32, _vp, _vp, _vp, _vp]
     lib.prism_paged_evict.argtypes = [_vp, C, C, _i32, _i32, _i32, _vp, _vp]
+    S = P(_Scales)
+    lib.prism_paged_attend_window.argtypes = [_vp, C, _i32, _i32, _i32, _vp, _vp, _vp, _vp]
+    lib.prism_paged_append_codes.argtypes = [_vp, C, S, _vp, _vp]
+    lib.prism_paged_read_codes.argtypes = [_vp, C, S, _vp, _vp, _i32, _vp, _vp, _vp]
+    lib.prism_paged_attend_codes.argtypes = [_vp, C, S, _i32, _i32, _i32, _vp, _vp, _vp, _vp]
     lib.prism_paged_status.argtypes = [_vp, _vp, P(_i32)]
     lib.prism_paged_error.argtypes = [_vp]
     lib.prism_paged_error.restype = ctypes.c_char_p
     for f in ("prism_paged_create", "prism_paged_destroy", "prism_qk_norm_rope", "prism_qk_norm_rope_backward",
-              "prism_paged_append", "prism_paged_attend", "prism_paged_evict", "prism_paged_status"):
+              "prism_paged_append", "prism_paged_attend", "prism_paged_evict", "prism_paged_status", "prism_paged_attend_window",
+              "prism_paged_append_codes", "prism_paged_read_codes", "prism_paged_attend_codes"):
         getattr(lib, f).restype = ctypes.c_int
 
 
@@ -87,10 +107,13 @@ def rope_table(positions: int, head_dim: int, theta: float = 10000.0, device=0) 
 
 class PagedCache:
     """A paged cache bound by :meth:`PagedAttention.cache`: its tensors, checked
-    once, and the struct the calls pass on."""
+    once, and the structs the calls pass on (``scales`` None: a cache of the handle's
+    own type)."""
 
-    def __init__(self, fields, tensors, batch, rows, dtype, device, heads):
+    def __init__(self, fields, tensors, batch, rows, dtype, device, heads, scales=None, k_scales=None, v_scales=None):
         self.fields, self.ref = fields, ctypes.byref(fields)
+        self.scales, self.k_scales, self.v_scales = scales, k_scales, v_scales
+        self.scales_ref = None if scales is None else ctypes.byref(scales)
         self.k_pages, self.v_pages, self.block_table, self.kv_len, self.weights = tensors
         self.batch, self.rows = batch, rows          # sequences; rows a block-table line holds
         self.key = (dtype, device, heads)
@@ -99,7 +122,8 @@ class PagedCache:
 class PagedAttention:
     """Paged-cache operators of one attention layout on one GPU.
 
-    ``dtype`` "bf16" or "f32" is that of queries, keys, values, gains and cache;
+    ``dtype`` "bf16" or "f32" is that of queries, keys, values, gains and cache (but
+    for one held in 8 bits);
     ``max_batch`` and ``max_pages`` bound the calls that take a cache;
     ``track_weights`` allots the workspace that accumulating attention weights
     needs; ``softmax_scale`` None means ``head_dim ** -0.5``.  A handle's calls
@@ -123,6 +147,8 @@ class PagedAttention:
         self.h = h
         self._index, self._dims = self.device.index, (head_dim,)
         self._rows, self._grads = ctypes.create_string_buffer(_ROWS.size), ctypes.create_string_buffer(_GRADS.size)
+        self._k_rows, self._v_rows = ctypes.create_string_buffer(_HEADS.size), ctypes.create_string_buffer(_HEADS.size)
+        self._k_rows_at, self._v_rows_at = ctypes.addressof(self._k_rows), ctypes.addressof(self._v_rows)
         self._rows_at, self._grads_at = ctypes.addressof(self._rows), ctypes.addressof(self._grads)
         self._key = (self.tdtype, self.device, (n_kv_heads, page_size, head_dim))
 
@@ -182,17 +208,35 @@ class PagedAttention:
         return cache.ref
 
     # ------------------------------------------------------------ calls
-    def cache(self, k_pages, v_pages, block_table, kv_len, weights=None) -> PagedCache:
+    def cache(self, k_pages, v_pages, block_table, kv_len, weights=None, k_scales=None, v_scales=None) -> PagedCache:
         """Bind a paged cache.  ``k_pages``, ``v_pages`` [n_pages, Hkv, page_size,
         D], dense in D, with the same strides otherwise (a permuted view of [n_pages,
         page_size, Hkv, D] storage will do; dimensions of one element do not count);
         ``block_table`` int32 [batch, pages]; ``kv_len`` int32 [batch]; ``weights``
-        fp32 [n_pages, Hkv, page_size]."""
+        fp32 [n_pages, Hkv, page_size].
+
+        With ``k_scales`` and ``v_scales``, fp32 [n_pages, Hkv, page_size / r], a cache
+        held in 8 bits: pages of ``torch.float8_e4m3fn`` or ``torch.int8``, a scale for
+        each r rows of a page and head (``prism_paged_scales``), no weights."""
         n_pages = k_pages.shape[0]
+        scales, dtype = None, self.tdtype
+        if (k_scales is None) != (v_scales is None):
+            raise ValueError("k_scales and v_scales are given together or not at all")
+        if k_scales is not None:
+            dtype = k_pages.dtype
+            if dtype not in _CODES:
+                raise ValueError(f"k_pages: expected torch.float8_e4m3fn or torch.int8 with scales, got {dtype}")
+            if weights is not None:
+                raise ValueError("a cache held in 8 bits has no weights")
+            if k_scales.dim() != 3 or k_scales.shape[2] < 1 or self.page_size % k_scales.shape[2]:
+                raise ValueError(f"k_scales: expected [n_pages, n_kv_heads, blocks], blocks a divisor of {self.page_size}")
+            blocks = (n_pages, self.n_kv_heads, k_scales.shape[2])
+            scales = _Scales(self._tensor(k_scales, blocks, torch.float32, "k_scales"), self._tensor(v_scales, blocks, torch.float32, "v_scales"),
+                             _CODES[dtype], self.page_size // blocks[2])
         shape = (n_pages, self.n_kv_heads, self.page_size, self.head_dim)
         for t, name in ((k_pages, "k_pages"), (v_pages, "v_pages")):
-            if t.dtype is not self.tdtype or t.shape != shape or t.device != self.device:
-                raise ValueError(f"{name}: expected {self.tdtype} {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} "
+            if t.dtype is not dtype or t.shape != shape or t.device != self.device:
+                raise ValueError(f"{name}: expected {dtype} {shape} on {self.device}, got {t.dtype} {tuple(t.shape)} "
                                  f"on {t.device}")
             if t.stride(3) != 1 or any(a != b for n, a, b in zip(shape, t.stride(), k_pages.stride()) if n > 1):
                 raise ValueError(f"{name}: K and V need the same strides and a dense head dimension")
@@ -207,7 +251,8 @@ class PagedAttention:
         fields = _Cache(k_pages.data_ptr(), v_pages.data_ptr(), s[0], s[1], s[2],
                         None if weights is None else weights.data_ptr(), block_table.data_ptr(), kv_len.data_ptr(),
                         n_pages, pages, batch)
-        return PagedCache(fields, (k_pages, v_pages, block_table, kv_len, weights), batch, pages * self.page_size, *self._key)
+        return PagedCache(fields, (k_pages, v_pages, block_table, kv_len, weights), batch, pages * self.page_size, *self._key,
+                          scales, k_scales, v_scales)
 
     def _shapes(self, B, n):
         return (B, n, self.n_q_heads, self.head_dim), (B, n, self.n_kv_heads, self.head_dim)
@@ -237,25 +282,65 @@ class PagedAttention:
     def append(self, cache, q, k, v, q_out, rope, g_q=None, g_k=None, pos=None, n_new=None, stream=None):
         """``prism_paged_append``: q, q_out [B, n, Hq, D]; k, v [B, n, Hkv, D].
         Rows i < n_new[b] go to slots kv_len[b] + i, at positions pos[b] + i (pos
-        None: their slots).  kv_len is not advanced."""
+        None: their slots).  kv_len is not advanced.  A cache held in 8 bits takes the
+        keys and values quantised (``prism_paged_append_codes``)."""
         ref = self._bound(cache)
         sq, sk = self._shapes(cache.batch, q.shape[1])
         self._pack(sq, sk, q, k, v, q_out, None, rope, pos, g_q, g_k, n_new)
-        self._check(self.lib.prism_paged_append(self.h, ref, self._rows_at, self._stream(stream)))
+        if cache.scales is not None:
+            self._check(self.lib.prism_paged_append_codes(self.h, ref, cache.scales_ref, self._rows_at, self._stream(stream)))
+        else:
+            self._check(self.lib.prism_paged_append(self.h, ref, self._rows_at, self._stream(stream)))
 
-    def attend(self, cache, q, out, lse=None, added=1, stream=None):
+    def attend(self, cache, q, out, lse=None, added=1, stream=None, window=None, sinks=0):
         """``prism_paged_attend``: q, out [B, Hq, D]; lse fp32 [B, Hq] or None;
-        over kv_len[b] + added rows.  A cache with weights accumulates them."""
+        over kv_len[b] + added rows; with ``window`` over the last ``window`` and the
+        first ``sinks`` of them (``prism_paged_attend_window``).  A cache with weights
+        accumulates them; one held in 8 bits is read as it is
+        (``prism_paged_attend_codes``)."""
         ref = self._bound(cache)
         shape = (cache.batch, self.n_q_heads, self.head_dim)
-        self._check(self.lib.prism_paged_attend(
-            self.h, ref, added, self._tensor(q, shape, self.tdtype, "q"), self._tensor(out, shape, self.tdtype, "out"),
-            None if lse is None else self._tensor(lse, shape[:2], torch.float32, "lse"), self._stream(stream)))
+        if window is None:
+            if sinks:
+                raise ValueError("sinks without a window")
+            window = -1
+        elif window < 0:
+            raise ValueError("window is negative")
+        window = min(window, 0x7FFFFFFF)
+        sinks = min(sinks, 0x7FFFFFFF)
+        args = (self._tensor(q, shape, self.tdtype, "q"), self._tensor(out, shape, self.tdtype, "out"),
+                None if lse is None else self._tensor(lse, shape[:2], torch.float32, "lse"), self._stream(stream))
+        if cache.scales is not None:
+            self._check(self.lib.prism_paged_attend_codes(self.h, ref, cache.scales_ref, added, window, sinks, *args))
+        elif window < 0:
+            self._check(self.lib.prism_paged_attend(self.h, ref, added, *args))
+        else:
+            self._check(self.lib.prism_paged_attend_window(self.h, ref, added, window, sinks, *args))
+
+    def read(self, cache, k_out, v_out, start=None, n_rows=None, stream=None):
+        """``prism_paged_read_codes``: rows start[b] + i, i < n_rows[b], of a cache held
+        in 8 bits, in the handle's type; k_out, v_out [B, n, Hkv, D] (strided but for
+        D); start, n_rows int32 [B] (None: 0 and n).  Rows past n_rows[b] keep what
+        they hold."""
+        ref = self._bound(cache)
+        if cache.scales is None:
+            raise ValueError("read: the cache is not held in 8 bits")
+        B, n = cache.batch, k_out.shape[1]
+        shape = (B, n, self.n_kv_heads, self.head_dim)
+        _HEADS.pack_into(self._k_rows, 0, *self._heads(k_out, shape, "k_out"))
+        _HEADS.pack_into(self._v_rows, 0, *self._heads(v_out, shape, "v_out"))
+        self._check(self.lib.prism_paged_read_codes(
+            self.h, ref, cache.scales_ref, None if start is None else self._tensor(start, (B,), torch.int32, "start"),
+            None if n_rows is None else self._tensor(n_rows, (B,), torch.int32, "n_rows"), n, self._k_rows_at, self._v_rows_at,
+            self._stream(stream)))
 
     def evict(self, src, dst, kept, sinks=0, recent=0, stream=None):
         """``prism_paged_evict``: the rows of ``src`` to keep go, in order, to the
-        pages of ``dst``; ``kept`` int32 [B, Hkv, budget] receives their slots."""
+        pages of ``dst``; ``kept`` int32 [B, Hkv, budget] receives their slots.  Not
+        for caches held in 8 bits, which have no weights."""
         rs, rd = self._bound(src), self._bound(dst)
+        if src.scales is not None or dst.scales is not None:
+            raise ValueError("evict: caches held in 8 bits are not evicted from")
         if kept.dim() != 3:
             raise ValueError("kept: expected three dimensions")
         budget = kept.shape[2]
