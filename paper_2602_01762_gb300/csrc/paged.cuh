@@ -11,6 +11,20 @@ enum PagedErr : int {
     kErrPosition = 32,  // a rotary position outside the table
 };
 
+// Division of n < 2^31 by a divisor that the launch knows: floor(n / d) = (floor(n m / 2^32)
+// + n) / 2^s with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1.
+struct Divisor {
+    uint32_t d, m, s;
+    Divisor() = default;
+    explicit Divisor(uint32_t by) : d(by), m(0), s(0) {
+        while (s < 31 && (1u << s) < d) ++s;
+        m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
+    }
+#ifdef __CUDACC__
+    __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
+#endif
+};
+
 enum CodeFormat : int { kE4m3 = 0, kInt8 = 1 };
 
 // A paged cache on the device.  Strides in bytes; row `slot` of sequence b and
@@ -70,6 +84,7 @@ struct AttendArgs {
     int window, sinks;                   // window < 0: every row is seen
     const float *k_scales, *v_scales;    // 8-bit caches: [n_pages, Hkv, scale_blocks]
     int scale_rows, scale_blocks;        // rows of a block; blocks of a page
+    Divisor by_page, by_scale;           // 8-bit caches: by page_size, by scale_rows
     int *err;
 };
 
@@ -113,7 +128,7 @@ constexpr int kAttendCost = 1;           // units that a segment costs beside it
 inline int attend_head_tile(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }
 int attend_head_tiles(int G);
 size_t attend_part_floats(int D, int G, int sms);
-int attend_ctas(int sms);
+constexpr int kAttendMaxCtas = 3;        // CTAs an SM of any of its kernels
 // Kernel attributes, before any capture.
 cudaError_t prepare_attend_kernels(bool bf16, int D, int G);
 cudaError_t prepare_window_attend_kernels(bool bf16, int D, int G);

@@ -199,7 +199,7 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
         return cuda_status(nullptr, e, "prism_paged_create");
     }
     p->segments = c.max_batch * c.n_kv_heads * attend_head_tiles(G);
-    p->cta_tickets = 2 * attend_ctas(p->sms);
+    p->cta_tickets = 2 * kAttendMaxCtas * p->sms;
     size_t bytes = 0;
     auto take = [&](size_t n) {
         const size_t at = bytes;

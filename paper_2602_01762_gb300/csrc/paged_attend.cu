@@ -90,10 +90,8 @@ __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel
 
 int attend_head_tiles(int G) { return (G + 7) / 8; }
 
-int attend_ctas(int sms) { return sms * kPaCtasPerSm; }
-
 size_t attend_part_floats(int D, int G, int sms) {
-    return (size_t)2 * attend_ctas(sms) * attend_head_tile(G) * (D + 2);
+    return (size_t)2 * kAttendMaxCtas * sms * attend_head_tile(G) * (D + 2);
 }
 
 cudaError_t prepare_attend_kernels(bool bf16, int D, int G) { return prepare_attend_tiles<AllRows>(bf16, D, G); }

@@ -10,7 +10,6 @@ namespace {
 
 constexpr int kPaWarps = 4;
 constexpr int kPaThreads = 32 * kPaWarps;
-constexpr int kPaCtasPerSm = 2;
 constexpr float kLn2 = 0.693147180559945309f;
 
 __device__ __forceinline__ void lds_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -85,6 +84,9 @@ struct WindowRows {
     __device__ __forceinline__ int count() const { return len - shift; }
     __device__ __forceinline__ int key(int r) const { return r < split ? r : r + shift; }
     __device__ __forceinline__ bool sees(int key) const { return key < len && (key < sinks || key >= start); }
+    // all, any of the n rows from `key` on
+    __device__ __forceinline__ bool sees_all(int key, int n) const { return key + n <= len && (key + n <= sinks || key >= start); }
+    __device__ __forceinline__ bool sees_any(int key, int n) const { return key < len && (key < sinks || key + n > start); }
 };
 template <typename Rows> __device__ __forceinline__ int seen_rows(const AttendArgs &a, int len) {
     Rows r;
@@ -259,7 +261,7 @@ template <typename P> constexpr size_t attend_smem() {
     return (size_t)kPaWarps * (P::kStages * P::kStage + 4 * P::kHeads * (P::kMergeStride + 2));
 }
 
-// Persistent CTAs of four warps, two per SM.  The ragged (sequence, KV head,
+// Persistent CTAs of four warps, P::kCtas per SM.  The ragged (sequence, KV head,
 // block of 64 keys) units are cut into equal contiguous shares, one per CTA, so
 // that long and short sequences keep every SM equally busy; a segment cut between
 // CTAs is joined by the last of them to finish (in CTA order: the result does not
@@ -275,7 +277,7 @@ template <typename P> constexpr size_t attend_smem() {
 // Rows says which rows of a sequence are seen; the others are not read, and their
 // block-table entries neither.  P::kScaled: 8-bit rows with a scale for each.
 template <typename P, bool CLUSTER, typename Rows>
-__global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(AttendArgs a) {
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads, kStage = P::kStage;
     constexpr int kPart = Joined<P>::kPart, kGroup = Joined<P>::kGroup;   // kPart: sums [H][D], then (maximum, sum) [H]
@@ -290,7 +292,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
 
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
     UnitRange r;
-    Pieces<Rows> p;                                            // the piece being computed
+    Pieces<Rows> p;                                      // the piece being computed
     const int rank = CLUSTER ? (int)blockIdx.x % a.cluster : 0;
     if (CLUSTER) {
         p.only(a, blockIdx.x / a.cluster, rank, heads);
@@ -315,11 +317,34 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     while (more && ft * KT >= f.rows()) more = f.next(a);
     struct Place {
         int page, row, head;
-        bool in, live;                                   // a row that counts; a tile at all
+        bool live;                                       // a tile at all
+        int in;                                          // lane's row counts; with `whole` one bit for each row that it copies, bit 8 for that of its scale
     };
+    // 8-bit rows: a tile lies in one page where tiles divide pages
+    const bool whole = P::kScaled && a.cache.page_size % KT == 0;
+    const long long lane_at = lane / kChunks * a.cache.row_stride + lane % kChunks * 16;
     auto look_up = [&]() {                               // lane's row of the walk's tile (lanes past KT repeat), then on
-        Place w{0, 0, f.h / tiles, false, more};
+        Place w{0, 0, tiles == 1 ? f.h : f.h / tiles, more, 0};
         if (!more) return w;
+        if constexpr (P::kScaled) {
+            if (whole) {
+                const int key = f.seen.key(f.blk0 * kAttendUnit + ft * KT), slot = a.by_page.of(key);
+                w.row = key - slot * a.cache.page_size;
+                if (f.seen.sees_any(key, KT)) w.page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
+                w.in = 0x10F;
+                if (!f.seen.sees_all(key, KT)) {
+                    w.in = f.seen.sees(key + lane % KT) << 8;
+#pragma unroll
+                    for (int i = 0; i < KT / kRowsPer; ++i) w.in |= f.seen.sees(key + i * kRowsPer + lane / kChunks) << i;
+                }
+                ft += kPaWarps;
+                while (more && ft * KT >= f.rows()) {
+                    more = f.next(a);
+                    ft = warp;
+                }
+                return w;
+            }
+        }
         const int key = f.seen.key(f.blk0 * kAttendUnit + ft * KT) + (lane % KT);
         const int slot = (unsigned)key / (unsigned)a.cache.page_size;
         w.in = f.seen.sees(key);
@@ -338,9 +363,30 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
     // (up to 16 query heads a KV head read them once; the next head tile of more reads them again)
     const uint64_t once = l2_evict_first_policy();
     auto issue = [&]() {
-        if (next0.live) {
-            const bool known = (unsigned)next0.page < (unsigned)a.cache.n_pages;
-            if (next0.in && !known) set_err(a.err, kErrPage);
+        const bool known = (unsigned)next0.page < (unsigned)a.cache.n_pages;
+        if (next0.in && !known) set_err(a.err, kErrPage);
+        if (P::kScaled && whole && next0.live) {
+            const int in = known ? next0.in : 0;
+            const int page = known ? next0.page : 0;
+            const uint32_t ks = ring + stage_in * kStage, vs = ks + KT * kRow, to = vs + KT * kRow + 4 * lane;
+            const long long at = page * a.cache.page_stride + next0.head * a.cache.head_stride + next0.row * a.cache.row_stride + lane_at;
+            const char *kp = a.cache.k + at, *vp = a.cache.v + at;
+#pragma unroll
+            for (int i = 0; i < KT / kRowsPer; ++i) {
+                const uint32_t piece = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
+                cp16_once(ks + piece, kp, in >> i & 1, once);
+                cp16_once(vs + piece, vp, in >> i & 1, once);
+                kp += kRowsPer * a.cache.row_stride;
+                vp += kRowsPer * a.cache.row_stride;
+            }
+            const long long s = (page * (long long)a.Hkv + next0.head) * a.scale_blocks + a.by_scale.of(next0.row + lane % KT);
+            if (KT == 32) {
+                cp4(to, a.k_scales + s, in & 0x100);
+                cp4(to + 4 * KT, a.v_scales + s, in & 0x100);
+            } else {                                     // 16: K's by the lower lanes, V's by the upper ones
+                cp4(to, (lane < KT ? a.k_scales : a.v_scales) + s, in & 0x100);
+            }
+        } else if (next0.live) {
             const int ok = next0.in && known;
             const long long off = ok ? next0.page * a.cache.page_stride + next0.head * a.cache.head_stride + next0.row * a.cache.row_stride : 0;
             const uint32_t ks = ring + stage_in * kStage, vs = ks + KT * kRow;
@@ -354,7 +400,7 @@ __global__ void __launch_bounds__(kPaThreads, kPaCtasPerSm) paged_attend_kernel(
                 cp16_once(vs + P::piece(row, c), a.cache.v + at, in, once);
             }
             if constexpr (P::kScaled) {                  // the rows' scales behind them, K's, then V's
-                const long long s = ok ? (next0.page * (long long)a.Hkv + next0.head) * a.scale_blocks + (unsigned)next0.row / (unsigned)a.scale_rows : 0;
+                const long long s = ok ? (next0.page * (long long)a.Hkv + next0.head) * a.scale_blocks + a.by_scale.of(next0.row) : 0;
                 const uint32_t to = vs + KT * kRow + 4 * lane;
                 if (KT == 32) {
                     cp4(to, a.k_scales + s, ok);
@@ -538,7 +584,7 @@ inline long long attend_rows(const AttendArgs &a) {
 // heads each, 1000 rows 7.6 and 14.3, 4000 rows 13.0 and 18.9.
 inline int attend_cluster(long long segments, long long cap, int rows, int sms) {
     int cs = 1;
-    while (cs < 8 && cs * (long long)kAttendUnit < cap && 2 * cs * segments <= attend_ctas(sms)) cs *= 2;
+    while (cs < 8 && cs * (long long)kAttendUnit < cap && cs * segments <= sms) cs *= 2;
     return cap <= cs * (long long)rows ? cs : 1;
 }
 
@@ -550,7 +596,8 @@ template <typename P, typename Rows> cudaError_t start_attend(AttendArgs a, int 
     a.cluster = attend_cluster(segments, cap, P::kClusterRows, sms);
     if (a.cluster > 1)
         return launch_cluster(paged_attend_kernel<P, true, Rows>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<P>(), a.cluster, s, a);
-    const int grid = (int)(most < attend_ctas(sms) ? most : attend_ctas(sms));
+    const long long ctas = (long long)P::kCtas * sms;
+    const int grid = (int)(most < ctas ? most : ctas);
     return launch_k(paged_attend_kernel<P, false, Rows>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
 }
 template <typename P, typename Rows> cudaError_t prepare_attend() {

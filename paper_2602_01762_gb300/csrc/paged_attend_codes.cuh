@@ -39,6 +39,13 @@ __device__ __forceinline__ void two_parts(float x, float y, uint32_t &p0, uint32
     p1 = cvt_f16x2(x - v.x, y - v.y);
 }
 
+// 2^x; 0 below 2^-126.
+__device__ __forceinline__ float power2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+
 // Four codes as fp16: `lo` the first two, `hi` the others.
 template <int FORMAT> __device__ __forceinline__ void code_values(uint32_t codes, uint32_t &lo, uint32_t &hi) {
     if (FORMAT == kE4m3) {
@@ -78,7 +85,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     static constexpr int kQ = sizeof(T) == 4 && MODE != kPacked ? 2 : 1;    // products of K and q
     static constexpr int kParts = MODE == kPacked ? 1 : 2;                  // products of V and W
     static constexpr int kMergeStride = D + 4;
-    static constexpr int kStages = MODE == kSixteen ? 4 : 5;
+    static constexpr int kCtas = MODE == kSixteen ? 2 : 3, kStages = MODE == kSixteen ? 4 : 3;
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a
     // whole number: W up to 2^15 leaves the most below.
@@ -210,7 +217,8 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
             const float k0 = lds4(scales + 4 * (r + g)), k1 = lds4(scales + 4 * (r + g + 8));
             const float v0 = lds4(scales + 4 * (KT + r + g)), v1 = lds4(scales + 4 * (KT + r + g + 8));
             const float e0 = whole_log2(v0), e1 = whole_log2(v1);
-            const bool in0 = seen.sees(base + g), in1 = seen.sees(base + g + 8);
+            const bool all = seen.sees_all(base, 16);
+            const bool in0 = all || seen.sees(base + g), in1 = all || seen.sees(base + g + 8);
             bool grew = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -262,7 +270,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
                 const float b0 = base_of(m[t][0]), b1 = base_of(m[t][1]);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float p0 = exp2f(s[t][2 * u] - b0), p1 = exp2f(s[t][2 * u + 1] - b1), v = u ? v1 : v0;
+                    const float p0 = power2(s[t][2 * u] - b0), p1 = power2(s[t][2 * u + 1] - b1), v = u ? v1 : v0;
                     l[t][0] += p0;
                     l[t][1] += p1;
                     uint32_t x, y;

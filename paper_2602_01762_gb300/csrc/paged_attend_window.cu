@@ -23,6 +23,8 @@ cudaError_t prepare_code_attend_kernels(bool bf16, int D, int G) {
 cudaError_t launch_code_attend(const AttendArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
     AttendArgs a = args;
     if (a.window < 0) a.window = 0x7FFFFFFF;
+    a.by_page = Divisor((uint32_t)a.cache.page_size);
+    a.by_scale = Divisor((uint32_t)a.scale_rows);
     return format == kE4m3 ? start_e4m3_attend(a, bf16, D, sms, s) : start_int8_attend(a, bf16, D, sms, s);
 }
 
