@@ -85,6 +85,7 @@ struct AttendArgs {
     const float *k_scales, *v_scales;    // 8-bit caches: [n_pages, Hkv, scale_blocks]
     int scale_rows, scale_blocks;        // rows of a block; blocks of a page
     Divisor by_page, by_scale;           // 8-bit caches: by page_size, by scale_rows
+    int whole;                           // and whether tiles of rows divide pages
     int *err;
 };
 
@@ -188,6 +189,9 @@ __device__ __forceinline__ void cp16(uint32_t dst, const void *src, bool ok) {
 __device__ __forceinline__ void cp16_once(uint32_t dst, const void *src, bool ok, uint64_t policy) {
     const int n = ok ? 16 : 0;
     asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2, %3;" ::"r"(dst), "l"(src), "r"(n), "l"(policy) : "memory");
+}
+__device__ __forceinline__ void cp16_once(uint32_t dst, const void *src, uint64_t policy) {
+    asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
 }
 // 4 bytes.
 __device__ __forceinline__ void cp4(uint32_t dst, const void *src, bool ok) {

@@ -257,6 +257,201 @@ template <typename P> struct Joined {
     }
 };
 
+// The loads of a warp: a walk over the pieces of its own, and the pool place of each
+// lane's row of the next two tiles.
+template <typename P, typename Rows> struct RowFeed {
+    static constexpr int KT = P::KT, S = P::kStages, kStage = P::kStage, kRow = P::kRow, kChunks = kRow / 16, kRowsPer = 32 / kChunks;
+    struct Place {
+        int page, row, head;
+        bool in, live;                                   // a row that counts; a tile at all
+    };
+    Pieces<Rows> f;
+    Place next0, next1;
+    uint64_t once;
+    uint32_t ring;
+    int ft, warp, tiles, stage_in;
+    bool more;
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows> &p, uint32_t at, int w, int n_tiles) {
+        f = p;
+        ft = warp = w;
+        tiles = n_tiles;
+        ring = at;
+        stage_in = 0;
+        // K and V leave L2 first, so that scores, weights and pieces stay for the next reader
+        // (up to 16 query heads a KV head read them once; the next head tile of more reads them again)
+        once = l2_evict_first_policy();
+        more = true;
+        while (more && ft * KT >= f.rows()) more = f.next(a);
+        next0 = look_up(a);
+        next1 = look_up(a);
+    }
+    __device__ __forceinline__ Place look_up(const AttendArgs &a) {   // lane's row of the walk's tile (lanes past KT repeat), then on
+        Place w{0, 0, f.h / tiles, false, more};
+        if (!more) return w;
+        const int key = f.seen.key(f.blk0 * kAttendUnit + ft * KT) + (int)(threadIdx.x & 31) % KT;
+        const int slot = (unsigned)key / (unsigned)a.cache.page_size;
+        w.in = f.seen.sees(key);
+        w.row = key - slot * a.cache.page_size;
+        if (w.in) w.page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
+        ft += kPaWarps;
+        while (more && ft * KT >= f.rows()) {
+            more = f.next(a);
+            ft = warp;
+        }
+        return w;
+    }
+    __device__ __forceinline__ void issue(const AttendArgs &a) {
+        if (next0.live) {
+            const int lane = threadIdx.x & 31;
+            const bool known = (unsigned)next0.page < (unsigned)a.cache.n_pages;
+            if (next0.in && !known) set_err(a.err, kErrPage);
+            const int ok = next0.in && known;
+            const long long off = ok ? next0.page * a.cache.page_stride + next0.head * a.cache.head_stride + next0.row * a.cache.row_stride : 0;
+            const uint32_t ks = ring + stage_in * kStage, vs = ks + KT * kRow;
+            const int c = lane % kChunks;
+#pragma unroll
+            for (int i = 0; i < KT / kRowsPer; ++i) {
+                const int row = i * kRowsPer + lane / kChunks;
+                const long long at = __shfl_sync(0xFFFFFFFFu, off, row) + 16 * c;
+                const bool in = __shfl_sync(0xFFFFFFFFu, ok, row);
+                cp16_once(ks + P::piece(row, c), a.cache.k + at, in, once);
+                cp16_once(vs + P::piece(row, c), a.cache.v + at, in, once);
+            }
+        }
+        cp_group();
+        next0 = next1;
+        next1 = look_up(a);
+        stage_in = stage_in + 1 == S ? 0 : stage_in + 1;
+    }
+};
+
+// The same for 8-bit rows and their scales, one tile ahead.  Where tiles divide pages
+// (a.whole) a tile is one run of a page and everything but its page and row is the
+// piece's: of the 548 instructions that a tile of 16 rows took with the feed above some
+// 300 were its own.
+template <typename P, typename Rows> struct CodeFeed {
+    static constexpr int KT = P::KT, S = P::kStages, kStage = P::kStage, kRow = P::kRow, kChunks = kRow / 16, kRowsPer = 32 / kChunks;
+    static constexpr int kStep = kPaWarps * KT;
+    Pieces<Rows> f;
+    const int32_t *table;                                // of the sequence
+    const char *k_at;                                    // K of the head and of this lane's part of a run
+    uint64_t once;
+    uint32_t to, ring_end;                               // the next stage; the last one's end
+    long long head_scale;
+    int place, end, warp, tiles;
+    int page, row, in;                                   // next tile: bit i: this lane's row of copy i counts; bit 8: its scale's
+    bool more, live;
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows> &p, uint32_t at, int w, int n_tiles) {
+        f = p;
+        warp = w;
+        tiles = n_tiles;
+        to = at;
+        ring_end = at + S * kStage;
+        once = l2_evict_first_policy();                  // see RowFeed
+        enter(a);
+        more = true;
+        walk(a);
+        look_up(a);
+    }
+    __device__ __forceinline__ void enter(const AttendArgs &a) {
+        const int lane = threadIdx.x & 31, head = tiles == 1 ? f.h : f.h / tiles;
+        table = a.cache.table + (long long)f.b * a.cache.table_pages;
+        k_at = a.cache.k + head * a.cache.head_stride + (a.whole ? lane / kChunks * a.cache.row_stride : 0) + lane % kChunks * 16;
+        head_scale = (long long)head * a.scale_blocks;
+        place = f.blk0 * kAttendUnit + warp * KT;
+        end = f.blk0 * kAttendUnit + f.rows();
+    }
+    __device__ __forceinline__ void walk(const AttendArgs &a) {
+        while (place >= end) {
+            more = f.next(a);
+            if (!more) break;
+            enter(a);
+        }
+    }
+    __device__ __forceinline__ void look_up(const AttendArgs &a) {
+        const int lane = threadIdx.x & 31;
+        live = more;
+        if (!more) return;
+        const int key = f.seen.key(place);
+        if (a.whole) {
+            const int slot = a.by_page.of(key);
+            row = key - slot * a.cache.page_size;
+            in = 0x10F;
+            page = 0;
+            if (f.seen.sees_any(key, KT)) page = table[slot];
+            if (!f.seen.sees_all(key, KT)) {
+                in = f.seen.sees(key + lane % KT) << 8;
+#pragma unroll
+                for (int i = 0; i < KT / kRowsPer; ++i) in |= f.seen.sees(key + i * kRowsPer + lane / kChunks) << i;
+            }
+        } else {                                         // this lane's row (lanes past KT repeat)
+            const int slot = a.by_page.of(key + lane % KT);
+            row = key + lane % KT - slot * a.cache.page_size;
+            in = f.seen.sees(key + lane % KT) << 8;
+            page = in ? table[slot] : 0;
+        }
+    }
+    __device__ __forceinline__ void issue(const AttendArgs &a) {
+        const int lane = threadIdx.x & 31;
+        const long long v_from_k = a.cache.v - a.cache.k;
+        if (live) {
+            if ((unsigned)page >= (unsigned)a.cache.n_pages) {
+                if (in) set_err(a.err, kErrPage);
+                in = page = 0;
+            }
+            const uint32_t vs = to + KT * kRow;
+            if (a.whole) {
+                const char *kp = k_at + page * a.cache.page_stride + row * a.cache.row_stride;
+                if (in == 0x10F) {
+#pragma unroll
+                    for (int i = 0; i < KT / kRowsPer; ++i) {
+                        const uint32_t piece = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
+                        cp16_once(to + piece, kp, once);
+                        cp16_once(vs + piece, kp + v_from_k, once);
+                        kp += kRowsPer * a.cache.row_stride;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < KT / kRowsPer; ++i) {
+                        const uint32_t piece = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
+                        cp16_once(to + piece, kp, in >> i & 1, once);
+                        cp16_once(vs + piece, kp + v_from_k, in >> i & 1, once);
+                        kp += kRowsPer * a.cache.row_stride;
+                    }
+                }
+                row += lane % KT;
+            } else {
+                const long long off = page * a.cache.page_stride + row * a.cache.row_stride;
+#pragma unroll
+                for (int i = 0; i < KT / kRowsPer; ++i) {
+                    const int r = i * kRowsPer + lane / kChunks;
+                    const char *kp = k_at + __shfl_sync(0xFFFFFFFFu, off, r);
+                    const bool ok = __shfl_sync(0xFFFFFFFFu, in, r);
+                    cp16_once(to + P::piece(r, lane % kChunks), kp, ok, once);
+                    cp16_once(vs + P::piece(r, lane % kChunks), kp + v_from_k, ok, once);
+                }
+            }
+            // the rows' scales behind them, K's, then V's
+            const uint32_t st = vs + KT * kRow + 4 * lane;
+            const long long s = (page * (long long)a.Hkv) * a.scale_blocks + head_scale + a.by_scale.of(row);
+            if (KT == 32) {
+                cp4(st, a.k_scales + s, in & 0x100);
+                cp4(st + 4 * KT, a.v_scales + s, in & 0x100);
+            } else {                                     // 16: K's by the lower lanes, V's by the upper ones
+                cp4(st, (lane < KT ? a.k_scales : a.v_scales) + s, in & 0x100);
+            }
+            place += kStep;
+            if (place >= end) walk(a);
+            look_up(a);
+        }
+        cp_group();
+        to += kStage;
+        if (to == ring_end) to -= S * kStage;
+    }
+};
+template <typename P, typename Rows, bool SCALED = P::kScaled> struct FeedOf { using type = RowFeed<P, Rows>; };
+template <typename P, typename Rows> struct FeedOf<P, Rows, true> { using type = CodeFeed<P, Rows>; };
+
 template <typename P> constexpr size_t attend_smem() {
     return (size_t)kPaWarps * (P::kStages * P::kStage + 4 * P::kHeads * (P::kMergeStride + 2));
 }
@@ -281,7 +476,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads, kStage = P::kStage;
     constexpr int kPart = Joined<P>::kPart, kGroup = Joined<P>::kGroup;   // kPart: sums [H][D], then (maximum, sum) [H]
-    constexpr int kRow = P::kRow, kChunks = kRow / 16, kRowsPer = 32 / kChunks;
+    constexpr int kRow = P::kRow;
     extern __shared__ __align__(128) unsigned char smem[];
     __shared__ Cut joins[2];
     __shared__ int join_group[2], last;
@@ -309,114 +504,13 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
     float *sm = merge + kPaWarps * H * P::kMergeStride, *sl = sm + kPaWarps * H;    // [warps][H]
     float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
 
-    // Loads run ahead of the computation: their own walk, and the pool place of each
-    // lane's row of the next two tiles, so that no load waits for a block-table entry.
-    Pieces<Rows> f = p;
-    int ft = warp;
-    bool more = true;
-    while (more && ft * KT >= f.rows()) more = f.next(a);
-    struct Place {
-        int page, row, head;
-        bool live;                                       // a tile at all
-        int in;                                          // lane's row counts; with `whole` one bit for each row that it copies, bit 8 for that of its scale
-    };
-    // 8-bit rows: a tile lies in one page where tiles divide pages
-    const bool whole = P::kScaled && a.cache.page_size % KT == 0;
-    const long long lane_at = lane / kChunks * a.cache.row_stride + lane % kChunks * 16;
-    auto look_up = [&]() {                               // lane's row of the walk's tile (lanes past KT repeat), then on
-        Place w{0, 0, tiles == 1 ? f.h : f.h / tiles, more, 0};
-        if (!more) return w;
-        if constexpr (P::kScaled) {
-            if (whole) {
-                const int key = f.seen.key(f.blk0 * kAttendUnit + ft * KT), slot = a.by_page.of(key);
-                w.row = key - slot * a.cache.page_size;
-                if (f.seen.sees_any(key, KT)) w.page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
-                w.in = 0x10F;
-                if (!f.seen.sees_all(key, KT)) {
-                    w.in = f.seen.sees(key + lane % KT) << 8;
+    // Loads run ahead of the computation: their own walk, and the pool place of the next
+    // tiles' rows, so that no load waits for a block-table entry.
+    using Feed = typename FeedOf<P, Rows>::type;
+    Feed feed;
+    feed.begin(a, p, ring, warp, tiles);
 #pragma unroll
-                    for (int i = 0; i < KT / kRowsPer; ++i) w.in |= f.seen.sees(key + i * kRowsPer + lane / kChunks) << i;
-                }
-                ft += kPaWarps;
-                while (more && ft * KT >= f.rows()) {
-                    more = f.next(a);
-                    ft = warp;
-                }
-                return w;
-            }
-        }
-        const int key = f.seen.key(f.blk0 * kAttendUnit + ft * KT) + (lane % KT);
-        const int slot = (unsigned)key / (unsigned)a.cache.page_size;
-        w.in = f.seen.sees(key);
-        w.row = key - slot * a.cache.page_size;
-        if (w.in) w.page = a.cache.table[(long long)f.b * a.cache.table_pages + slot];
-        ft += kPaWarps;
-        while (more && ft * KT >= f.rows()) {
-            more = f.next(a);
-            ft = warp;
-        }
-        return w;
-    };
-    Place next0 = look_up(), next1 = look_up();
-    int stage_in = 0;
-    // K and V leave L2 first, so that scores, weights and pieces stay for the next reader
-    // (up to 16 query heads a KV head read them once; the next head tile of more reads them again)
-    const uint64_t once = l2_evict_first_policy();
-    auto issue = [&]() {
-        const bool known = (unsigned)next0.page < (unsigned)a.cache.n_pages;
-        if (next0.in && !known) set_err(a.err, kErrPage);
-        if (P::kScaled && whole && next0.live) {
-            const int in = known ? next0.in : 0;
-            const int page = known ? next0.page : 0;
-            const uint32_t ks = ring + stage_in * kStage, vs = ks + KT * kRow, to = vs + KT * kRow + 4 * lane;
-            const long long at = page * a.cache.page_stride + next0.head * a.cache.head_stride + next0.row * a.cache.row_stride + lane_at;
-            const char *kp = a.cache.k + at, *vp = a.cache.v + at;
-#pragma unroll
-            for (int i = 0; i < KT / kRowsPer; ++i) {
-                const uint32_t piece = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
-                cp16_once(ks + piece, kp, in >> i & 1, once);
-                cp16_once(vs + piece, vp, in >> i & 1, once);
-                kp += kRowsPer * a.cache.row_stride;
-                vp += kRowsPer * a.cache.row_stride;
-            }
-            const long long s = (page * (long long)a.Hkv + next0.head) * a.scale_blocks + a.by_scale.of(next0.row + lane % KT);
-            if (KT == 32) {
-                cp4(to, a.k_scales + s, in & 0x100);
-                cp4(to + 4 * KT, a.v_scales + s, in & 0x100);
-            } else {                                     // 16: K's by the lower lanes, V's by the upper ones
-                cp4(to, (lane < KT ? a.k_scales : a.v_scales) + s, in & 0x100);
-            }
-        } else if (next0.live) {
-            const int ok = next0.in && known;
-            const long long off = ok ? next0.page * a.cache.page_stride + next0.head * a.cache.head_stride + next0.row * a.cache.row_stride : 0;
-            const uint32_t ks = ring + stage_in * kStage, vs = ks + KT * kRow;
-            const int c = lane % kChunks;
-#pragma unroll
-            for (int i = 0; i < KT / kRowsPer; ++i) {
-                const int row = i * kRowsPer + lane / kChunks;
-                const long long at = __shfl_sync(0xFFFFFFFFu, off, row) + 16 * c;
-                const bool in = __shfl_sync(0xFFFFFFFFu, ok, row);
-                cp16_once(ks + P::piece(row, c), a.cache.k + at, in, once);
-                cp16_once(vs + P::piece(row, c), a.cache.v + at, in, once);
-            }
-            if constexpr (P::kScaled) {                  // the rows' scales behind them, K's, then V's
-                const long long s = ok ? (next0.page * (long long)a.Hkv + next0.head) * a.scale_blocks + a.by_scale.of(next0.row) : 0;
-                const uint32_t to = vs + KT * kRow + 4 * lane;
-                if (KT == 32) {
-                    cp4(to, a.k_scales + s, ok);
-                    cp4(to + 4 * KT, a.v_scales + s, ok);
-                } else {                                 // 16: the upper lanes repeat the rows
-                    cp4(to, (lane < KT ? a.k_scales : a.v_scales) + s, ok);
-                }
-            }
-        }
-        cp_group();
-        next0 = next1;
-        next1 = look_up();
-        stage_in = stage_in + 1 == S ? 0 : stage_in + 1;
-    };
-#pragma unroll
-    for (int i = 0; i < S - 1; ++i) issue();
+    for (int i = 0; i < S - 1; ++i) feed.issue(a);
 
     int stage = 0;
     P state;
@@ -433,7 +527,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
         for (int t = warp; t * KT < rows; t += kPaWarps) {
             cp_wait_group<S - 2>();
             __syncwarp();
-            issue();
+            feed.issue(a);
             const uint32_t ks = ring + stage * kStage;
             state.tile(ks, ks + KT * kRow, own, p.seen.key(p.blk0 * kAttendUnit + t * KT), p.seen, a.scale_log2, scores, n);
             stage = stage + 1 == S ? 0 : stage + 1;

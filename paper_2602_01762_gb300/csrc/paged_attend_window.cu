@@ -25,6 +25,7 @@ cudaError_t launch_code_attend(const AttendArgs &args, CodeFormat format, bool b
     if (a.window < 0) a.window = 0x7FFFFFFF;
     a.by_page = Divisor((uint32_t)a.cache.page_size);
     a.by_scale = Divisor((uint32_t)a.scale_rows);
+    a.whole = a.cache.page_size % (2048 / D) == 0;       // rows of a tile
     return format == kE4m3 ? start_e4m3_attend(a, bf16, D, sms, s) : start_int8_attend(a, bf16, D, sms, s);
 }
 
