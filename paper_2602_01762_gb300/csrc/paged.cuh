@@ -85,7 +85,8 @@ struct AttendArgs {
     const float *k_scales, *v_scales;    // 8-bit caches: [n_pages, Hkv, scale_blocks]
     int scale_rows, scale_blocks;        // rows of a block; blocks of a page
     Divisor by_page, by_scale;           // 8-bit caches: by page_size, by scale_rows
-    int whole;                           // and whether tiles of rows divide pages
+    int run;                             // 1: tiles divide pages and offsets are short, 2: dense rows besides
+    int short_page, short_row, page_scales;   // then: page_stride, row_stride, scales of a page
     int *err;
 };
 
@@ -309,17 +310,26 @@ __device__ __forceinline__ void dsmem_st(int *local, uint32_t rank, int v) {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(dsmem_at(local, rank)), "r"(v) : "memory");
 }
 
-// Ragged work split into equal contiguous shares.  Sequence b of rows(b) rows has
+// How units are shared out, CTA by CTA: the same to each.
+struct EvenShares {
+    int per;
+    __device__ __forceinline__ void set(int units, int ctas) { per = (units + ctas - 1) / ctas; }
+    // a share's first unit, and the share that a unit is in
+    __device__ __forceinline__ long long first(int cta) const { return (long long)cta * per; }
+    __device__ __forceinline__ int cta_of(int u) const { return u / per; }
+};
+// Ragged work split into contiguous shares.  Sequence b of rows(b) rows has
 // blocks_of(rows) >= 1 blocks of keys, each for `heads` heads; units run over (b, head, block).
-// Every CTA takes `per` units from u0 on, in sequence b; false: none are left for
+// Every CTA takes the units u0 .. u1 - 1, from sequence b on; false: none are left for
 // it.  All threads of the CTA call it.
-struct UnitRange {
-    int u0, u1, per;   // this CTA's units; units per CTA
+template <typename Shares = EvenShares> struct UnitRange {
+    int u0, u1;        // this CTA's units
+    Shares shares;
     int b, first;      // sequence of u0 and that sequence's first unit
     int lens;          // lane i: rows of sequence i (B <= 32 alone)
 };
-template <int THREADS, typename Rows, typename Blocks>
-__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, const Rows &rows, const Blocks &blocks_of) {
+template <int THREADS, typename Shares, typename Rows, typename Blocks>
+__device__ __forceinline__ bool unit_range(UnitRange<Shares> &r, int B, int heads, const Rows &rows, const Blocks &blocks_of) {
     const int tid = threadIdx.x, lane = tid & 31;
     const int cta = blockIdx.x, ctas = gridDim.x;
     auto blocks = [&](int b) { return blocks_of(rows(b)); };
@@ -333,10 +343,10 @@ __device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, const
             if (lane >= o) s += t;
         }
         const int units = __shfl_sync(0xFFFFFFFFu, s, 31) * heads;
-        r.per = (units + ctas - 1) / ctas;
-        if ((long long)cta * r.per >= units) return false;
-        r.u0 = cta * r.per;
-        r.u1 = min(r.u0 + r.per, units);
+        r.shares.set(units, ctas);
+        if (r.shares.first(cta) >= units) return false;
+        r.u0 = (int)r.shares.first(cta);
+        r.u1 = (int)min(r.shares.first(cta + 1), (long long)units);
         const int at = r.u0 / heads;
         r.b = __popc(__ballot_sync(0xFFFFFFFFu, lane < B && s <= at));
         r.first = __shfl_sync(0xFFFFFFFFu, s - n, r.b) * heads;
@@ -353,10 +363,10 @@ __device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, const
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) total += warp_sum[w];
     const int units = total * heads;
-    r.per = (units + ctas - 1) / ctas;
-    if ((long long)cta * r.per >= units) return false;
-    r.u0 = cta * r.per;
-    r.u1 = min(r.u0 + r.per, units);
+    r.shares.set(units, ctas);
+    if (r.shares.first(cta) >= units) return false;
+    r.u0 = (int)r.shares.first(cta);
+    r.u1 = (int)min(r.shares.first(cta + 1), (long long)units);
     const int at = r.u0 / heads;
     int before = 0;
     for (int base = 0; base < B && before <= at; base += THREADS) {

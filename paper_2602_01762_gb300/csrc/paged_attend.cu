@@ -37,7 +37,7 @@ __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel
     pdl_trigger();
     auto rows = [&](int b) { return paged_len(a.cache, b, a.added, nullptr); };
     auto blocks = [](int n) { return max(1, (n + kWtThreads - 1) / kWtThreads); };
-    UnitRange r;
+    UnitRange<> r;
     if (!unit_range<kWtThreads>(r, a.B, a.Hkv, rows, blocks)) {
         pdl_wait();
         return;

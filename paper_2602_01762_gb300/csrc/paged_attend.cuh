@@ -117,7 +117,7 @@ template <typename Rows> struct Pieces {
         blk1 = max(u - seg - kAttendCost, 0);
         return blk0 < blk1;
     }
-    __device__ __forceinline__ bool begin(const AttendArgs &a, const UnitRange &r, int n_heads) {
+    template <typename Shares> __device__ __forceinline__ bool begin(const AttendArgs &a, const UnitRange<Shares> &r, int n_heads) {
         u = r.u0;
         u1 = r.u1;
         b = r.b;
@@ -190,7 +190,7 @@ struct Cut {
 template <typename P> struct Joined {
     static constexpr int D = P::D, H = P::kHeads, kPart = H * (D + 2);
     static constexpr int kRound = kPaWarps * P::kStages * P::kStage / (4 * kPart);   // pieces that the rings hold
-    static constexpr int kGroup = kRound > 16 ? kRound : 16;
+    static constexpr int kGroup = kRound > 16 ? (P::kScaled && kRound < 64 ? 64 : kRound) : 16;
     static constexpr int kCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;
     float x[kCols][4], M[kCols], L[kCols];
 
@@ -271,6 +271,7 @@ template <typename P, typename Rows> struct RowFeed {
     uint32_t ring;
     int ft, warp, tiles, stage_in;
     bool more;
+    __device__ __forceinline__ uint32_t free_stage() const { return ring + stage_in * kStage; }
     __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows> &p, uint32_t at, int w, int n_tiles) {
         f = p;
         ft = warp = w;
@@ -325,29 +326,36 @@ template <typename P, typename Rows> struct RowFeed {
     }
 };
 
-// The same for 8-bit rows and their scales, one tile ahead.  Where tiles divide pages
-// (a.whole) a tile is one run of a page and everything but its page and row is the
-// piece's: of the 548 instructions that a tile of 16 rows took with the feed above some
-// 300 were its own.
+// The same for 8-bit rows and their scales, one tile of two runs of kRunRows rows ahead.
+// Where runs divide pages and offsets are short (a.run), a run lies in one page and all
+// but its page and row is known from the piece or from the launch.
+constexpr int kRunRows = 16;
 template <typename P, typename Rows> struct CodeFeed {
     static constexpr int KT = P::KT, S = P::kStages, kStage = P::kStage, kRow = P::kRow, kChunks = kRow / 16, kRowsPer = 32 / kChunks;
-    static constexpr int kStep = kPaWarps * KT;
+    static constexpr int kStep = kPaWarps * KT, kCopies = kRunRows / kRowsPer, kAll = (1 << kCopies) - 1;
+    static_assert(KT == 2 * kRunRows, "a lane's scale is that of its row");
     Pieces<Rows> f;
     const int32_t *table;                                // of the sequence
-    const char *k_at;                                    // K of the head and of this lane's part of a run
+    const char *k_at, *v_at;                             // of the head and of this lane's part of a run
+    const float *scales;                                 // K's of the head
     uint64_t once;
-    uint32_t to, ring_end;                               // the next stage; the last one's end
-    long long head_scale;
+    uint32_t to, ring_end;                               // the next stage, which is free; the last one's end
+    uint32_t piece[2];                                   // of this lane's copies, even and odd ones
     int place, end, warp, tiles;
-    int page, row, in;                                   // next tile: bit i: this lane's row of copy i counts; bit 8: its scale's
+    int page[2], row[2], in[2];                          // next tile's runs: bit i: this lane's row of copy i counts
+    int own;                                             // and whether row `lane` of the tile does
     bool more, live;
+    __device__ __forceinline__ uint32_t free_stage() const { return to; }
     __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows> &p, uint32_t at, int w, int n_tiles) {
+        const int lane = threadIdx.x & 31;
         f = p;
         warp = w;
         tiles = n_tiles;
         to = at;
         ring_end = at + S * kStage;
         once = l2_evict_first_policy();                  // see RowFeed
+#pragma unroll
+        for (int i = 0; i < 2; ++i) piece[i] = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
         enter(a);
         more = true;
         walk(a);
@@ -355,9 +363,11 @@ template <typename P, typename Rows> struct CodeFeed {
     }
     __device__ __forceinline__ void enter(const AttendArgs &a) {
         const int lane = threadIdx.x & 31, head = tiles == 1 ? f.h : f.h / tiles;
+        const long long at = head * a.cache.head_stride + (a.run ? lane / kChunks * a.cache.row_stride : 0) + lane % kChunks * 16;
         table = a.cache.table + (long long)f.b * a.cache.table_pages;
-        k_at = a.cache.k + head * a.cache.head_stride + (a.whole ? lane / kChunks * a.cache.row_stride : 0) + lane % kChunks * 16;
-        head_scale = (long long)head * a.scale_blocks;
+        k_at = a.cache.k + at;
+        v_at = a.cache.v + at;
+        scales = a.k_scales + (long long)head * a.scale_blocks;
         place = f.blk0 * kAttendUnit + warp * KT;
         end = f.blk0 * kAttendUnit + f.rows();
     }
@@ -369,77 +379,95 @@ template <typename P, typename Rows> struct CodeFeed {
         }
     }
     __device__ __forceinline__ void look_up(const AttendArgs &a) {
-        const int lane = threadIdx.x & 31;
         live = more;
         if (!more) return;
-        const int key = f.seen.key(place);
-        if (a.whole) {
-            const int slot = a.by_page.of(key);
-            row = key - slot * a.cache.page_size;
-            in = 0x10F;
-            page = 0;
-            if (f.seen.sees_any(key, KT)) page = table[slot];
-            if (!f.seen.sees_all(key, KT)) {
-                in = f.seen.sees(key + lane % KT) << 8;
+        const int lane = threadIdx.x & 31, key = f.seen.key(place);
+        const bool all = f.seen.sees_all(key, KT);
+        own = all || f.seen.sees(key + lane);
+        if (a.run) {
 #pragma unroll
-                for (int i = 0; i < KT / kRowsPer; ++i) in |= f.seen.sees(key + i * kRowsPer + lane / kChunks) << i;
+            for (int j = 0; j < 2; ++j) {
+                const int k = key + j * kRunRows, slot = a.by_page.of(k);
+                row[j] = k - slot * a.cache.page_size;
+                in[j] = kAll;
+                page[j] = 0;
+                if (all || f.seen.sees_any(k, kRunRows)) page[j] = table[slot];
+                if (!all) {
+                    in[j] = 0;
+#pragma unroll
+                    for (int i = 0; i < kCopies; ++i) in[j] |= f.seen.sees(k + i * kRowsPer + lane / kChunks) << i;
+                }
             }
-        } else {                                         // this lane's row (lanes past KT repeat)
-            const int slot = a.by_page.of(key + lane % KT);
-            row = key + lane % KT - slot * a.cache.page_size;
-            in = f.seen.sees(key + lane % KT) << 8;
-            page = in ? table[slot] : 0;
+        } else {                                         // this lane's row
+            const int slot = a.by_page.of(key + lane);
+            row[0] = key + lane - slot * a.cache.page_size;
+            page[0] = own ? table[slot] : 0;
+        }
+    }
+    // Shared address of this lane's copy i: rows come back to the same banks every other copy.
+    __device__ __forceinline__ uint32_t place_of(int i) const { return to + piece[i & 1] + (i >> 1) * (2 * kRowsPer * kRow); }
+    // One run's. STEP: bytes from a copy's row to the next one's, 0 unless they are dense.
+    template <int STEP> __device__ __forceinline__ void copies(const AttendArgs &a, int j, bool known) {
+        const long long at = (long long)page[j] * a.short_page + (long long)row[j] * a.short_row;
+        const char *kp = k_at + at, *vp = v_at + at;
+        if (known && in[j] == kAll) {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                cp16_once(place_of(j * kCopies + i), kp + i * STEP, once);
+                cp16_once(place_of(j * kCopies + i) + KT * kRow, vp + i * STEP, once);
+                if (!STEP) kp += kRowsPer * a.short_row, vp += kRowsPer * a.short_row;
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < kCopies; ++i) {
+                const bool ok = known && (in[j] >> i & 1);
+                cp16_once(place_of(j * kCopies + i), kp + i * STEP, ok, once);
+                cp16_once(place_of(j * kCopies + i) + KT * kRow, vp + i * STEP, ok, once);
+                if (!STEP) kp += kRowsPer * a.short_row, vp += kRowsPer * a.short_row;
+            }
         }
     }
     __device__ __forceinline__ void issue(const AttendArgs &a) {
-        const int lane = threadIdx.x & 31;
-        const long long v_from_k = a.cache.v - a.cache.k;
         if (live) {
-            if ((unsigned)page >= (unsigned)a.cache.n_pages) {
-                if (in) set_err(a.err, kErrPage);
-                in = page = 0;
-            }
-            const uint32_t vs = to + KT * kRow;
-            if (a.whole) {
-                const char *kp = k_at + page * a.cache.page_stride + row * a.cache.row_stride;
-                if (in == 0x10F) {
+            const int lane = threadIdx.x & 31;
+            const float *s;
+            bool ok = own;
+            if (a.run) {
+                bool known[2];
 #pragma unroll
-                    for (int i = 0; i < KT / kRowsPer; ++i) {
-                        const uint32_t piece = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
-                        cp16_once(to + piece, kp, once);
-                        cp16_once(vs + piece, kp + v_from_k, once);
-                        kp += kRowsPer * a.cache.row_stride;
+                for (int j = 0; j < 2; ++j) {
+                    known[j] = (unsigned)page[j] < (unsigned)a.cache.n_pages;
+                    if (!known[j]) {
+                        set_err(a.err, kErrPage);        // an unseen run has page 0
+                        page[j] = 0;
                     }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < KT / kRowsPer; ++i) {
-                        const uint32_t piece = P::piece(i * kRowsPer + lane / kChunks, lane % kChunks);
-                        cp16_once(to + piece, kp, in >> i & 1, once);
-                        cp16_once(vs + piece, kp + v_from_k, in >> i & 1, once);
-                        kp += kRowsPer * a.cache.row_stride;
-                    }
+                    if (a.run == 2) copies<kRowsPer * kRow>(a, j, known[j]);
+                    else copies<0>(a, j, known[j]);
                 }
-                row += lane % KT;
+                ok = ok && (lane < kRunRows ? known[0] : known[1]);
+                const int p = lane < kRunRows ? page[0] : page[1], r = lane < kRunRows ? row[0] : row[1];
+                s = scales + (p * a.page_scales + a.by_scale.of(r + lane % kRunRows));
             } else {
-                const long long off = page * a.cache.page_stride + row * a.cache.row_stride;
+                if ((unsigned)page[0] >= (unsigned)a.cache.n_pages) {
+                    set_err(a.err, kErrPage);
+                    ok = false;
+                    page[0] = 0;
+                }
+                const long long off = page[0] * a.cache.page_stride + row[0] * a.cache.row_stride;
 #pragma unroll
                 for (int i = 0; i < KT / kRowsPer; ++i) {
                     const int r = i * kRowsPer + lane / kChunks;
-                    const char *kp = k_at + __shfl_sync(0xFFFFFFFFu, off, r);
-                    const bool ok = __shfl_sync(0xFFFFFFFFu, in, r);
-                    cp16_once(to + P::piece(r, lane % kChunks), kp, ok, once);
-                    cp16_once(vs + P::piece(r, lane % kChunks), kp + v_from_k, ok, once);
+                    const long long at = __shfl_sync(0xFFFFFFFFu, off, r);
+                    const bool in_r = __shfl_sync(0xFFFFFFFFu, (int)ok, r);
+                    cp16_once(place_of(i), k_at + at, in_r, once);
+                    cp16_once(place_of(i) + KT * kRow, v_at + at, in_r, once);
                 }
+                s = scales + (page[0] * (long long)a.Hkv * a.scale_blocks + a.by_scale.of(row[0]));
             }
             // the rows' scales behind them, K's, then V's
-            const uint32_t st = vs + KT * kRow + 4 * lane;
-            const long long s = (page * (long long)a.Hkv) * a.scale_blocks + head_scale + a.by_scale.of(row);
-            if (KT == 32) {
-                cp4(st, a.k_scales + s, in & 0x100);
-                cp4(st + 4 * KT, a.v_scales + s, in & 0x100);
-            } else {                                     // 16: K's by the lower lanes, V's by the upper ones
-                cp4(st, (lane < KT ? a.k_scales : a.v_scales) + s, in & 0x100);
-            }
+            const uint32_t st = to + 2 * KT * kRow + 4 * lane;
+            cp4(st, s, ok);
+            cp4(st + 4 * KT, s + (a.v_scales - a.k_scales), ok);
             place += kStep;
             if (place >= end) walk(a);
             look_up(a);
@@ -452,8 +480,12 @@ template <typename P, typename Rows> struct CodeFeed {
 template <typename P, typename Rows, bool SCALED = P::kScaled> struct FeedOf { using type = RowFeed<P, Rows>; };
 template <typename P, typename Rows> struct FeedOf<P, Rows, true> { using type = CodeFeed<P, Rows>; };
 
+// Rings, then a sum area (P::kScaled: one for a cluster's sums, a warp's own goes to its
+// ring's free stage; else one for each warp), then maxima and sums.
+template <typename P> constexpr int kAttendSums = P::kScaled ? 4 * P::kHeads * (P::D + 2) : kPaWarps * 4 * P::kHeads * P::kMergeStride;
 template <typename P> constexpr size_t attend_smem() {
-    return (size_t)kPaWarps * (P::kStages * P::kStage + 4 * P::kHeads * (P::kMergeStride + 2));
+    static_assert(!P::kScaled || 4 * P::kHeads * P::kMergeStride <= P::kStage, "a stage holds a warp's sums");
+    return (size_t)kPaWarps * (P::kStages * P::kStage + 8 * P::kHeads) + kAttendSums<P>;
 }
 
 // Persistent CTAs of four warps, P::kCtas per SM.  The ragged (sequence, KV head,
@@ -486,7 +518,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
     pdl_trigger();
 
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
-    UnitRange r;
+    UnitRange<typename P::Shares> r;
     Pieces<Rows> p;                                      // the piece being computed
     const int rank = CLUSTER ? (int)blockIdx.x % a.cluster : 0;
     if (CLUSTER) {
@@ -501,15 +533,17 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * kStage);
     float *merge = (float *)(smem + kPaWarps * S * kStage);                       // [warps][H][stride]
-    float *sm = merge + kPaWarps * H * P::kMergeStride, *sl = sm + kPaWarps * H;    // [warps][H]
+    float *sm = (float *)(smem + kPaWarps * S * kStage + kAttendSums<P>), *sl = sm + kPaWarps * H;    // [warps][H]
     float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
+    float *sums = P::kScaled ? merge : (float *)smem;    // a cluster's, for its other ranks
+    __shared__ uint32_t own_at[kPaWarps];                // P::kScaled: where the warps' shares are
 
     // Loads run ahead of the computation: their own walk, and the pool place of the next
     // tiles' rows, so that no load waits for a block-table entry.
     using Feed = typename FeedOf<P, Rows>::type;
     Feed feed;
     feed.begin(a, p, ring, warp, tiles);
-#pragma unroll
+#pragma unroll P::kScaled ? 1 : S
     for (int i = 0; i < S - 1; ++i) feed.issue(a);
 
     int stage = 0;
@@ -535,11 +569,16 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
         Pieces<Rows> after = p;
         go = after.next(a);
         if (go) state.load_q((const T *)a.q + first_head(after) * D, head_count(after), a.scale_log2);   // on its way during the merge
+        if (P::kScaled) {
+            __syncwarp();                                // the stage was read
+            own = (float *)(smem + (feed.free_stage() - (uint32_t)__cvta_generic_to_shared(smem)));
+            if (lane == 0) own_at[warp] = (uint32_t)(own - (float *)smem);
+        }
         state.store(own, sm + warp * H, sl + warp * H);
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
         const int first = p.seg + kAttendCost;           // unit of the segment's first block
-        const int c0 = CLUSTER ? 0 : first / r.per, c1 = CLUSTER ? 0 : (first + p.nblk - 1) / r.per;
+        const int c0 = CLUSTER ? 0 : r.shares.cta_of(first), c1 = CLUSTER ? 0 : r.shares.cta_of(first + p.nblk - 1);
         const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
         float *part = a.part + (long long)slot * kPart;
         for (int e = tid; e < n * (D / 4); e += kPaThreads) {
@@ -552,7 +591,8 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
 #pragma unroll
             for (int w = 0; w < kPaWarps; ++w) {
                 const float k = exp2f(sm[w * H + h] - base);
-                const float4 y = *(const float4 *)(merge + (w * H + h) * P::kMergeStride + d);
+                const float *from = P::kScaled ? (const float *)smem + own_at[w] : merge + w * H * P::kMergeStride;
+                const float4 y = *(const float4 *)(from + h * P::kMergeStride + d);
                 L = fmaf(k, sl[w * H + h], L);
                 x[0] = fmaf(k, y.x, x[0]);
                 x[1] = fmaf(k, y.y, x[1]);
@@ -561,9 +601,9 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
             }
             if (!CLUSTER && whole) {
                 write_out<T, D>(a, hq + h, d, x, M, L);
-            } else if (CLUSTER) {                        // for the other ranks, where the rings were
-                *(float4 *)((float *)smem + h * D + d) = make_float4(x[0], x[1], x[2], x[3]);
-                if (d == 0) *(float2 *)((float *)smem + H * D + 2 * h) = make_float2(M, L);
+            } else if (CLUSTER) {                        // for the other ranks
+                *(float4 *)(sums + h * D + d) = make_float4(x[0], x[1], x[2], x[3]);
+                if (d == 0) *(float2 *)(sums + H * D + 2 * h) = make_float2(M, L);
             } else {
                 __stcg((float4 *)(part + h * D + d), make_float4(x[0], x[1], x[2], x[3]));
                 if (d == 0) {
@@ -582,8 +622,8 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
 #pragma unroll
                 for (int k = 0; k < 8; ++k)
                     if (k < a.cluster) {
-                        dsmem_ld((float *)smem + h * D + d, k, y[k]);
-                        dsmem_ld((float *)smem + H * D + 2 * h, k, ml[k]);
+                        dsmem_ld(sums + h * D + d, k, y[k]);
+                        dsmem_ld(sums + H * D + 2 * h, k, ml[k]);
                     }
                 float M = -INFINITY, x[4] = {0.f, 0.f, 0.f, 0.f}, L = 0.f;
 #pragma unroll

@@ -78,14 +78,15 @@ template <int FORMAT> __device__ __forceinline__ void code_values(uint32_t codes
 enum HeadMode : int { kPacked = 0, kEight = 1, kSixteen = 2 };
 template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     using T = T_;
-    static constexpr int D = D_, KT = 2048 / D, NT = MODE == kSixteen ? 2 : 1;
+    static constexpr int D = D_, KT = 32, NT = MODE == kSixteen ? 2 : 1;
     static constexpr int kRow = D, kStage = 2 * KT * kRow + 8 * KT;   // bytes
     static constexpr bool kScaled = true;
+    using Shares = EvenShares;
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
     static constexpr int kQ = sizeof(T) == 4 && MODE != kPacked ? 2 : 1;    // products of K and q
     static constexpr int kParts = MODE == kPacked ? 1 : 2;                  // products of V and W
     static constexpr int kMergeStride = D + 4;
-    static constexpr int kCtas = MODE == kSixteen ? 2 : 3, kStages = MODE == kSixteen ? 4 : 3;
+    static constexpr int kCtas = MODE == kSixteen ? 2 : 3, kStages = (D == 128 ? 2 : 4) + (MODE == kSixteen ? 1 : 0);
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a
     // whole number: W up to 2^15 leaves the most below.
@@ -167,10 +168,9 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
             for (int d = 0; d < D / 16; ++d) o[d][t][0] = o[d][t][1] = 0ull;
         }
     }
-    // log2 of a scale, its fraction cut (of an infinite one or NaN 128).
+    // log2 of a scale, its fraction cut (of 0 -127, of an infinite one or NaN 128).
     static __device__ __forceinline__ float whole_log2(float s) {
-        const uint32_t b = __float_as_uint(s) & 0x7FFFFFFFu;
-        return b == 0 ? -INFINITY : (float)((int)(b >> 23) - 127);
+        return __uint_as_float((__float_as_uint(s) & 0x7FFFFFFFu) >> 23 | 0x4B000000u) - 8388735.f;   // 2^23 + exponent
     }
     static __device__ __forceinline__ float lds4(uint32_t addr) {
         float v;
@@ -192,7 +192,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, float *, int key0, const Rows &seen, float, float *, int) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
         const uint32_t scales = vs + KT * kRow;
-#pragma unroll
+#pragma unroll 1
         for (int sub = 0; sub < KT / 16; ++sub) {
             const int base = key0 + 16 * sub, r = 16 * sub;
             if (sub > 0 && base >= seen.len) break;

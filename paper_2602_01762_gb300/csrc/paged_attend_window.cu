@@ -25,7 +25,13 @@ cudaError_t launch_code_attend(const AttendArgs &args, CodeFormat format, bool b
     if (a.window < 0) a.window = 0x7FFFFFFF;
     a.by_page = Divisor((uint32_t)a.cache.page_size);
     a.by_scale = Divisor((uint32_t)a.scale_rows);
-    a.whole = a.cache.page_size % (2048 / D) == 0;       // rows of a tile
+    const PagedView &c = a.cache;
+    const long long scales = (long long)a.Hkv * a.scale_blocks, most = 0x7FFFFFFF;
+    if (c.page_size % kRunRows == 0 && c.page_stride <= most && c.page_stride >= -most && c.row_stride <= most / 8 && c.row_stride >= -most / 8 &&
+        scales * c.n_pages <= most) {
+        a.run = c.row_stride == D ? 2 : 1;
+        a.short_page = (int)c.page_stride, a.short_row = (int)c.row_stride, a.page_scales = (int)scales;
+    }
     return format == kE4m3 ? start_e4m3_attend(a, bf16, D, sms, s) : start_int8_attend(a, bf16, D, sms, s);
 }
 
