@@ -124,7 +124,7 @@ struct EvictArgs {
 };
 
 constexpr int kAttendUnit = 64;          // keys per unit of the attention's work split
-constexpr int kAttendCost = 1;           // units that a segment costs beside its keys
+constexpr int kAttendCost = 1;           // units that a segment costs beside its keys, at least
 // Query heads that share a pass over the rows; the most passes over a KV head's rows
 // that its G query heads take.
 inline int attend_head_tile(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }

@@ -50,10 +50,9 @@ constexpr float kSlack = 8.f;
 __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f : m; }
 
 // A segment is one (sequence, KV head, head tile): blocks of kAttendUnit keys, and
-// before them kAttendCost units without keys that stand for what a segment costs
+// before them P::kCost units without keys that stand for what a segment costs
 // beside its rows (its queries, merge and result).
 __device__ __forceinline__ int blocks_of(int len) { return max(1, (len + kAttendUnit - 1) / kAttendUnit); }
-__device__ __forceinline__ int units_of(int len) { return kAttendCost + blocks_of(len); }
 
 // The rows of a sequence that are attended to, in blocks side by side: `count` rows
 // from place 0 on, of which place r is row key(r) and counts where it is seen.
@@ -98,7 +97,7 @@ template <typename Rows> __device__ __forceinline__ int seen_rows(const AttendAr
 // segment after the other; parts of a segment without blocks are passed over.  Each
 // lane keeps the length of one of the next 32 sequences, so that a step waits for
 // no load.
-template <typename Rows> struct Pieces {
+template <typename Rows, int COST> struct Pieces {
     int u, u1, seg, b, h, heads, blk0, blk1, nblk;   // seg: the segment's first unit
     Rows seen;
     int base, lens;                      // lane i: rows of sequence base + i
@@ -112,9 +111,9 @@ template <typename Rows> struct Pieces {
         nblk = blocks_of(seen.count());
     }
     __device__ __forceinline__ bool cut() {
-        blk0 = max(u - seg - kAttendCost, 0);
-        u = min(seg + kAttendCost + nblk, u1);
-        blk1 = max(u - seg - kAttendCost, 0);
+        blk0 = max(u - seg - COST, 0);
+        u = min(seg + COST + nblk, u1);
+        blk1 = max(u - seg - COST, 0);
         return blk0 < blk1;
     }
     template <typename Shares> __device__ __forceinline__ bool begin(const AttendArgs &a, const UnitRange<Shares> &r, int n_heads) {
@@ -129,8 +128,8 @@ template <typename Rows> struct Pieces {
             fetch(a);
         }
         sequence(a);
-        h = (u - r.first) / (kAttendCost + nblk);
-        seg = r.first + h * (kAttendCost + nblk);
+        h = (u - r.first) / (COST + nblk);
+        seg = r.first + h * (COST + nblk);
         return cut() || next(a);
     }
     // A cluster's rank takes its run of the blocks of segment i, and no other piece.
@@ -190,7 +189,7 @@ struct Cut {
 template <typename P> struct Joined {
     static constexpr int D = P::D, H = P::kHeads, kPart = H * (D + 2);
     static constexpr int kRound = kPaWarps * P::kStages * P::kStage / (4 * kPart);   // pieces that the rings hold
-    static constexpr int kGroup = kRound > 16 ? (P::kScaled && kRound < 64 ? 64 : kRound) : 16;
+    static constexpr int kGroup = kRound > 16 && !P::kScaled ? kRound : 16;
     static constexpr int kCols = H * D / 4 / kPaThreads > 0 ? H * D / 4 / kPaThreads : 1;
     float x[kCols][4], M[kCols], L[kCols];
 
@@ -265,14 +264,14 @@ template <typename P, typename Rows> struct RowFeed {
         int page, row, head;
         bool in, live;                                   // a row that counts; a tile at all
     };
-    Pieces<Rows> f;
+    Pieces<Rows, P::kCost> f;
     Place next0, next1;
     uint64_t once;
     uint32_t ring;
     int ft, warp, tiles, stage_in;
     bool more;
     __device__ __forceinline__ uint32_t free_stage() const { return ring + stage_in * kStage; }
-    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows> &p, uint32_t at, int w, int n_tiles) {
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows, P::kCost> &p, uint32_t at, int w, int n_tiles) {
         f = p;
         ft = warp = w;
         tiles = n_tiles;
@@ -334,7 +333,7 @@ template <typename P, typename Rows> struct CodeFeed {
     static constexpr int KT = P::KT, S = P::kStages, kStage = P::kStage, kRow = P::kRow, kChunks = kRow / 16, kRowsPer = 32 / kChunks;
     static constexpr int kStep = kPaWarps * KT, kCopies = kRunRows / kRowsPer, kAll = (1 << kCopies) - 1;
     static_assert(KT == 2 * kRunRows, "a lane's scale is that of its row");
-    Pieces<Rows> f;
+    Pieces<Rows, P::kCost> f;
     const int32_t *table;                                // of the sequence
     const char *k_at, *v_at;                             // of the head and of this lane's part of a run
     const float *scales;                                 // K's of the head
@@ -346,7 +345,7 @@ template <typename P, typename Rows> struct CodeFeed {
     int own;                                             // and whether row `lane` of the tile does
     bool more, live;
     __device__ __forceinline__ uint32_t free_stage() const { return to; }
-    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows> &p, uint32_t at, int w, int n_tiles) {
+    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows, P::kCost> &p, uint32_t at, int w, int n_tiles) {
         const int lane = threadIdx.x & 31;
         f = p;
         warp = w;
@@ -519,14 +518,14 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
 
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
     UnitRange<typename P::Shares> r;
-    Pieces<Rows> p;                                      // the piece being computed
+    Pieces<Rows, P::kCost> p;                                      // the piece being computed
     const int rank = CLUSTER ? (int)blockIdx.x % a.cluster : 0;
     if (CLUSTER) {
         p.only(a, blockIdx.x / a.cluster, rank, heads);
     } else {
         if (!unit_range<kPaThreads>(r, a.B, heads,
                                     [&](int b) { return paged_len(a.cache, b, a.added, a.err); },
-                                    [&](int len) { return units_of(seen_rows<Rows>(a, len)); }))
+                                    [&](int len) { return P::kCost + blocks_of(seen_rows<Rows>(a, len)); }))
             return;
         if (!p.begin(a, r, heads)) return;
     }
@@ -549,8 +548,8 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
     int stage = 0;
     P state;
     bool go = true;
-    auto first_head = [&](const Pieces<Rows> &w) { return (long long)w.b * a.Hq + w.h / tiles * G + w.h % tiles * H; };
-    auto head_count = [&](const Pieces<Rows> &w) { return min(H, G - w.h % tiles * H); };
+    auto first_head = [&](const Pieces<Rows, P::kCost> &w) { return (long long)w.b * a.Hq + w.h / tiles * G + w.h % tiles * H; };
+    auto head_count = [&](const Pieces<Rows, P::kCost> &w) { return min(H, G - w.h % tiles * H); };
     state.load_q((const T *)a.q + first_head(p) * D, head_count(p), a.scale_log2);
     while (go) {
         const int kvh = p.h / tiles, h0 = (p.h % tiles) * H, n = head_count(p);
@@ -566,7 +565,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
             state.tile(ks, ks + KT * kRow, own, p.seen.key(p.blk0 * kAttendUnit + t * KT), p.seen, a.scale_log2, scores, n);
             stage = stage + 1 == S ? 0 : stage + 1;
         }
-        Pieces<Rows> after = p;
+        Pieces<Rows, P::kCost> after = p;
         go = after.next(a);
         if (go) state.load_q((const T *)a.q + first_head(after) * D, head_count(after), a.scale_log2);   // on its way during the merge
         if (P::kScaled) {
@@ -577,7 +576,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
         state.store(own, sm + warp * H, sl + warp * H);
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
-        const int first = p.seg + kAttendCost;           // unit of the segment's first block
+        const int first = p.seg + P::kCost;           // unit of the segment's first block
         const int c0 = CLUSTER ? 0 : r.shares.cta_of(first), c1 = CLUSTER ? 0 : r.shares.cta_of(first + p.nblk - 1);
         const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
         float *part = a.part + (long long)slot * kPart;
@@ -726,7 +725,7 @@ inline int attend_cluster(long long segments, long long cap, int rows, int sms) 
 template <typename P, typename Rows> cudaError_t start_attend(AttendArgs a, int ht, int sms, cudaStream_t s) {
     const int G = a.Hq / a.Hkv;
     const long long cap = attend_rows(a), segments = a.B * (long long)a.Hkv * ((G + ht - 1) / ht);
-    const long long most = segments * (kAttendCost + (cap + kAttendUnit - 1) / kAttendUnit);
+    const long long most = segments * (P::kCost + (cap + kAttendUnit - 1) / kAttendUnit);
     a.cluster = attend_cluster(segments, cap, P::kClusterRows, sms);
     if (a.cluster > 1)
         return launch_cluster(paged_attend_kernel<P, true, Rows>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<P>(), a.cluster, s, a);

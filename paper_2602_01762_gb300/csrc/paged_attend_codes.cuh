@@ -86,6 +86,9 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     static constexpr int kQ = sizeof(T) == 4 && MODE != kPacked ? 2 : 1;    // products of K and q
     static constexpr int kParts = MODE == kPacked ? 1 : 2;                  // products of V and W
     static constexpr int kMergeStride = D + 4;
+    // a segment's end costs what two blocks of 8-bit rows do: 16 sequences of 1 to 8192 rows
+    // with 1, 2 and 3 units 40.3, 34.0 and 33.4 us
+    static constexpr int kCost = 2;
     static constexpr int kCtas = MODE == kSixteen ? 2 : 3, kStages = (D == 128 ? 2 : 4) + (MODE == kSixteen ? 1 : 0);
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a
@@ -178,28 +181,30 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
         return v;
     }
     // This lane's D / 8 bytes of a row of V.
-    static __device__ __forceinline__ void value_row(uint32_t vs, int r, uint32_t (&w)[D / 32]) {
-        const int g = (threadIdx.x & 31) >> 2;
+    static __device__ __forceinline__ void value_row(uint32_t at, uint32_t (&w)[D / 32]) {
         if (D == 128) {
-            const uint4 u = lds16(vs + piece(r, g));
+            const uint4 u = lds16(at);
             w[0] = u.x, w[1] = u.y, w[D / 32 - 2] = u.z, w[D / 32 - 1] = u.w;
         } else {
-            const F2 u = lds8(vs + piece(r, g >> 1) + 8 * (g & 1));
+            const F2 u = lds8(at);
             w[0] = (uint32_t)u, w[1] = (uint32_t)(u >> 32);
         }
     }
     template <typename Rows>
     __device__ __forceinline__ void tile(uint32_t ks, uint32_t vs, float *, int key0, const Rows &seen, float, float *, int) {
         const int lane = threadIdx.x & 31, g = lane >> 2, t4 = lane & 3;
-        const uint32_t scales = vs + KT * kRow;
+        // piece() of row g's first part and of this lane's part of row 2 t; eight rows on it
+        // is the same, a step over D or an odd row the other 64 bytes of a line
+        uint32_t k_at = ks + piece(g, t4), v_at = vs + (D == 128 ? piece(2 * t4, g) : piece(2 * t4, g >> 1) + 8 * (g & 1));
+        uint32_t scales = vs + KT * kRow + 4 * g;
+        int base = key0;
 #pragma unroll 1
-        for (int sub = 0; sub < KT / 16; ++sub) {
-            const int base = key0 + 16 * sub, r = 16 * sub;
+        for (int sub = 0; sub < KT / 16; ++sub, base += 16, k_at += 16 * kRow, v_at += 16 * kRow, scales += 64) {
             if (sub > 0 && base >= seen.len) break;
             float s[NT][4], s2[NT][4];                   // even and odd steps over D: half the chain of products
 #pragma unroll
             for (int c = 0; c < D / 64; ++c) {
-                const uint4 x = lds16(ks + piece(r + g, 4 * c + t4)), y = lds16(ks + piece(r + g + 8, 4 * c + t4));
+                const uint4 x = lds16(k_at ^ 64 * c), y = lds16((k_at ^ 64 * c) + 8 * kRow);
                 const uint32_t xw[4] = {x.x, x.y, x.z, x.w}, yw[4] = {y.x, y.y, y.z, y.w};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
@@ -214,8 +219,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
                             mma_f16(k & 1 ? s2[t] : s[t], a, qf[k][i][t][0], qf[k][i][t][1], k < 2 && i == kQ - 1);
                 }
             }
-            const float k0 = lds4(scales + 4 * (r + g)), k1 = lds4(scales + 4 * (r + g + 8));
-            const float v0 = lds4(scales + 4 * (KT + r + g)), v1 = lds4(scales + 4 * (KT + r + g + 8));
+            const float k0 = lds4(scales), k1 = lds4(scales + 32), v0 = lds4(scales + 4 * KT), v1 = lds4(scales + 4 * KT + 32);
             const float e0 = whole_log2(v0), e1 = whole_log2(v1);
             const bool all = seen.sees_all(base, 16);
             const bool in0 = all || seen.sees(base + g), in1 = all || seen.sees(base + g + 8);
@@ -285,7 +289,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
             }
             uint32_t v[4][D / 32];                       // rows 2 t4, 2 t4 + 1, 2 t4 + 8, 2 t4 + 9
 #pragma unroll
-            for (int i = 0; i < 4; ++i) value_row(vs, r + 2 * t4 + (i & 1) + 8 * (i >> 1), v[i]);
+            for (int i = 0; i < 4; ++i) value_row((i & 1 ? (v_at ^ 64) + (D == 128 ? kRow : 0) : v_at) + (i >> 1) * 8 * kRow, v[i]);
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
                 const uint32_t pick = d & 1 ? 0x7362 : 0x5140;
