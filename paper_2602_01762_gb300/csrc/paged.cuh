@@ -100,7 +100,8 @@ struct StoreCodesArgs {
     const float *rope;
     const int32_t *pos, *n_new;
     int rope_len, B, max_new, Hkv;
-    int team, per, tasks;                // see store_codes_kernel
+    int team, per, tasks, span;          // see store_codes_kernel; tiles of a sequence
+    Divisor by_tasks, by_scale, by_page; // by tasks, scale_rows, page_size
     float eps;
     int *err;
 };
@@ -148,6 +149,7 @@ cudaError_t launch_code_attend(const AttendArgs &a, CodeFormat format, bool bf16
 cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
 int norm_rope_grad_ctas(int sms);
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t prepare_store_codes_kernels(bool bf16, int D);
 cudaError_t launch_store_codes(const StoreCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, cudaStream_t s);
 cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s);

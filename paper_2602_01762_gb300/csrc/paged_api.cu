@@ -192,6 +192,7 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
     if (e == cudaSuccess) e = prepare_attend_kernels(p->bf16, c.head_dim, G);
     if (e == cudaSuccess) e = prepare_window_attend_kernels(p->bf16, c.head_dim, G);
     if (e == cudaSuccess) e = prepare_code_attend_kernels(p->bf16, c.head_dim, G);
+    if (e == cudaSuccess) e = prepare_store_codes_kernels(p->bf16, c.head_dim);
     if (e == cudaSuccess) e = prepare_evict_kernels();
     if (e == cudaSuccess) e = prepare_rope_kernels();
     if (e != cudaSuccess) {

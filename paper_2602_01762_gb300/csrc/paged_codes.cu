@@ -22,7 +22,10 @@ namespace prism {
 namespace {
 
 constexpr int kScThreads = 128;
+constexpr int kScAngles = 64;            // rows of a tile whose angles are kept in shared memory, at most
 constexpr int kScKeep = 4;               // rows of a lane group kept in registers between a block's maximum and its codes
+constexpr int kScStage = kScKeep * 1024; // bytes of a warp's rows of one head: two pieces a lane and row
+constexpr int kScRing = kScThreads / 32 * 2 * kScStage;
 
 __device__ __forceinline__ void e4m3_values(uint32_t codes, float (&f)[4]) {
     uint32_t lo, hi;
@@ -63,79 +66,130 @@ template <int FORMAT> __device__ __forceinline__ float power_of_two(uint32_t top
     return top == 0 ? 0.f : __uint_as_float((uint32_t)max(e, 1) << 23);
 }
 
-// A team of a.team warps, or with a.per > 1 a part of a warp, per block, head and K or
-// V: rows of lanes as in the norm (E values at j and at j + D/2 each), the block's
-// largest value over the team, then the codes.  Up to kScKeep rows a lane group stay in
-// registers; longer blocks' further rows are read (from L2) and computed again.
-template <typename T, int D, int FORMAT>
-__global__ void __launch_bounds__(kScThreads) store_codes_kernel(StoreCodesArgs a) {
+// Larger of magnitudes; NaN if one is.
+__device__ __forceinline__ float top_of(float a, float b, float c) {
+    float d;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+    return d;
+}
+
+// A CTA per tile of rows, a block's or with a.per > 1 those of a.per short blocks that a
+// warp has side by side, and a.span of its heads of K or of V; what depends on the rows
+// alone (lengths, place, angles) is found once.  A team of a.team warps takes a head:
+// rows of lanes as in the norm (E values at j and at j + D/2 each), the block's largest
+// value over the team, then the codes, the next head's rows on their way meanwhile.  Up
+// to kScKeep rows a lane group stay in registers; longer blocks' further rows are read
+// and computed again.
+template <typename T, int D, int FORMAT, bool KEYS>
+__device__ __forceinline__ void store_tile(const StoreCodesArgs &a, const HeadsView &rows, char *pages, float *scales, int w0) {
     using R = Rope<T, D>;
     constexpr int N = R::N, E = R::E, kRows = R::kHeads;   // rows a warp has at a time
-    __shared__ uint32_t tops[kScThreads / 32];
-    pdl_wait();
-    pdl_trigger();
+    __shared__ float tops[2][kScThreads / 32];
+    extern __shared__ __align__(16) unsigned char dyn[];   // two stages a warp, then the angles
+    float *const angles = (float *)(dyn + kScRing);
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % R::kLanes, group = lane / R::kLanes;
-    const unsigned task = blockIdx.x * (kScThreads / 32 / a.team) + warp / a.team;
-    const unsigned run = task / (2u * a.Hkv), b = run / (unsigned)a.tasks;
-    if (b >= (unsigned)a.B) return;                      // whole teams
-    const int which = (int)(task - run * (2u * a.Hkv));
-    const bool is_k = which < a.Hkv;
-    const int h = is_k ? which : which - a.Hkv;
-    const int block = (int)(run - b * a.tasks) * a.per + (a.per > 1 ? group / a.scale_rows : 0);
-    const int step = kRows * a.team;                     // rows of the team at a time
-    const int j0 = a.per > 1 ? group % a.scale_rows : warp % a.team * kRows + group;
-    // the block's rows are slots first + j, 0 <= j < scale_rows; new ones from j_new on, up to j_end
-    const int len = a.cache.kv_len[b], n = row_count(a.n_new, b, a.max_new, a.err);
-    const long long first = ((long long)(len < 0 ? 0 : len) / a.scale_rows + block) * a.scale_rows;
-    const int j_new = first < len ? (int)(len - first) : 0;
-    long long end = len + (long long)n - first;
-    int j_end = (int)(end < 0 ? 0 : end > a.scale_rows ? a.scale_rows : end);
+    const int team = warp / a.team, teams = kScThreads / 32 / a.team, in_team = warp - team * a.team;
+    const int b = a.by_tasks.of((int)blockIdx.x), tile = (int)blockIdx.x - b * a.tasks;
+    const int w1 = min(w0 + a.span, a.Hkv);
+    const int in_warp = a.per > 1 ? a.by_scale.of(group) : 0;    // this lane's block of the warp's
+    const int step = kRows * a.team, j0 = a.per > 1 ? group - in_warp * a.scale_rows : in_team * kRows + group;
+    // a block's rows are slots first + j, 0 <= j < scale_rows; new ones from j_new on, up to j_end
+    const int held = a.cache.kv_len[b], cap = a.cache.table_pages * a.cache.page_size, pos = KEYS ? a.pos[b] : 0;
+    const bool fits = held >= 0 && held <= cap;          // no slot beyond a length that does not is a row's
+    const int len = fits ? held : 0, n = row_count(a.n_new, b, a.max_new, a.err);
+    const int tile_first = (a.by_scale.of(len) + tile * a.per) * a.scale_rows, first = tile_first + in_warp * a.scale_rows;
+    const int j_new = max(len - first, 0), j_end = min(max(len + n - first, 0), a.scale_rows);
+    const int shift = first - len;                       // row j is new row j + shift
+    // turns of the warp with a new row, and this lane's rows in them
+    uint32_t turns = 1, mine = 0;
+    if (a.per == 1) {
+        turns = 0;
+#pragma unroll
+        for (int c = 0; c < kScKeep; ++c) {
+            const int at = c * step + in_team * kRows;
+            turns |= (at < j_end && at + kRows > j_new) << c;
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < kScKeep; ++c) mine |= (turns >> c & 1 && c * step + j0 >= j_new && c * step + j0 < j_end) << c;
+    const char *src = rows.p + (long long)b * rows.sb + (long long)(j0 + shift) * rows.st + sub * 16;
+    // this lane's rows of a head, requested before their place is known; each lane copies
+    // what it reads itself, so that its own waits are enough
+    const uint32_t ring = (uint32_t)__cvta_generic_to_shared(dyn) + warp * (2 * kScStage) + lane * 16;
+    auto fetch = [&](int w, int stage) {
+        if (w < w1) {
+            const char *from = src + w * rows.sh;
+#pragma unroll
+            for (int c = 0; c < kScKeep; ++c) {
+                if (mine >> c & 1) {
+                    cp16(ring + stage * kScStage + c * 1024, from, true);
+                    cp16(ring + stage * kScStage + c * 1024 + 512, from + D / 2 * sizeof(T), true);
+                }
+                from += step * rows.st;
+            }
+        }
+        cp_group();
+    };
+    int w = w0 + team;
+    fetch(w, 0);
     int page = 0, row = 0;
-    if (j_new < j_end) {
-        if (len < 0 || first >= (long long)a.cache.table_pages * a.cache.page_size) {
+    bool live = j_new < j_end;
+    if (live) {
+        if (!fits || first >= cap) {
             set_err(a.err, kErrCache);
-            j_end = 0;
+            live = false;
         } else {
-            const int slot = (int)(first / a.cache.page_size);
-            row = (int)(first - (long long)slot * a.cache.page_size);
+            const int slot = a.by_page.of(first);
+            row = first - slot * a.cache.page_size;
             page = a.cache.table[(long long)b * a.cache.table_pages + slot];
             if ((unsigned)page >= (unsigned)a.cache.n_pages) {
                 set_err(a.err, kErrPage);
-                j_end = 0;
+                live = false;
             }
         }
     }
-    if (len < 0 && n > 0) set_err(a.err, kErrCache);
-    const bool live = j_new < j_end;
-    if (a.per > 1 ? !__any_sync(0xFFFFFFFFu, live) : !live) return;
-
-    const HeadsView &from = is_k ? a.k : a.v;
-    const char *src = from.p + (long long)b * from.sb + h * from.sh + sub * 16;
-    const int shift = (int)(first - len);                // row j is new row j + shift
+    if (!__any_sync(0xFFFFFFFFu, live)) {                // the same for every warp of the CTA
+        cp_wait_group<0>();
+        return;
+    }
+    if (!live) mine = 0;
+    float *const scale_at = scales + (long long)page * a.Hkv * a.scale_blocks + a.by_scale.of(row);
+    float before = live && j_new > 0 && w < w1 ? scale_at[(long long)w * a.scale_blocks] : 0.f;
+    // the rows' angles, of a tile's first kScAngles rows
+    auto position = [&](int i) {                         // of new row i, held to the table
+        const long long at = (long long)pos + i;
+        if (at >= 0 && at < a.rope_len) return (int)at;
+        set_err(a.err, kErrPosition);
+        return at < 0 ? 0 : a.rope_len - 1;
+    };
     Gain<T, D> gain;
-    const bool norm = is_k && a.g_k != nullptr;
-    if (norm) gain.load(a.g_k);
-    // Row j's values, zeros where it is none of the new ones.
-    auto load = [&](int j, F2 (&x)[N], F2 (&y)[N]) {
-        const bool in = live && j >= j_new && j < j_end;
-        const int i = in ? j + shift : 0;
-        uint4 l = make_uint4(0u, 0u, 0u, 0u), r = l;
-        if (in) {
-            l = *(const uint4 *)(src + i * from.st);
-            r = *(const uint4 *)(src + i * from.st + D / 2 * sizeof(T));
+    const bool norm = a.g_k != nullptr;
+    if (KEYS) {
+        if (norm) gain.load(a.g_k);
+        const int count = min(a.per > 1 ? kRows : a.scale_rows, kScAngles);
+        for (int e = threadIdx.x; e < count * (D / 4); e += kScThreads) {
+            const int i = tile_first + e / (D / 4) - len;
+            if (i >= 0 && i < n) *(float4 *)(angles + 4 * e) = __ldg((const float4 *)(a.rope + (long long)position(i) * D) + e % (D / 4));
         }
+        __syncthreads();
+    }
+    const uint32_t angles_at = (uint32_t)__cvta_generic_to_shared(angles);
+    // Row j's values from what was read of it.
+    auto values = [&](int j, bool in, const uint4 &l, const uint4 &r, F2 (&x)[N], F2 (&y)[N]) {
         Pairs<T>::unpack(l, x);
         Pairs<T>::unpack(r, y);
-        if (!is_k) return;
+        if (!KEYS) return;
         R rope;
-        rope.load(a.rope, in ? row_position(a.pos, b, i, a.rope_len, a.err) : 0);
+        const int at = !in ? 0 : a.per > 1 ? group : j;   // a turn's last rows may be past the block's
+        if (at < kScAngles) rope.load_shared(angles_at + at * (D * 4));
+        else rope.load(a.rope, in ? position(j + shift) : 0);
         if (norm) {
             F2 s = f2_mul(x[0], x[0]);
 #pragma unroll
             for (int e = 1; e < N; ++e) s = f2_fma(x[e], x[e], s);
 #pragma unroll
             for (int e = 0; e < N; ++e) s = f2_fma(y[e], y[e], s);
-            const float f = in ? rsqrtf(lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + a.eps) : (lanes_sum<R::kLanes>(f2_sum(s)), 0.f);
+            const float f = rsqrtf(lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + a.eps);
             const F2 ff = f2(f, f);
 #pragma unroll
             for (int e = 0; e < N; ++e) {
@@ -149,116 +203,143 @@ __global__ void __launch_bounds__(kScThreads) store_codes_kernel(StoreCodesArgs 
             y[e] = f2_fma(y[e], rope.cs[e], f2_mul(x[e], rope.sn[e]));
             x[e] = p;
         }
-        if (!in)
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = y[e] = 0ull;
     };
-    uint32_t top = 0, odd = 0;                           // bits of the largest finite magnitude; whether any is not finite
-    auto look = [&](const F2 (&x)[N], const F2 (&y)[N]) {
+    auto magnitude = [&](const F2 (&x)[N], const F2 (&y)[N], float top) {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float2 u = f2_values(x[e]), v = f2_values(y[e]);
+            top = top_of(u.x, u.y, top_of(v.x, v.y, top));
+        }
+        return top;
+    };
+    auto finite = [&](const F2 (&x)[N], const F2 (&y)[N], float top) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float2 u = f2_values(x[e]), v = f2_values(y[e]);
             const float f[4] = {u.x, u.y, v.x, v.y};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const uint32_t bits = __float_as_uint(f[i]) & 0x7FFFFFFFu;
-                if (bits < 0x7F800000u) top = max(top, bits);
-                else odd = 1;
-            }
+            for (int i = 0; i < 4; ++i)
+                if (fabsf(f[i]) < INFINITY) top = fmaxf(top, fabsf(f[i]));
         }
+        return top;
     };
-    F2 x[kScKeep][N], y[kScKeep][N];
-#pragma unroll
-    for (int c = 0; c < kScKeep; ++c) {
-        // whole warps: a team's rows of one turn
-        const int turn = c * step + (a.per > 1 ? 0 : warp % a.team * kRows);
-        if (a.per > 1 ? c == 0 : turn < j_end && turn + kRows > j_new) {
-            load(c * step + j0, x[c], y[c]);
-            look(x[c], y[c]);
-        }
-    }
-    if (a.per == 1)
-        for (int c = kScKeep; c * step < j_end; ++c) {
-            F2 u[N], v[N];
-            load(c * step + j0, u, v);
-            look(u, v);
-        }
+    // further rows of a long block, read and computed once more wherever they are asked for
+    auto further = [&](int w, const auto &f) {
+        if (a.per == 1)
+            for (int c = kScKeep; c * step < j_end; ++c) {
+                const bool in = c * step + j0 >= j_new && c * step + j0 < j_end;
+                uint4 l = make_uint4(0u, 0u, 0u, 0u), r = l;
+                if (in) {
+                    const char *from = src + w * rows.sh + c * step * rows.st;
+                    l = *(const uint4 *)from;
+                    r = *(const uint4 *)(from + D / 2 * sizeof(T));
+                }
+                F2 u[N], v[N];
+                values(c * step + j0, in, l, r, u, v);
+                if (in) f(c * step + j0, u, v);
+            }
+    };
     const int width = a.per > 1 ? R::kLanes * a.scale_rows : 32;   // lanes of a block
-    top |= odd << 31;                                    // the maximum carries both
-    {
-        uint32_t any = top >> 31, most = top & 0x7FFFFFFFu;
-        for (int o = width / 2; o > 0; o >>= 1) {
-            most = max(most, __shfl_xor_sync(0xFFFFFFFFu, most, o));
-            any |= __shfl_xor_sync(0xFFFFFFFFu, any, o);
-        }
-        top = most | any << 31;
-    }
-    if (a.team > 1) {
-        if (lane == 0) tops[warp] = top;
-        asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / a.team), "r"(32 * a.team) : "memory");
-        const int base = warp / a.team * a.team;
-        for (int w = 0; w < a.team; ++w) {
-            const uint32_t t = tops[base + w];
-            top = max(top & 0x7FFFFFFFu, t & 0x7FFFFFFFu) | ((top | t) & 0x80000000u);
-        }
-    }
-    const bool any_odd = top >> 31;
-    float *scale_at = (is_k ? a.k_scales : a.v_scales) + ((long long)page * a.Hkv + h) * a.scale_blocks + row / a.scale_rows;
-    const float before = live && j_new > 0 ? *scale_at : 0.f;
-    // every thread has read the scale before it is written
-    if (a.team > 1) asm volatile("bar.sync %0, %1;" ::"r"(1 + warp / a.team), "r"(32 * a.team) : "memory");
-    else __syncwarp();
-    if (!live) return;
-    float s = power_of_two<FORMAT>(top & 0x7FFFFFFFu);
-    if (FORMAT == kInt8 && any_odd) s = __int_as_float(0x7FFFFFFF);   // int8 has no code for it: the block reads as NaN
-    if (!(before < s) && !(s != s)) s = before;          // a NaN stays one
-    const float per_s = s > 0.f ? 1.f / s : 0.f;
-    char *to = (is_k ? a.cache.k : a.cache.v) + page * a.cache.page_stride + h * a.cache.head_stride + row * a.cache.row_stride;
-    const int in_team = a.per > 1 ? lane % width : warp % a.team * 32 + lane, threads = a.per > 1 ? width : 32 * a.team;
-    if (in_team == 0 && (j_new == 0 || s != before)) *scale_at = s;
-    if (j_new > 0 && before < s) {                       // earlier rows in the grown scale
-        const float f = before / s;
-#pragma unroll 4
-        for (int e = in_team; e < j_new * (D / 4); e += threads) {
-            uint32_t *p = (uint32_t *)(to + e / (D / 4) * a.cache.row_stride) + e % (D / 4);
-            float v[4];
-            decode<FORMAT>(*p, v);
-            *p = encode<FORMAT>(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-        }
-    }
-    auto put = [&](int j, const F2 (&x)[N], const F2 (&y)[N]) {
-        if (j < j_new || j >= j_end) return;
-        float f[2][E];
+    const int thread = a.per > 1 ? lane % width : in_team * 32 + lane, threads = a.per > 1 ? width : 32 * a.team;
+    const long long page_at = page * a.cache.page_stride + row * a.cache.row_stride;
+    for (int turn = 0; w < w1; w += teams, turn ^= 1) {
+        const float was = before;
+        fetch(w + teams, turn ^ 1);
+        if (w + teams < w1) before = live && j_new > 0 ? scale_at[(long long)(w + teams) * a.scale_blocks] : 0.f;
+        cp_wait_group<1>();
+        F2 x[kScKeep][N], y[kScKeep][N];
+        float top = 0.f;
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            const float2 u = f2_values(x[e]), v = f2_values(y[e]);
-            f[0][2 * e] = u.x, f[0][2 * e + 1] = u.y, f[1][2 * e] = v.x, f[1][2 * e + 1] = v.y;
-        }
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            uint32_t w[E / 4];
-            if (any_odd) {                               // e4m3: infinities become NaN
-#pragma unroll
-                for (int e = 0; e < E; ++e)
-                    if (!(fabsf(f[i][e]) < INFINITY)) f[i][e] = FORMAT == kE4m3 ? __int_as_float(0x7FFFFFFF) : 0.f;
+        for (int c = 0; c < kScKeep; ++c)
+            if (turns >> c & 1) {                        // rows that are not new hold anything: their values are not used
+                const uint32_t at = ring + turn * kScStage + c * 1024;
+                values(c * step + j0, mine >> c & 1, lds16(at), lds16(at + 512), x[c], y[c]);
+                if (mine >> c & 1) top = magnitude(x[c], y[c], top);
             }
+        further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N]) { top = magnitude(u, v, top); });
+        // over the block's lanes, then the team's warps; of a block with a NaN or an infinity
+        // the largest finite value, with the sign bit for a mark
+        for (int o = width / 2; o > 0; o >>= 1) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, o), 0.f);
+        if (__any_sync(0xFFFFFFFFu, !(top < INFINITY))) {
+            const bool odd = !(top < INFINITY);
+            float t = 0.f;
 #pragma unroll
-            for (int e = 0; e < E / 4; ++e)
-                w[e] = encode<FORMAT>(f[i][4 * e] * per_s, f[i][4 * e + 1] * per_s, f[i][4 * e + 2] * per_s, f[i][4 * e + 3] * per_s);
-            char *at = to + j * a.cache.row_stride + i * (D / 2) + sub * E;
-            if (E == 8) *(uint2 *)at = make_uint2(w[0], w[E / 4 - 1]);
-            else *(uint32_t *)at = w[0];
+            for (int c = 0; c < kScKeep; ++c)
+                if (mine >> c & 1) t = finite(x[c], y[c], t);
+            further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N]) { t = finite(u, v, t); });
+            for (int o = width / 2; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, o));
+            top = odd ? -t : t;
         }
-    };
+        if (a.team > 1) {
+            if (lane == 0) tops[turn][warp] = top;
+            asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * a.team) : "memory");
+            uint32_t mark = 0;
+            float most = 0.f;
+            for (int i = 0; i < a.team; ++i) {
+                most = fmaxf(most, fabsf(tops[turn][team * a.team + i]));
+                mark |= __float_as_uint(tops[turn][team * a.team + i]) & 0x80000000u;
+            }
+            top = __uint_as_float(__float_as_uint(most) | mark);
+        } else {
+            __syncwarp();                                // every lane has read the scale before it is written
+        }
+        if (!live) continue;
+        const bool any_odd = __float_as_uint(top) >> 31;
+        float s = power_of_two<FORMAT>(__float_as_uint(top) & 0x7FFFFFFFu);
+        if (FORMAT == kInt8 && any_odd) s = __int_as_float(0x7FFFFFFF);   // int8 has no code for it: the block reads as NaN
+        if (!(was < s) && !(s != s)) s = was;            // a NaN stays one
+        const float per_s = s > 0.f ? 1.f / s : 0.f;
+        char *to = pages + w * a.cache.head_stride + page_at;
+        if (thread == 0 && (j_new == 0 || s != was)) scale_at[(long long)w * a.scale_blocks] = s;
+        if (j_new > 0 && was < s) {                      // earlier rows in the grown scale
+            const float f = was / s;
+#pragma unroll 4
+            for (int e = thread; e < j_new * (D / 4); e += threads) {
+                uint32_t *p = (uint32_t *)(to + e / (D / 4) * a.cache.row_stride) + e % (D / 4);
+                float v[4];
+                decode<FORMAT>(*p, v);
+                *p = encode<FORMAT>(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+            }
+        }
+        auto put = [&](int j, const F2 (&x)[N], const F2 (&y)[N]) {
 #pragma unroll
-    for (int c = 0; c < kScKeep; ++c)
-        if (a.per > 1 ? c == 0 : c * step < j_end) put(c * step + j0, x[c], y[c]);
-    if (a.per == 1)
-        for (int c = kScKeep; c * step < j_end; ++c) {
-            F2 u[N], v[N];
-            load(c * step + j0, u, v);
-            put(c * step + j0, u, v);
-        }
+            for (int i = 0; i < 2; ++i) {
+                uint32_t c[E / 4];
+#pragma unroll
+                for (int e = 0; e < E / 4; ++e) {
+                    F2 u = i ? y[2 * e] : x[2 * e], v = i ? y[2 * e + 1] : x[2 * e + 1];
+                    if (any_odd) {                       // e4m3: infinities become NaN
+                        float f[4] = {f2_values(u).x, f2_values(u).y, f2_values(v).x, f2_values(v).y};
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (!(fabsf(f[k]) < INFINITY)) f[k] = FORMAT == kE4m3 ? __int_as_float(0x7FFFFFFF) : 0.f;
+                        u = f2(f[0], f[1]), v = f2(f[2], f[3]);
+                    }
+                    const float2 p = f2_values(f2_mul(u, f2(per_s, per_s))), q = f2_values(f2_mul(v, f2(per_s, per_s)));
+                    c[e] = encode<FORMAT>(p.x, p.y, q.x, q.y);
+                }
+                char *at = to + j * a.cache.row_stride + i * (D / 2) + sub * E;
+                if (E == 8) *(uint2 *)at = make_uint2(c[0], c[E / 4 - 1]);
+                else *(uint32_t *)at = c[0];
+            }
+        };
+#pragma unroll
+        for (int c = 0; c < kScKeep; ++c)
+            if (mine >> c & 1) put(c * step + j0, x[c], y[c]);
+        further(w, put);
+    }
+}
+
+template <typename T, int D, int FORMAT>
+__global__ void __launch_bounds__(kScThreads, 3) store_codes_kernel(StoreCodesArgs a) {
+    // The queries' kernel, launched before this one, lets it start once its own wait is
+    // over: rows, lengths and cache are final, and the two run side by side.  The wait
+    // at the end makes this kernel's end the end of both.
+    pdl_trigger();
+    const int splits = gridDim.y / 2;                    // of the keys' heads, then of the values'
+    if ((int)blockIdx.y < splits) store_tile<T, D, FORMAT, true>(a, a.k, a.cache.k, a.k_scales, blockIdx.y * a.span);
+    else store_tile<T, D, FORMAT, false>(a, a.v, a.cache.v, a.v_scales, (blockIdx.y - splits) * a.span);
+    pdl_wait();
 }
 
 // Rows read back, 16 bytes of the result a lane: a CTA takes kRcRows rows of a
@@ -347,17 +428,38 @@ template <typename F> cudaError_t with_codes(CodeFormat format, bool bf16, int D
 
 }  // namespace
 
-cudaError_t launch_store_codes(const StoreCodesArgs &args, CodeFormat format, bool bf16, int D, int, cudaStream_t s) {
+cudaError_t prepare_store_codes_kernels(bool bf16, int D) {
+    cudaError_t e = cudaSuccess;
+    for (const CodeFormat format : {kE4m3, kInt8})
+        if (e == cudaSuccess)
+            e = with_codes(format, bf16, D, [&](auto t, auto d, auto form) {
+                return cudaFuncSetAttribute(store_codes_kernel<decltype(t), d, form>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                            kScRing + 4 * D * kScAngles);
+            });
+    return e;
+}
+
+cudaError_t launch_store_codes(const StoreCodesArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
     StoreCodesArgs a = args;
     const int rows = 32 / (D / 2 / (bf16 ? 8 : 4)), R = a.scale_rows;   // rows a warp has at a time
     a.per = R < rows && rows % R == 0 ? rows / R : 1;
-    a.team = R <= kScKeep * rows ? 1 : R <= 2 * kScKeep * rows ? 2 : 4;
+    a.team = 1;
+    while (a.team < kScThreads / 32 && a.team * kScKeep * rows < R) a.team *= 2;
     const long long blocks = (a.max_new + 2LL * R - 2) / R;              // that a sequence's new rows may touch
     a.tasks = (int)((blocks + a.per - 1) / a.per);
-    const long long warps = (long long)a.B * a.tasks * 2 * a.Hkv * a.team;
-    const dim3 grid((unsigned)((warps + kScThreads / 32 - 1) / (kScThreads / 32)));
+    a.by_tasks = Divisor((uint32_t)a.tasks);
+    a.by_scale = Divisor((uint32_t)R), a.by_page = Divisor((uint32_t)a.cache.page_size);
+    // heads of a CTA: fewer than all where the tiles alone give an SM less than four CTAs
+    const long long tiles = (long long)a.B * a.tasks;
+    const int teams = kScThreads / 32 / a.team;
+    int splits = 1;
+    while (splits * tiles < 2LL * sms && splits * teams < a.Hkv) splits *= 2;
+    a.span = (a.Hkv + splits - 1) / splits;
+    const int angles = a.per > 1 ? rows : R < kScAngles ? R : kScAngles;
+    const size_t shared = kScRing + sizeof(float) * D * angles;
+    const dim3 grid((unsigned)tiles, 2u * ((a.Hkv + a.span - 1) / a.span));
     return with_codes(format, bf16, D, [&](auto t, auto d, auto form) {
-        return launch_k(store_codes_kernel<decltype(t), d, form>, grid, dim3(kScThreads), 0, s, true, a);
+        return launch_k(store_codes_kernel<decltype(t), d, form>, grid, dim3(kScThreads), shared, s, true, a);
     });
 }
 
