@@ -51,6 +51,7 @@ struct NormRopeArgs {
     const float *rope;                   // [rope_len, 2, D/2]: cosines, then sines
     const int32_t *pos, *n_new;          // [B]; n_new null: max_new rows each
     int rope_len, B, max_new, Hq, Hkv, split, heads;   // heads: of a row that a warp takes at a time
+    int one_row;                         // and whether it takes one row
     float eps;
     int *err;
 };
@@ -100,8 +101,11 @@ struct StoreCodesArgs {
     const float *rope;
     const int32_t *pos, *n_new;
     int rope_len, B, max_new, Hkv;
-    int team, per, tasks, span;          // see store_codes_kernel; tiles of a sequence
-    Divisor by_tasks, by_scale, by_page; // by tasks, scale_rows, page_size
+    // see store_codes_kernel: tiles of a sequence, heads of a CTA, its CTAs of keys and as many
+    // of values to a tile, CTAs, and of how many CTAs one is theirs
+    int team, per, tasks, span, splits, ctas, every;
+    int beside;                          // the queries' kernel was launched before this one
+    Divisor by_tasks, by_tiles, by_every, by_scale, by_page;   // by tasks, B tasks, every, scale_rows, page_size
     float eps;
     int *err;
 };
@@ -146,11 +150,14 @@ cudaError_t prepare_int8_attend(bool bf16, int D, int G);
 cudaError_t start_e4m3_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t start_int8_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_code_attend(const AttendArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
+// CTAs, and split and heads of `a`.
+unsigned plan_norm_rope(NormRopeArgs &a, bool bf16, int D, bool append, int sms);
 cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
 int norm_rope_grad_ctas(int sms);
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t prepare_store_codes_kernels(bool bf16, int D);
-cudaError_t launch_store_codes(const StoreCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
+// Norm and rotation of the queries, and their keys and values into the cache.
+cudaError_t launch_store_codes(const NormRopeArgs &q, const StoreCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, cudaStream_t s);
 cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s);
 

@@ -311,12 +311,11 @@ prism_status prism_paged_append_codes(prism_paged *p, const prism_paged_cache *c
     if (!q.pos) q.pos = cache->kv_len;
     a.g_k = q.g_k, a.rope = q.rope, a.pos = q.pos, a.n_new = q.n_new, a.rope_len = q.rope_len, a.B = q.B, a.max_new = q.max_new, a.Hkv = q.Hkv;
     a.eps = q.eps, a.err = p->err;
-    q.Hkv = 0;                                   // the queries alone
+    q.Hkv = 0;                                   // the queries' part, the queries alone
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
-    cudaError_t e = launch_norm_rope(q, p->bf16, p->cfg.head_dim, false, p->sms, (cudaStream_t)stream);
-    if (e == cudaSuccess) e = launch_store_codes(a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream);
-    return cuda_status(p, e, "prism_paged_append_codes");
+    return cuda_status(p, launch_store_codes(q, a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream),
+                       "prism_paged_append_codes");
 }
 
 prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales,

@@ -81,15 +81,14 @@ __device__ __forceinline__ float top_of(float a, float b, float c) {
 // to kScKeep rows a lane group stay in registers; longer blocks' further rows are read
 // and computed again.
 template <typename T, int D, int FORMAT, bool KEYS>
-__device__ __forceinline__ void store_tile(const StoreCodesArgs &a, const HeadsView &rows, char *pages, float *scales, int w0) {
+__device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int w0, const HeadsView &rows, char *pages, float *scales, unsigned char *dyn) {
     using R = Rope<T, D>;
     constexpr int N = R::N, E = R::E, kRows = R::kHeads;   // rows a warp has at a time
     __shared__ float tops[2][kScThreads / 32];
-    extern __shared__ __align__(16) unsigned char dyn[];   // two stages a warp, then the angles
-    float *const angles = (float *)(dyn + kScRing);
+    float *const angles = (float *)(dyn + kScRing);      // behind two stages a warp
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % R::kLanes, group = lane / R::kLanes;
     const int team = warp / a.team, teams = kScThreads / 32 / a.team, in_team = warp - team * a.team;
-    const int b = a.by_tasks.of((int)blockIdx.x), tile = (int)blockIdx.x - b * a.tasks;
+    const int b = a.by_tasks.of(run), tile = run - b * a.tasks;
     const int w1 = min(w0 + a.span, a.Hkv);
     const int in_warp = a.per > 1 ? a.by_scale.of(group) : 0;    // this lane's block of the warp's
     const int step = kRows * a.team, j0 = a.per > 1 ? group - in_warp * a.scale_rows : in_team * kRows + group;
@@ -330,16 +329,25 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, const HeadsV
     }
 }
 
-template <typename T, int D, int FORMAT>
-__global__ void __launch_bounds__(kScThreads, 3) store_codes_kernel(StoreCodesArgs a) {
-    // The queries' kernel, launched before this one, lets it start once its own wait is
-    // over: rows, lengths and cache are final, and the two run side by side.  The wait
-    // at the end makes this kernel's end the end of both.
+// Every a.every-th CTA stores keys or values, a.ctas in all; the others, if any, norm and
+// rotate the queries.  With a.beside a kernel of their own does, launched before this
+// one, which lets it start once its own wait is over: rows, lengths and cache are final
+// then, the two run side by side, and the wait at the end makes this one's end the end of
+// both.
+template <typename T, int D, int FORMAT, bool ROWS>
+__global__ void __launch_bounds__(kScThreads, 3) store_codes_kernel(NormRopeArgs q, StoreCodesArgs a) {
+    extern __shared__ __align__(16) unsigned char dyn[];
+    if (!a.beside) pdl_wait();
     pdl_trigger();
-    const int splits = gridDim.y / 2;                    // of the keys' heads, then of the values'
-    if ((int)blockIdx.y < splits) store_tile<T, D, FORMAT, true>(a, a.k, a.cache.k, a.k_scales, blockIdx.y * a.span);
-    else store_tile<T, D, FORMAT, false>(a, a.v, a.cache.v, a.v_scales, (blockIdx.y - splits) * a.span);
-    pdl_wait();
+    const int i = (int)blockIdx.x, turn = a.by_every.of(i);
+    if (turn * a.every == i && turn < a.ctas) {
+        const int y = a.by_tiles.of(turn), run = turn - y * a.B * a.tasks;   // the keys' CTAs, which take longer, first
+        if (y < a.splits) store_tile<T, D, FORMAT, true>(a, run, y * a.span, a.k, a.cache.k, a.k_scales, dyn);
+        else store_tile<T, D, FORMAT, false>(a, run, (y - a.splits) * a.span, a.v, a.cache.v, a.v_scales, dyn);
+    } else {
+        norm_rope_rows<T, D, false, ROWS>(q, (unsigned)(i - min(turn + 1, a.ctas)), dyn);
+    }
+    if (a.beside) pdl_wait();
 }
 
 // Rows read back, 16 bytes of the result a lane: a CTA takes kRcRows rows of a
@@ -430,36 +438,54 @@ template <typename F> cudaError_t with_codes(CodeFormat format, bool bf16, int D
 
 cudaError_t prepare_store_codes_kernels(bool bf16, int D) {
     cudaError_t e = cudaSuccess;
+    auto set = [&](auto k) {
+        return e != cudaSuccess ? e : cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, kScRing + 4 * D * kScAngles);
+    };
     for (const CodeFormat format : {kE4m3, kInt8})
-        if (e == cudaSuccess)
-            e = with_codes(format, bf16, D, [&](auto t, auto d, auto form) {
-                return cudaFuncSetAttribute(store_codes_kernel<decltype(t), d, form>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                            kScRing + 4 * D * kScAngles);
-            });
+        e = with_codes(format, bf16, D, [&](auto t, auto d, auto form) {
+            e = set(store_codes_kernel<decltype(t), d, form, false>);
+            return set(store_codes_kernel<decltype(t), d, form, true>);
+        });
     return e;
 }
 
-cudaError_t launch_store_codes(const StoreCodesArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
+cudaError_t launch_store_codes(const NormRopeArgs &queries, const StoreCodesArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
+    NormRopeArgs q = queries;
     StoreCodesArgs a = args;
+    static_assert(kNrThreads == kScThreads && kNrShared <= kScRing, "one launch");
+    unsigned others = plan_norm_rope(q, bf16, D, false, sms);
     const int rows = 32 / (D / 2 / (bf16 ? 8 : 4)), R = a.scale_rows;   // rows a warp has at a time
     a.per = R < rows && rows % R == 0 ? rows / R : 1;
     a.team = 1;
     while (a.team < kScThreads / 32 && a.team * kScKeep * rows < R) a.team *= 2;
     const long long blocks = (a.max_new + 2LL * R - 2) / R;              // that a sequence's new rows may touch
     a.tasks = (int)((blocks + a.per - 1) / a.per);
-    a.by_tasks = Divisor((uint32_t)a.tasks);
-    a.by_scale = Divisor((uint32_t)R), a.by_page = Divisor((uint32_t)a.cache.page_size);
     // heads of a CTA: fewer than all where the tiles alone give an SM less than four CTAs
     const long long tiles = (long long)a.B * a.tasks;
     const int teams = kScThreads / 32 / a.team;
     int splits = 1;
     while (splits * tiles < 2LL * sms && splits * teams < a.Hkv) splits *= 2;
     a.span = (a.Hkv + splits - 1) / splits;
+    a.splits = (a.Hkv + a.span - 1) / a.span;
+    a.ctas = (int)(tiles * 2 * a.splits);
+    // one launch where all of it runs at once, else the queries' rows on a kernel that takes
+    // less of an SM.  Measured, 32 query and 8 KV heads: 16 rows 3.7 and 4.1 us (and 2 us of a
+    // launch), 8 prompts of 1021 to 2048 rows 67.5 and 57 us.
+    a.beside = a.ctas + (long long)others > 3LL * sms;
+    if (a.beside) {
+        const cudaError_t e = launch_norm_rope(queries, bf16, D, false, sms, s);
+        if (e != cudaSuccess) return e;
+        others = 0;
+    }
+    a.every = (int)((a.ctas + (long long)others) / a.ctas);
+    a.by_tasks = Divisor((uint32_t)a.tasks), a.by_tiles = Divisor((uint32_t)tiles), a.by_every = Divisor((uint32_t)a.every);
+    a.by_scale = Divisor((uint32_t)R), a.by_page = Divisor((uint32_t)a.cache.page_size);
     const int angles = a.per > 1 ? rows : R < kScAngles ? R : kScAngles;
     const size_t shared = kScRing + sizeof(float) * D * angles;
-    const dim3 grid((unsigned)tiles, 2u * ((a.Hkv + a.span - 1) / a.span));
+    const dim3 grid((unsigned)a.ctas + others);
     return with_codes(format, bf16, D, [&](auto t, auto d, auto form) {
-        return launch_k(store_codes_kernel<decltype(t), d, form>, grid, dim3(kScThreads), shared, s, true, a);
+        using T = decltype(t);
+        return launch_k(q.one_row ? store_codes_kernel<T, d, form, false> : store_codes_kernel<T, d, form, true>, grid, dim3(kScThreads), shared, s, true, q, a);
     });
 }
 
