@@ -116,7 +116,8 @@ struct ReadCodesArgs {
     const float *k_scales, *v_scales;
     int scale_rows, scale_blocks;
     const int32_t *start, *n_rows;       // [B]; null: 0, max_rows
-    int B, max_rows, Hkv;
+    int B, max_rows, Hkv, span;          // span: heads of a CTA
+    Divisor by_chunks, by_scale, by_page;   // by CTAs' row chunks of a sequence, scale_rows, page_size
     int *err;
 };
 
@@ -158,7 +159,7 @@ cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, i
 cudaError_t prepare_store_codes_kernels(bool bf16, int D);
 // Norm and rotation of the queries, and their keys and values into the cache.
 cudaError_t launch_store_codes(const NormRopeArgs &q, const StoreCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
-cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, cudaStream_t s);
+cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_paged_evict(const EvictArgs &a, int row_bytes, int sms, cudaStream_t s);
 
 // Launch in clusters of cs CTAs, with programmatic stream serialization.

@@ -336,7 +336,7 @@ prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cac
     a.start = start, a.n_rows = n_rows, a.B = cache->batch, a.max_rows = max_rows, a.Hkv = p->cfg.n_kv_heads, a.err = p->err;
     OnDevice on(p->device);
     if (on.e != cudaSuccess) return cuda_status(p, on.e, "cudaSetDevice");
-    return cuda_status(p, launch_read_codes(a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, (cudaStream_t)stream), "prism_paged_read_codes");
+    return cuda_status(p, launch_read_codes(a, (CodeFormat)scales->format, p->bf16, p->cfg.head_dim, p->sms, (cudaStream_t)stream), "prism_paged_read_codes");
 }
 
 prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,

@@ -351,7 +351,7 @@ __global__ void __launch_bounds__(kScThreads, 3) store_codes_kernel(NormRopeArgs
 }
 
 // Rows read back, 16 bytes of the result a lane: a CTA takes kRcRows rows of a
-// sequence and walks over their heads.
+// sequence and walks over a.span of their heads.
 constexpr int kRcThreads = 256;
 constexpr int kRcRows = 16;
 template <typename T, int D, int FORMAT>
@@ -360,35 +360,35 @@ __global__ void __launch_bounds__(kRcThreads) read_codes_kernel(ReadCodesArgs a)
     constexpr int kAhead = 4;            // rows and heads of a lane at a time, K and V of each
     pdl_wait();
     pdl_trigger();
-    const unsigned chunks = (a.max_rows + kRcRows - 1) / (unsigned)kRcRows, b = blockIdx.x / chunks;
-    const int i0 = (int)(blockIdx.x - b * chunks) * kRcRows;
+    const int b = a.by_chunks.of((int)blockIdx.x), i0 = ((int)blockIdx.x - b * (int)a.by_chunks.d) * kRcRows;
+    const int h0 = blockIdx.y * a.span, h1 = min(h0 + a.span, a.Hkv);
     const int n = min(row_count(a.n_rows, b, a.max_rows, a.err), i0 + kRcRows) - i0;
     if (n <= 0) return;
     const long long start = (a.start ? a.start[b] : 0) + (long long)i0, cap = (long long)a.cache.table_pages * a.cache.page_size;
     const int sub = threadIdx.x % kLanes;
-    for (int e0 = threadIdx.x / kLanes; e0 < kRcRows * a.Hkv; e0 += kAhead * kGroups) {
+    for (int e0 = threadIdx.x / kLanes; e0 < kRcRows * (h1 - h0); e0 += kAhead * kGroups) {
         uint32_t c[kAhead][2][E / 4];
         float s[kAhead][2];
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int e = e0 + u * kGroups, r = e % kRcRows, h = e / kRcRows;
+            const int e = e0 + u * kGroups, r = e % kRcRows, h = h0 + e / kRcRows;
             s[u][0] = s[u][1] = 0.f;
 #pragma unroll
             for (int w = 0; w < E / 4; ++w) c[u][0][w] = c[u][1][w] = 0u;
-            if (h >= a.Hkv || r >= n) continue;
+            if (h >= h1 || r >= n) continue;
             const long long slot = start + r;
             if (slot < 0 || slot >= cap) {
                 set_err(a.err, kErrCache);
                 continue;
             }
-            const int idx = (int)slot / a.cache.page_size, row = (int)slot - idx * a.cache.page_size;
+            const int idx = a.by_page.of((int)slot), row = (int)slot - idx * a.cache.page_size;
             const int page = a.cache.table[(long long)b * a.cache.table_pages + idx];
             if ((unsigned)page >= (unsigned)a.cache.n_pages) {
                 set_err(a.err, kErrPage);
                 continue;
             }
             const long long at = page * a.cache.page_stride + h * a.cache.head_stride + row * a.cache.row_stride + sub * E;
-            const long long scale = ((long long)page * a.Hkv + h) * a.scale_blocks + row / a.scale_rows;
+            const long long scale = ((long long)page * a.Hkv + h) * a.scale_blocks + a.by_scale.of(row);
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 const char *p = (kv ? a.cache.v : a.cache.k) + at;
@@ -403,8 +403,8 @@ __global__ void __launch_bounds__(kRcThreads) read_codes_kernel(ReadCodesArgs a)
         }
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
-            const int e = e0 + u * kGroups, r = e % kRcRows, h = e / kRcRows;
-            if (h >= a.Hkv || r >= n) continue;
+            const int e = e0 + u * kGroups, r = e % kRcRows, h = h0 + e / kRcRows;
+            if (h >= h1 || r >= n) continue;
 #pragma unroll
             for (int kv = 0; kv < 2; ++kv) {
                 float f[E];
@@ -489,8 +489,15 @@ cudaError_t launch_store_codes(const NormRopeArgs &queries, const StoreCodesArgs
     });
 }
 
-cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, cudaStream_t s) {
-    const dim3 grid((unsigned)a.B * ((a.max_rows + kRcRows - 1) / kRcRows));
+cudaError_t launch_read_codes(const ReadCodesArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
+    ReadCodesArgs a = args;
+    const unsigned chunks = (a.max_rows + kRcRows - 1) / (unsigned)kRcRows;
+    // fewer heads a CTA where there would be less than one to an SM
+    int splits = 1;
+    while (splits < a.Hkv && (long long)a.B * chunks * splits < sms) splits *= 2;
+    a.span = (a.Hkv + splits - 1) / splits;
+    a.by_chunks = Divisor(chunks), a.by_scale = Divisor((uint32_t)a.scale_rows), a.by_page = Divisor((uint32_t)a.cache.page_size);
+    const dim3 grid(a.B * chunks, (unsigned)((a.Hkv + a.span - 1) / a.span));
     return with_codes(format, bf16, D, [&](auto t, auto d, auto form) {
         return launch_k(read_codes_kernel<decltype(t), d, form>, grid, dim3(kRcThreads), 0, s, true, a);
     });

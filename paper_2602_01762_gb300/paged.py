@@ -68,7 +68,7 @@ _CODES = {torch.float8_e4m3fn: 0, torch.int8: 1}
 # prism_rows (five strided tensors of four words, five addresses, three sizes) and
 # prism_row_grads (four strided tensors, two addresses)
 _ROWS, _GRADS = struct.Struct("=20q5Q3i4x"), struct.Struct("=16q2Q")
-_HEADS = struct.Struct("=4q")        # prism_heads
+_HEADS2 = struct.Struct("=8q")       # two prism_heads
 _NONE = (0, 0, 0, 0)
 
 
@@ -147,8 +147,9 @@ class PagedAttention:
         self.h = h
         self._index, self._dims = self.device.index, (head_dim,)
         self._rows, self._grads = ctypes.create_string_buffer(_ROWS.size), ctypes.create_string_buffer(_GRADS.size)
-        self._k_rows, self._v_rows = ctypes.create_string_buffer(_HEADS.size), ctypes.create_string_buffer(_HEADS.size)
-        self._k_rows_at, self._v_rows_at = ctypes.addressof(self._k_rows), ctypes.addressof(self._v_rows)
+        self._kv_rows = ctypes.create_string_buffer(_HEADS2.size)
+        self._k_rows_at = ctypes.addressof(self._kv_rows)
+        self._v_rows_at = self._k_rows_at + _HEADS2.size // 2
         self._rows_at, self._grads_at = ctypes.addressof(self._rows), ctypes.addressof(self._grads)
         self._key = (self.tdtype, self.device, (n_kv_heads, page_size, head_dim))
 
@@ -327,8 +328,7 @@ class PagedAttention:
             raise ValueError("read: the cache is not held in 8 bits")
         B, n = cache.batch, k_out.shape[1]
         shape = (B, n, self.n_kv_heads, self.head_dim)
-        _HEADS.pack_into(self._k_rows, 0, *self._heads(k_out, shape, "k_out"))
-        _HEADS.pack_into(self._v_rows, 0, *self._heads(v_out, shape, "v_out"))
+        _HEADS2.pack_into(self._kv_rows, 0, *self._heads(k_out, shape, "k_out"), *self._heads(v_out, shape, "v_out"))
         self._check(self.lib.prism_paged_read_codes(
             self.h, ref, cache.scales_ref, None if start is None else self._tensor(start, (B,), torch.int32, "start"),
             None if n_rows is None else self._tensor(n_rows, (B,), torch.int32, "n_rows"), n, self._k_rows_at, self._v_rows_at,
