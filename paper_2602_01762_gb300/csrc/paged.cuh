@@ -3,26 +3,13 @@
 #pragma once
 
 #include "common.cuh"
+#include "paged_rows.h"
 
 namespace prism {
 
 enum PagedErr : int {
     kErrPage = 16,      // a block-table entry outside the pool
     kErrPosition = 32,  // a rotary position outside the table
-};
-
-// Division of n < 2^31 by a divisor that the launch knows: floor(n / d) = (floor(n m / 2^32)
-// + n) / 2^s with s = ceil(log2 d) and m = floor(2^32 (2^s - d) / d) + 1.
-struct Divisor {
-    uint32_t d, m, s;
-    Divisor() = default;
-    explicit Divisor(uint32_t by) : d(by), m(0), s(0) {
-        while (s < 31 && (1u << s) < d) ++s;
-        m = (uint32_t)((((1ull << s) - d) << 32) / d + 1);
-    }
-#ifdef __CUDACC__
-    __device__ __forceinline__ int of(int n) const { return (int)((__umulhi((uint32_t)n, m) + (uint32_t)n) >> s); }
-#endif
 };
 
 enum CodeFormat : int { kE4m3 = 0, kInt8 = 1 };
@@ -129,7 +116,6 @@ struct EvictArgs {
     int *err;
 };
 
-constexpr int kAttendUnit = 64;          // keys per unit of the attention's work split
 constexpr int kAttendCost = 1;           // units that a segment costs beside its keys, at least
 // Query heads that share a pass over the rows; the most passes over a KV head's rows
 // that its G query heads take.

@@ -54,8 +54,7 @@ __device__ __forceinline__ float base_of(float m) { return m == -INFINITY ? 0.f 
 // beside its rows (its queries, merge and result).
 __device__ __forceinline__ int blocks_of(int len) { return max(1, (len + kAttendUnit - 1) / kAttendUnit); }
 
-// The rows of a sequence that are attended to, in blocks side by side: `count` rows
-// from place 0 on, of which place r is row key(r) and counts where it is seen.
+// The rows of a sequence that are attended to (paged_rows.h).
 struct AllRows {
     int len;
     __device__ __forceinline__ void set(const AttendArgs &, int n) { len = n; }
@@ -63,29 +62,8 @@ struct AllRows {
     __device__ __forceinline__ int key(int r) const { return r; }
     __device__ __forceinline__ bool sees(int key) const { return key < len; }
 };
-// The first `sinks` and the last `window`: whole blocks of the sinks, then, `shift`
-// rows on, those of the window.
-struct WindowRows {
-    int len, sinks, start, split, shift;
-    __device__ __forceinline__ void set(const AttendArgs &a, int n) {
-        len = n;
-        sinks = a.sinks;
-        start = n - min(n, a.window);
-        split = shift = 0;
-        if (start <= sinks) {
-            start = 0;
-        } else {
-            const int sink_blocks = (sinks + kAttendUnit - 1) / kAttendUnit;
-            split = sink_blocks * kAttendUnit;
-            shift = max(start / kAttendUnit, sink_blocks) * kAttendUnit - split;
-        }
-    }
-    __device__ __forceinline__ int count() const { return len - shift; }
-    __device__ __forceinline__ int key(int r) const { return r < split ? r : r + shift; }
-    __device__ __forceinline__ bool sees(int key) const { return key < len && (key < sinks || key >= start); }
-    // all, any of the n rows from `key` on
-    __device__ __forceinline__ bool sees_all(int key, int n) const { return key + n <= len && (key + n <= sinks || key >= start); }
-    __device__ __forceinline__ bool sees_any(int key, int n) const { return key < len && (key < sinks || key + n > start); }
+struct WindowRows : SeenRows {
+    __device__ __forceinline__ void set(const AttendArgs &a, int n) { SeenRows::set(n, a.window, a.sinks); }
 };
 template <typename Rows> __device__ __forceinline__ int seen_rows(const AttendArgs &a, int len) {
     Rows r;
