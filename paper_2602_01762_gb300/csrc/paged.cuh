@@ -38,9 +38,9 @@ struct NormRopeArgs {
     const float *rope;                   // [rope_len, 2, D/2]: cosines, then sines
     const int32_t *pos, *n_new;          // [B]; n_new null: max_new rows each
     int rope_len, B, max_new, Hq, Hkv, split, heads;   // heads: of a row that a warp takes at a time
-    int one_row;                         // and whether it takes one row
     float eps;
     int *err;
+    int one_row;                         // whether a warp takes one row
 };
 
 struct NormRopeGradArgs {
@@ -69,13 +69,16 @@ struct AttendArgs {
     int B, Hq, Hkv, added;
     int cluster;                         // CTAs of a cluster per segment; 1: a persistent grid (set by the launch)
     float scale_log2;                    // softmax scale * log2(e)
+    int *err;
     int window, sinks;                   // window < 0: every row is seen
-    const float *k_scales, *v_scales;    // 8-bit caches: [n_pages, Hkv, scale_blocks]
+};
+// Over a cache held in 8 bits.
+struct CodeAttendArgs : AttendArgs {
+    const float *k_scales, *v_scales;    // [n_pages, Hkv, scale_blocks]
     int scale_rows, scale_blocks;        // rows of a block; blocks of a page
-    Divisor by_page, by_scale;           // 8-bit caches: by page_size, by scale_rows
+    Divisor by_page, by_scale;           // by page_size, by scale_rows
     int run;                             // 1: tiles divide pages and offsets are short, 2: dense rows besides
     int short_page, short_row, page_scales;   // then: page_stride, row_stride, scales of a page
-    int *err;
 };
 
 // Rows quantised into a cache of codes; the first and last row of a cache read back.
@@ -134,9 +137,9 @@ cudaError_t launch_paged_attend(const AttendArgs &a, bool bf16, int D, int sms, 
 cudaError_t start_window_attend(const AttendArgs &a, bool bf16, int D, int ht, int sms, cudaStream_t s);
 cudaError_t prepare_e4m3_attend(bool bf16, int D, int G);
 cudaError_t prepare_int8_attend(bool bf16, int D, int G);
-cudaError_t start_e4m3_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
-cudaError_t start_int8_attend(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
-cudaError_t launch_code_attend(const AttendArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t start_e4m3_attend(const CodeAttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t start_int8_attend(const CodeAttendArgs &a, bool bf16, int D, int sms, cudaStream_t s);
+cudaError_t launch_code_attend(const CodeAttendArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
 // CTAs, and split and heads of `a`.
 unsigned plan_norm_rope(NormRopeArgs &a, bool bf16, int D, bool append, int sms);
 cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool append, int sms, cudaStream_t s);
@@ -306,26 +309,17 @@ __device__ __forceinline__ void dsmem_st(int *local, uint32_t rank, int v) {
     asm volatile("st.shared::cluster.s32 [%0], %1;" ::"r"(dsmem_at(local, rank)), "r"(v) : "memory");
 }
 
-// How units are shared out, CTA by CTA: the same to each.
-struct EvenShares {
-    int per;
-    __device__ __forceinline__ void set(int units, int ctas) { per = (units + ctas - 1) / ctas; }
-    // a share's first unit, and the share that a unit is in
-    __device__ __forceinline__ long long first(int cta) const { return (long long)cta * per; }
-    __device__ __forceinline__ int cta_of(int u) const { return u / per; }
-};
-// Ragged work split into contiguous shares.  Sequence b of rows(b) rows has
+// Ragged work split into equal contiguous shares.  Sequence b of rows(b) rows has
 // blocks_of(rows) >= 1 blocks of keys, each for `heads` heads; units run over (b, head, block).
-// Every CTA takes the units u0 .. u1 - 1, from sequence b on; false: none are left for
+// Every CTA takes `per` units from u0 on, in sequence b; false: none are left for
 // it.  All threads of the CTA call it.
-template <typename Shares = EvenShares> struct UnitRange {
-    int u0, u1;        // this CTA's units
-    Shares shares;
+struct UnitRange {
+    int u0, u1, per;   // this CTA's units; units per CTA
     int b, first;      // sequence of u0 and that sequence's first unit
     int lens;          // lane i: rows of sequence i (B <= 32 alone)
 };
-template <int THREADS, typename Shares, typename Rows, typename Blocks>
-__device__ __forceinline__ bool unit_range(UnitRange<Shares> &r, int B, int heads, const Rows &rows, const Blocks &blocks_of) {
+template <int THREADS, typename Rows, typename Blocks>
+__device__ __forceinline__ bool unit_range(UnitRange &r, int B, int heads, const Rows &rows, const Blocks &blocks_of) {
     const int tid = threadIdx.x, lane = tid & 31;
     const int cta = blockIdx.x, ctas = gridDim.x;
     auto blocks = [&](int b) { return blocks_of(rows(b)); };
@@ -339,10 +333,10 @@ __device__ __forceinline__ bool unit_range(UnitRange<Shares> &r, int B, int head
             if (lane >= o) s += t;
         }
         const int units = __shfl_sync(0xFFFFFFFFu, s, 31) * heads;
-        r.shares.set(units, ctas);
-        if (r.shares.first(cta) >= units) return false;
-        r.u0 = (int)r.shares.first(cta);
-        r.u1 = (int)min(r.shares.first(cta + 1), (long long)units);
+        r.per = (units + ctas - 1) / ctas;
+        if ((long long)cta * r.per >= units) return false;
+        r.u0 = cta * r.per;
+        r.u1 = min(r.u0 + r.per, units);
         const int at = r.u0 / heads;
         r.b = __popc(__ballot_sync(0xFFFFFFFFu, lane < B && s <= at));
         r.first = __shfl_sync(0xFFFFFFFFu, s - n, r.b) * heads;
@@ -359,10 +353,10 @@ __device__ __forceinline__ bool unit_range(UnitRange<Shares> &r, int B, int head
 #pragma unroll
     for (int w = 0; w < THREADS / 32; ++w) total += warp_sum[w];
     const int units = total * heads;
-    r.shares.set(units, ctas);
-    if (r.shares.first(cta) >= units) return false;
-    r.u0 = (int)r.shares.first(cta);
-    r.u1 = (int)min(r.shares.first(cta + 1), (long long)units);
+    r.per = (units + ctas - 1) / ctas;
+    if ((long long)cta * r.per >= units) return false;
+    r.u0 = cta * r.per;
+    r.u1 = min(r.u0 + r.per, units);
     const int at = r.u0 / heads;
     int before = 0;
     for (int base = 0; base < B && before <= at; base += THREADS) {

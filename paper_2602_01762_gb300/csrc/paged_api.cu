@@ -361,7 +361,7 @@ prism_status prism_paged_attend_codes(prism_paged *p, const prism_paged_cache *c
                                       int32_t window, int32_t sinks, const void *q, void *out, float *lse, void *stream) {
     if (!p) return fail(nullptr, PRISM_ERR_INVALID_ARG, "prism_paged_attend_codes: null handle");
     Check c{p};
-    AttendArgs a{};
+    CodeAttendArgs a{};
     c.codes(a, cache, scales);
     c.attend(a, cache, added, window, sinks, q, out, lse);
     if (c.s != PRISM_OK) return c.s;

@@ -30,14 +30,14 @@ namespace {
 // kept P in three parts: 52.1, 52.3 and 53.3 us): what bounds it is the chain of a row's loads, not their bytes.
 constexpr int kWtThreads = 256;
 constexpr int kWtCtasPerSm = 8;
-template <int V>
+template <int V, bool WINDOW>
 __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel(AttendArgs a, int head_tile) {
     // Before the wait: the attention kernel lets this one start once its own wait is
     // over, so lengths, table and weights are final; scores and stat are not.
     pdl_trigger();
     auto rows = [&](int b) { return paged_len(a.cache, b, a.added, nullptr); };
     auto blocks = [](int n) { return max(1, (n + kWtThreads - 1) / kWtThreads); };
-    UnitRange<> r;
+    UnitRange r;
     if (!unit_range<kWtThreads>(r, a.B, a.Hkv, rows, blocks)) {
         pdl_wait();
         return;
@@ -48,7 +48,7 @@ __global__ void __launch_bounds__(kWtThreads, kWtCtasPerSm) paged_weights_kernel
     int h = (r.u0 - r.first) / nblk, blk = (r.u0 - r.first) % nblk;
     for (int u = r.u0; u < r.u1; ++u) {
         const int j = blk * kWtThreads + threadIdx.x;
-        const bool seen = j < len && (a.window < 0 || j < a.sinks || j >= len - a.window);
+        const bool seen = j < len && (!WINDOW || j < a.sinks || j >= len - a.window);
         const int page = seen ? a.cache.table[(long long)b * a.cache.table_pages + j / a.cache.page_size] : -1;
         if (u == r.u0) pdl_wait();
         if ((unsigned)page < (unsigned)a.cache.n_pages) {   // else not seen, or reported by the attention
@@ -111,12 +111,12 @@ cudaError_t launch_paged_attend(const AttendArgs &args, bool bf16, int D, int sm
     const long long rows = (long long)a.cache.table_pages * a.cache.page_size;
     const long long chunks = a.B * (long long)a.Hkv * ((rows + kWtThreads - 1) / kWtThreads);
     const dim3 wt((unsigned)(chunks < sms * kWtCtasPerSm ? chunks : sms * kWtCtasPerSm));
-    auto go = [&](auto k) { return launch_k(k, wt, dim3(kWtThreads), 0, s, true, a, ht); };
+    auto go = [&](auto all, auto window) { return launch_k(a.window < 0 ? all : window, wt, dim3(kWtThreads), 0, s, true, a, ht); };
     // 4, 8 or 16 heads of one tile: a row's scores are one, two or four float4
-    if (G <= ht && G == 4) return go(paged_weights_kernel<1>);
-    if (G <= ht && G == 8) return go(paged_weights_kernel<2>);
-    if (G <= ht && G == 16) return go(paged_weights_kernel<4>);
-    return go(paged_weights_kernel<0>);
+    if (G <= ht && G == 4) return go(paged_weights_kernel<1, false>, paged_weights_kernel<1, true>);
+    if (G <= ht && G == 8) return go(paged_weights_kernel<2, false>, paged_weights_kernel<2, true>);
+    if (G <= ht && G == 16) return go(paged_weights_kernel<4, false>, paged_weights_kernel<4, true>);
+    return go(paged_weights_kernel<0, false>, paged_weights_kernel<0, true>);
 }
 
 }  // namespace prism

@@ -94,7 +94,7 @@ template <typename Rows, int COST> struct Pieces {
         blk1 = max(u - seg - COST, 0);
         return blk0 < blk1;
     }
-    template <typename Shares> __device__ __forceinline__ bool begin(const AttendArgs &a, const UnitRange<Shares> &r, int n_heads) {
+    __device__ __forceinline__ bool begin(const AttendArgs &a, const UnitRange &r, int n_heads) {
         u = r.u0;
         u1 = r.u1;
         b = r.b;
@@ -323,7 +323,7 @@ template <typename P, typename Rows> struct CodeFeed {
     int own;                                             // and whether row `lane` of the tile does
     bool more, live;
     __device__ __forceinline__ uint32_t free_stage() const { return to; }
-    __device__ __forceinline__ void begin(const AttendArgs &a, const Pieces<Rows, P::kCost> &p, uint32_t at, int w, int n_tiles) {
+    __device__ __forceinline__ void begin(const CodeAttendArgs &a, const Pieces<Rows, P::kCost> &p, uint32_t at, int w, int n_tiles) {
         const int lane = threadIdx.x & 31;
         f = p;
         warp = w;
@@ -338,7 +338,7 @@ template <typename P, typename Rows> struct CodeFeed {
         walk(a);
         look_up(a);
     }
-    __device__ __forceinline__ void enter(const AttendArgs &a) {
+    __device__ __forceinline__ void enter(const CodeAttendArgs &a) {
         const int lane = threadIdx.x & 31, head = tiles == 1 ? f.h : f.h / tiles;
         const long long at = head * a.cache.head_stride + (a.run ? lane / kChunks * a.cache.row_stride : 0) + lane % kChunks * 16;
         table = a.cache.table + (long long)f.b * a.cache.table_pages;
@@ -348,14 +348,14 @@ template <typename P, typename Rows> struct CodeFeed {
         place = f.blk0 * kAttendUnit + warp * KT;
         end = f.blk0 * kAttendUnit + f.rows();
     }
-    __device__ __forceinline__ void walk(const AttendArgs &a) {
+    __device__ __forceinline__ void walk(const CodeAttendArgs &a) {
         while (place >= end) {
             more = f.next(a);
             if (!more) break;
             enter(a);
         }
     }
-    __device__ __forceinline__ void look_up(const AttendArgs &a) {
+    __device__ __forceinline__ void look_up(const CodeAttendArgs &a) {
         live = more;
         if (!more) return;
         const int lane = threadIdx.x & 31, key = f.seen.key(place);
@@ -384,7 +384,7 @@ template <typename P, typename Rows> struct CodeFeed {
     // Shared address of this lane's copy i: rows come back to the same banks every other copy.
     __device__ __forceinline__ uint32_t place_of(int i) const { return to + piece[i & 1] + (i >> 1) * (2 * kRowsPer * kRow); }
     // One run's. STEP: bytes from a copy's row to the next one's, 0 unless they are dense.
-    template <int STEP> __device__ __forceinline__ void copies(const AttendArgs &a, int j, bool known) {
+    template <int STEP> __device__ __forceinline__ void copies(const CodeAttendArgs &a, int j, bool known) {
         const long long at = (long long)page[j] * a.short_page + (long long)row[j] * a.short_row;
         const char *kp = k_at + at, *vp = v_at + at;
         if (known && in[j] == kAll) {
@@ -404,7 +404,7 @@ template <typename P, typename Rows> struct CodeFeed {
             }
         }
     }
-    __device__ __forceinline__ void issue(const AttendArgs &a) {
+    __device__ __forceinline__ void issue(const CodeAttendArgs &a) {
         if (live) {
             const int lane = threadIdx.x & 31;
             const float *s;
@@ -481,7 +481,7 @@ template <typename P> constexpr size_t attend_smem() {
 // Rows says which rows of a sequence are seen; the others are not read, and their
 // block-table entries neither.  P::kScaled: 8-bit rows with a scale for each.
 template <typename P, bool CLUSTER, typename Rows>
-__global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(AttendArgs a) {
+__global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(const typename P::Args a) {
     using T = typename P::T;
     constexpr int D = P::D, KT = P::KT, S = P::kStages, H = P::kHeads, kStage = P::kStage;
     constexpr int kPart = Joined<P>::kPart, kGroup = Joined<P>::kGroup;   // kPart: sums [H][D], then (maximum, sum) [H]
@@ -495,7 +495,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
     pdl_trigger();
 
     const int G = a.Hq / a.Hkv, tiles = (G + H - 1) / H, heads = a.Hkv * tiles;
-    UnitRange<typename P::Shares> r;
+    UnitRange r;
     Pieces<Rows, P::kCost> p;                                      // the piece being computed
     const int rank = CLUSTER ? (int)blockIdx.x % a.cluster : 0;
     if (CLUSTER) {
@@ -510,7 +510,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
 
     const uint32_t ring = (uint32_t)__cvta_generic_to_shared(smem) + warp * (S * kStage);
     float *merge = (float *)(smem + kPaWarps * S * kStage);                       // [warps][H][stride]
-    float *sm = (float *)(smem + kPaWarps * S * kStage + kAttendSums<P>), *sl = sm + kPaWarps * H;    // [warps][H]
+    float *sm = merge + kAttendSums<P> / 4, *sl = sm + kPaWarps * H;                // [warps][H]
     float *own = merge + warp * H * P::kMergeStride;     // this warp's share, scratch until the segment's end
     float *sums = P::kScaled ? merge : (float *)smem;    // a cluster's, for its other ranks
     __shared__ uint32_t own_at[kPaWarps];                // P::kScaled: where the warps' shares are
@@ -520,8 +520,13 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
     using Feed = typename FeedOf<P, Rows>::type;
     Feed feed;
     feed.begin(a, p, ring, warp, tiles);
-#pragma unroll P::kScaled ? 1 : S
-    for (int i = 0; i < S - 1; ++i) feed.issue(a);
+    if constexpr (P::kScaled) {
+#pragma unroll 1
+        for (int i = 0; i < S - 1; ++i) feed.issue(a);   // one instance: what a launch fetches of the code counts
+    } else {
+#pragma unroll
+        for (int i = 0; i < S - 1; ++i) feed.issue(a);
+    }
 
     int stage = 0;
     P state;
@@ -555,7 +560,7 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
         __syncthreads();
         const bool whole = p.blk0 == 0 && p.blk1 == p.nblk;
         const int first = p.seg + P::kCost;           // unit of the segment's first block
-        const int c0 = CLUSTER ? 0 : r.shares.cta_of(first), c1 = CLUSTER ? 0 : r.shares.cta_of(first + p.nblk - 1);
+        const int c0 = CLUSTER ? 0 : first / r.per, c1 = CLUSTER ? 0 : (first + p.nblk - 1) / r.per;
         const int slot = 2 * blockIdx.x + (p.blk0 == 0 ? 1 : 0);
         float *part = a.part + (long long)slot * kPart;
         for (int e = tid; e < n * (D / 4); e += kPaThreads) {
@@ -568,8 +573,9 @@ __global__ void __launch_bounds__(kPaThreads, P::kCtas) paged_attend_kernel(Atte
 #pragma unroll
             for (int w = 0; w < kPaWarps; ++w) {
                 const float k = exp2f(sm[w * H + h] - base);
-                const float *from = P::kScaled ? (const float *)smem + own_at[w] : merge + w * H * P::kMergeStride;
-                const float4 y = *(const float4 *)(from + h * P::kMergeStride + d);
+                float4 y;
+                if constexpr (P::kScaled) y = *(const float4 *)((const float *)smem + own_at[w] + h * P::kMergeStride + d);
+                else y = *(const float4 *)(merge + (w * H + h) * P::kMergeStride + d);
                 L = fmaf(k, sl[w * H + h], L);
                 x[0] = fmaf(k, y.x, x[0]);
                 x[1] = fmaf(k, y.y, x[1]);
@@ -700,7 +706,7 @@ inline int attend_cluster(long long segments, long long cap, int rows, int sms) 
 }
 
 // ht: heads of a tile.
-template <typename P, typename Rows> cudaError_t start_attend(AttendArgs a, int ht, int sms, cudaStream_t s) {
+template <typename P, typename Rows> cudaError_t start_attend(typename P::Args a, int ht, int sms, cudaStream_t s) {
     const int G = a.Hq / a.Hkv;
     const long long cap = attend_rows(a), segments = a.B * (long long)a.Hkv * ((G + ht - 1) / ht);
     const long long most = segments * (P::kCost + (cap + kAttendUnit - 1) / kAttendUnit);

@@ -81,7 +81,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     static constexpr int D = D_, KT = 32, NT = MODE == kSixteen ? 2 : 1;
     static constexpr int kRow = D, kStage = 2 * KT * kRow + 8 * KT;   // bytes
     static constexpr bool kScaled = true;
-    using Shares = EvenShares;
+    using Args = CodeAttendArgs;
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
     static constexpr int kQ = sizeof(T) == 4 && MODE != kPacked ? 2 : 1;    // products of K and q
     static constexpr int kParts = MODE == kPacked ? 1 : 2;                  // products of V and W
@@ -351,7 +351,7 @@ template <int FORMAT, typename F> cudaError_t with_code_tile(bool bf16, int D, i
 template <int FORMAT> cudaError_t prepare_codes(bool bf16, int D, int G) {
     return with_code_tile<FORMAT>(bf16, D, attend_head_tile(G), [](auto tile) { return prepare_attend<decltype(tile), WindowRows>(); });
 }
-template <int FORMAT> cudaError_t start_codes(const AttendArgs &a, bool bf16, int D, int sms, cudaStream_t s) {
+template <int FORMAT> cudaError_t start_codes(const CodeAttendArgs &a, bool bf16, int D, int sms, cudaStream_t s) {
     const int ht = attend_head_tile(a.Hq / a.Hkv);
     return with_code_tile<FORMAT>(bf16, D, ht, [&](auto tile) { return start_attend<decltype(tile), WindowRows>(a, ht, sms, s); });
 }

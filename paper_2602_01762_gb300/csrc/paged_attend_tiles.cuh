@@ -27,8 +27,8 @@ template <int D_, int MODE> struct Bf16Tile {
     static constexpr int D = D_, KT = kPaStage / (4 * D), NT = MODE == kSixteen ? 2 : 1;
     static constexpr int kRow = 2 * D, kStage = kPaStage;   // bytes
     static constexpr bool kScaled = false;
+    using Args = AttendArgs;
     static constexpr int kCtas = 2, kCost = 1;
-    using Shares = EvenShares;
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
     static constexpr int kParts = MODE == kPacked ? 2 : 3;   // products of P and V
     static constexpr int kMergeStride = D + 4;
@@ -208,8 +208,8 @@ template <int D_> struct F32Tile {
     static constexpr int D = D_, KT = kPaStage / (8 * D), V = D / 64;   // V: pairs of dims of a lane
     static constexpr int kRow = 4 * D, kStage = kPaStage;   // bytes
     static constexpr bool kScaled = false;
+    using Args = AttendArgs;
     static constexpr int kCtas = 2, kCost = 1;
-    using Shares = EvenShares;
     static constexpr int kHeads = 4;
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = 3;
@@ -343,8 +343,8 @@ template <int D_, int NT> struct F32Mma {
     static constexpr int D = D_, KT = kPaStage / (8 * D);
     static constexpr int kRow = 4 * D, kStage = kPaStage;   // bytes
     static constexpr bool kScaled = false;
+    using Args = AttendArgs;
     static constexpr int kCtas = 2, kCost = 1;
-    using Shares = EvenShares;
     static constexpr int kHeads = 8 * NT;
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = NT == 2 ? 2 : 3;

@@ -20,8 +20,8 @@ cudaError_t prepare_code_attend_kernels(bool bf16, int D, int G) {
 }
 
 // Codes have one form for both: without a window the window is every row.
-cudaError_t launch_code_attend(const AttendArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
-    AttendArgs a = args;
+cudaError_t launch_code_attend(const CodeAttendArgs &args, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s) {
+    CodeAttendArgs a = args;
     if (a.window < 0) a.window = 0x7FFFFFFF;
     a.by_page = Divisor((uint32_t)a.cache.page_size);
     a.by_scale = Divisor((uint32_t)a.scale_rows);

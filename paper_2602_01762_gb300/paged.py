@@ -301,22 +301,22 @@ class PagedAttention:
         (``prism_paged_attend_codes``)."""
         ref = self._bound(cache)
         shape = (cache.batch, self.n_q_heads, self.head_dim)
+        q, out = self._tensor(q, shape, self.tdtype, "q"), self._tensor(out, shape, self.tdtype, "out")
+        lse = None if lse is None else self._tensor(lse, shape[:2], torch.float32, "lse")
         if window is None:
             if sinks:
                 raise ValueError("sinks without a window")
+            if cache.scales_ref is None:
+                self._check(self.lib.prism_paged_attend(self.h, ref, added, q, out, lse, self._stream(stream)))
+                return
             window = -1
         elif window < 0:
             raise ValueError("window is negative")
-        window = min(window, 0x7FFFFFFF)
-        sinks = min(sinks, 0x7FFFFFFF)
-        args = (self._tensor(q, shape, self.tdtype, "q"), self._tensor(out, shape, self.tdtype, "out"),
-                None if lse is None else self._tensor(lse, shape[:2], torch.float32, "lse"), self._stream(stream))
-        if cache.scales is not None:
-            self._check(self.lib.prism_paged_attend_codes(self.h, ref, cache.scales_ref, added, window, sinks, *args))
-        elif window < 0:
-            self._check(self.lib.prism_paged_attend(self.h, ref, added, *args))
+        window, sinks = min(window, 0x7FFFFFFF), min(sinks, 0x7FFFFFFF)
+        if cache.scales_ref is None:
+            self._check(self.lib.prism_paged_attend_window(self.h, ref, added, window, sinks, q, out, lse, self._stream(stream)))
         else:
-            self._check(self.lib.prism_paged_attend_window(self.h, ref, added, window, sinks, *args))
+            self._check(self.lib.prism_paged_attend_codes(self.h, ref, cache.scales_ref, added, window, sinks, q, out, lse, self._stream(stream)))
 
     def read(self, cache, k_out, v_out, start=None, n_rows=None, stream=None):
         """``prism_paged_read_codes``: rows start[b] + i, i < n_rows[b], of a cache held
