@@ -474,8 +474,8 @@ template <typename P> constexpr size_t attend_smem() {
 // softmax and no barrier until the segment's end; the ring runs on across
 // segments, so loads never stop.
 //
-// CLUSTER, for few short segments: a cluster of a.cluster CTAs takes one segment,
-// each an equal run of its blocks, and joins through distributed shared memory
+// CLUSTER, for few short segments: a cluster of a.cluster CTAs (or one CTA) takes one
+// segment, each an equal run of its blocks, and joins through distributed shared memory
 // instead of tickets and loads from L2.
 //
 // Rows says which rows of a sequence are seen; the others are not read, and their
@@ -705,15 +705,34 @@ inline int attend_cluster(long long segments, long long cap, int rows, int sms) 
     return cap <= cs * (long long)rows ? cs : 1;
 }
 
+// The same where a window bounds the rows: most sequences have outgrown it, and segments
+// are as long as each other.  Then a cluster, or a CTA of its own, to a segment also where
+// there are as many as CTAs, and with more rows to each (P::kWindowRows, clusters up to
+// P::kWindowCluster); 0: shares.  Measured, 8 KV heads of 128 and 4 query heads each,
+// shares against this: bf16, 32 sequences with a window of 256 rows 13.7 and 9.5 us, of
+// 1024 26.9 and 24.6, 16 of 1024 17.6 and 14.5, of 2048 26.7 and 24.1; fp32, 16 of 256
+// 13.7 and 10.7, of 1024 27.4 and 25.0; e4m3, 32 of 256 15.9 and 12.0, 16 of 1024 16.7 and
+// 15.6, 8 of 2048 (four CTAs each) 14.5 and 15.6, 16 of 2048 21.7 and 23.1.
+inline int window_cluster(long long segments, long long cap, int rows, int most, long long ctas) {
+    int cs = 1;
+    while (2 * cs <= most && 2 * cs * segments <= ctas) cs *= 2;
+    return segments <= ctas && cap <= cs * (long long)rows ? cs : 0;
+}
+
 // ht: heads of a tile.
 template <typename P, typename Rows> cudaError_t start_attend(typename P::Args a, int ht, int sms, cudaStream_t s) {
     const int G = a.Hq / a.Hkv;
     const long long cap = attend_rows(a), segments = a.B * (long long)a.Hkv * ((G + ht - 1) / ht);
     const long long most = segments * (P::kCost + (cap + kAttendUnit - 1) / kAttendUnit);
-    a.cluster = attend_cluster(segments, cap, P::kClusterRows, sms);
-    if (a.cluster > 1)
-        return launch_cluster(paged_attend_kernel<P, true, Rows>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<P>(), a.cluster, s, a);
     const long long ctas = (long long)P::kCtas * sms;
+    a.cluster = attend_cluster(segments, cap, P::kClusterRows, sms);
+    bool whole = a.cluster > 1;
+    if (!whole && cap < (long long)a.cache.table_pages * a.cache.page_size) {
+        a.cluster = window_cluster(segments, cap, P::kWindowRows, P::kWindowCluster, ctas);
+        whole = a.cluster > 0;
+    }
+    if (whole)
+        return launch_cluster(paged_attend_kernel<P, true, Rows>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<P>(), a.cluster, s, a);
     const int grid = (int)(most < ctas ? most : ctas);
     return launch_k(paged_attend_kernel<P, false, Rows>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
 }

@@ -91,6 +91,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     static constexpr int kCost = 2;
     static constexpr int kCtas = MODE == kSixteen ? 2 : 3, kStages = (D == 128 ? 2 : 4) + (MODE == kSixteen ? 1 : 0);
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
+    static constexpr int kWindowRows = kClusterRows * 5 / 4, kWindowCluster = 2;     // see window_cluster
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a
     // whole number: W up to 2^15 leaves the most below.
     static constexpr float kSlackW = 1.f, kLift = 8192.f;

@@ -34,6 +34,7 @@ template <int D_, int MODE> struct Bf16Tile {
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = MODE == kSixteen ? 2 : 3;
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
+    static constexpr int kWindowRows = 5 * kClusterRows, kWindowCluster = 8;         // see window_cluster
     uint32_t qf[D / 16][NT][2];
     float m[NT][2], l[NT][2];
     F2 o[D / 16][NT][2];                                 // rows g and g + 8 of a head pair
@@ -214,6 +215,7 @@ template <int D_> struct F32Tile {
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = 3;
     static constexpr int kClusterRows = 128 * 128 / D;
+    static constexpr int kWindowRows = 5 * kClusterRows, kWindowCluster = 8;
     F2 q[4][V], o[4][V];
     float m, l;                                          // of head lane % 4
 
@@ -349,6 +351,7 @@ template <int D_, int NT> struct F32Mma {
     static constexpr int kMergeStride = D + 4;
     static constexpr int kStages = NT == 2 ? 2 : 3;
     static constexpr int kClusterRows = NT == 2 ? 256 * 128 / D : 256;
+    static constexpr int kWindowRows = 5 * kClusterRows, kWindowCluster = 8;
     const T *q;                                          // this tile's, for scores recomputed
     uint32_t qf[D / 16][3][NT][2];                       // part, heads g + 8 u, two pairs of dims
     F2 o[D / 16][NT][2];
