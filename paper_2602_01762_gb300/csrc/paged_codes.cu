@@ -173,52 +173,59 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
         __syncthreads();
     }
     const uint32_t angles_at = (uint32_t)__cvta_generic_to_shared(angles);
-    // Row j's values from what was read of it.
+    // Row j's values from what was read of it, before the norm's factor, which is returned.
+    // The gain times a bf16 value is exact, and the factor meets a sum that is already
+    // turned: two roundings fewer than in the order of the formula, and as many products.
     auto values = [&](int j, bool in, const uint4 &l, const uint4 &r, F2 (&x)[N], F2 (&y)[N]) {
         Pairs<T>::unpack(l, x);
         Pairs<T>::unpack(r, y);
-        if (!KEYS) return;
+        if (!KEYS) return 1.f;
         R rope;
         const int at = !in ? 0 : a.per > 1 ? group : j;   // a turn's last rows may be past the block's
         if (at < kScAngles) rope.load_shared(angles_at + at * (D * 4));
         else rope.load(a.rope, in ? position(j + shift) : 0);
+        float f = 1.f;
         if (norm) {
             F2 s = f2_mul(x[0], x[0]);
 #pragma unroll
             for (int e = 1; e < N; ++e) s = f2_fma(x[e], x[e], s);
 #pragma unroll
             for (int e = 0; e < N; ++e) s = f2_fma(y[e], y[e], s);
-            const float f = rsqrtf(lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + a.eps);
-            const F2 ff = f2(f, f);
+            const float m = lanes_sum<R::kLanes>(f2_sum(s)) * (1.f / D) + a.eps;
+            f = rsqrtf(m);
+            const float more = fmaf(-(m * f), f, 1.f) * 0.5f;    // one Newton step: within one ulp
+            if (fabsf(more) < 1e-3f) f = fmaf(f, more, f);       // but not of 0, infinities and NaN
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                x[e] = f2_mul(f2_mul(x[e], ff), gain.x[e]);
-                y[e] = f2_mul(f2_mul(y[e], ff), gain.y[e]);
+                x[e] = f2_mul(x[e], gain.x[e]);
+                y[e] = f2_mul(y[e], gain.y[e]);
             }
         }
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-            const F2 p = f2_sub(f2_mul(x[e], rope.cs[e]), f2_mul(y[e], rope.sn[e]));
-            y[e] = f2_fma(y[e], rope.cs[e], f2_mul(x[e], rope.sn[e]));
-            x[e] = p;
+            const F2 p = f2_mul(y[e], rope.sn[e]), q = f2_mul(x[e], rope.sn[e]);
+            x[e] = f2_fma(x[e], rope.cs[e], p ^ 0x8000000080000000ull);
+            y[e] = f2_fma(y[e], rope.cs[e], q);
         }
+        return f;
     };
-    auto magnitude = [&](const F2 (&x)[N], const F2 (&y)[N], float top) {
+    auto magnitude = [&](const F2 (&x)[N], const F2 (&y)[N], float f, float top) {
+        float row = 0.f;
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float2 u = f2_values(x[e]), v = f2_values(y[e]);
-            top = top_of(u.x, u.y, top_of(v.x, v.y, top));
+            row = top_of(u.x, u.y, top_of(v.x, v.y, row));
         }
-        return top;
+        return top_of(top, row * f, 0.f);
     };
-    auto finite = [&](const F2 (&x)[N], const F2 (&y)[N], float top) {
+    auto finite = [&](const F2 (&x)[N], const F2 (&y)[N], float f, float top) {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float2 u = f2_values(x[e]), v = f2_values(y[e]);
-            const float f[4] = {u.x, u.y, v.x, v.y};
+            const float z[4] = {u.x * f, u.y * f, v.x * f, v.y * f};
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (fabsf(f[i]) < INFINITY) top = fmaxf(top, fabsf(f[i]));
+                if (fabsf(z[i]) < INFINITY) top = fmaxf(top, fabsf(z[i]));
         }
         return top;
     };
@@ -234,8 +241,8 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
                     r = *(const uint4 *)(from + D / 2 * sizeof(T));
                 }
                 F2 u[N], v[N];
-                values(c * step + j0, in, l, r, u, v);
-                if (in) f(c * step + j0, u, v);
+                const float factor = values(c * step + j0, in, l, r, u, v);
+                if (in) f(c * step + j0, u, v, factor);
             }
     };
     const int width = a.per > 1 ? R::kLanes * a.scale_rows : 32;   // lanes of a block
@@ -247,15 +254,15 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
         if (w + teams < w1) before = live && j_new > 0 ? scale_at[(long long)(w + teams) * a.scale_blocks] : 0.f;
         cp_wait_group<1>();
         F2 x[kScKeep][N], y[kScKeep][N];
-        float top = 0.f;
+        float factor[kScKeep], top = 0.f;
 #pragma unroll
         for (int c = 0; c < kScKeep; ++c)
             if (turns >> c & 1) {                        // rows that are not new hold anything: their values are not used
                 const uint32_t at = ring + turn * kScStage + c * 1024;
-                values(c * step + j0, mine >> c & 1, lds16(at), lds16(at + 512), x[c], y[c]);
-                if (mine >> c & 1) top = magnitude(x[c], y[c], top);
+                factor[c] = values(c * step + j0, mine >> c & 1, lds16(at), lds16(at + 512), x[c], y[c]);
+                if (mine >> c & 1) top = magnitude(x[c], y[c], factor[c], top);
             }
-        further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N]) { top = magnitude(u, v, top); });
+        further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N], float f) { top = magnitude(u, v, f, top); });
         // over the block's lanes, then the team's warps; of a block with a NaN or an infinity
         // the largest finite value, with the sign bit for a mark
         for (int o = width / 2; o > 0; o >>= 1) top = top_of(top, __shfl_xor_sync(0xFFFFFFFFu, top, o), 0.f);
@@ -264,8 +271,8 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
             float t = 0.f;
 #pragma unroll
             for (int c = 0; c < kScKeep; ++c)
-                if (mine >> c & 1) t = finite(x[c], y[c], t);
-            further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N]) { t = finite(u, v, t); });
+                if (mine >> c & 1) t = finite(x[c], y[c], factor[c], t);
+            further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N], float f) { t = finite(u, v, f, t); });
             for (int o = width / 2; o > 0; o >>= 1) t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, o));
             top = odd ? -t : t;
         }
@@ -300,13 +307,14 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
                 *p = encode<FORMAT>(v[0] * f, v[1] * f, v[2] * f, v[3] * f);
             }
         }
-        auto put = [&](int j, const F2 (&x)[N], const F2 (&y)[N]) {
+        auto put = [&](int j, const F2 (&x)[N], const F2 (&y)[N], float factor) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 uint32_t c[E / 4];
 #pragma unroll
                 for (int e = 0; e < E / 4; ++e) {
                     F2 u = i ? y[2 * e] : x[2 * e], v = i ? y[2 * e + 1] : x[2 * e + 1];
+                    if (KEYS) u = f2_mul(u, f2(factor, factor)), v = f2_mul(v, f2(factor, factor));
                     if (any_odd) {                       // e4m3: infinities become NaN
                         float f[4] = {f2_values(u).x, f2_values(u).y, f2_values(v).x, f2_values(v).y};
 #pragma unroll
@@ -324,7 +332,7 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
         };
 #pragma unroll
         for (int c = 0; c < kScKeep; ++c)
-            if (mine >> c & 1) put(c * step + j0, x[c], y[c]);
+            if (mine >> c & 1) put(c * step + j0, x[c], y[c], factor[c]);
         further(w, put);
     }
 }
