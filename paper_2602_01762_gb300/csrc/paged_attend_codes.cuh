@@ -7,6 +7,13 @@
 // to the tensor cores as fp16, which holds every code of both formats exactly (e4m3 by
 // the hardware's conversion, int8 as the low byte of 1024 + 128 + c), and the scales
 // stay outside: K's multiplies a row's score, V's its probability.
+//
+// Measured, D = 128, bf16 queries: e4m3, 64 sequences of 6001 to 16384 rows, G = 8, 233 us
+// (6.3 TB/s); one of 131071, G = 4, 50 us (5.4, of which 39 us are the bytes and the rest
+// its start and joins); int8 with a scale a row, 16 sequences of 1 to 8192 rows, 34 us
+// (4.1); 517 rows 6.2 us. A tile of 16 rows takes 377 instructions a warp with e4m3 (a
+// pair of codes is one conversion) and 483 with int8; three CTAs an SM give the warps that
+// hide them (two: 276 us for the first case; four, of 128 registers: 298).
 #pragma once
 
 #include "paged_attend.cuh"

@@ -14,6 +14,11 @@
 // code has the same relative precision wherever in its range it lies, so that a closer
 // scale would give it nothing; to int8 it would give half a bit on average, and lose
 // more than that where one more row a block has every code rounded again.
+//
+// Bound by bytes, but a block's codes wait for its largest value and that for the rows'
+// loads. Measured, 32 query and 8 KV heads of 128, bf16, blocks of 16: 8 prompts of 1021 to
+// 2048 rows 58 us (277 MB, 4.8 TB/s: the queries' kernel 33, keys and values mostly behind
+// it), 16 tokens 3.6 us; read back, 4 prefixes of 9001 to 16384 rows 49.5 us (6.3 TB/s).
 #include "paged_rope.cuh"
 
 #include <type_traits>
