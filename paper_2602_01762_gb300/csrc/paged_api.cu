@@ -117,6 +117,7 @@ struct Check {
         a.cache = cache(c, "cache", true);
         need(q && q->k_scales && q->v_scales, PRISM_ERR_INVALID_ARG, "scales: null");
         if (s != PRISM_OK) return;
+        need((((uintptr_t)q->k_scales | (uintptr_t)q->v_scales) & 3u) == 0, PRISM_ERR_INVALID_ARG, "scales: not aligned to their type");
         need(q->format == PRISM_E4M3 || q->format == PRISM_INT8, PRISM_ERR_INVALID_ARG, "scales: format must be PRISM_E4M3 or PRISM_INT8");
         need(q->scale_rows >= 1 && q->scale_rows <= p->cfg.page_size && p->cfg.page_size % q->scale_rows == 0, PRISM_ERR_SHAPE,
              "scales: scale_rows must divide page_size");

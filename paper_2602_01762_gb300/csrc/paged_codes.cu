@@ -299,7 +299,7 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
         float s = power_of_two<FORMAT>(__float_as_uint(top) & 0x7FFFFFFFu);
         if (FORMAT == kInt8 && any_odd) s = __int_as_float(0x7FFFFFFF);   // int8 has no code for it: the block reads as NaN
         if (!(was < s) && !(s != s)) s = was;            // a NaN stays one
-        const float per_s = s > 0.f ? 1.f / s : 0.f;
+        const float per_s = s >= 1.17549435e-38f ? 1.f / s : 0.f;   // of 0 and what is not normal: no code but 0
         char *to = pages + w * a.cache.head_stride + page_at;
         if (thread == 0 && (j_new == 0 || s != was)) scale_at[(long long)w * a.scale_blocks] = s;
         if (j_new > 0 && was < s) {                      // earlier rows in the grown scale

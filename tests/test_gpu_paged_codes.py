@@ -361,6 +361,20 @@ def test_append_extreme_values(pkg, fmt, dtype):
     h.close()
 
 
+def test_append_zeros_behind_rows_of_any_scale(pkg):
+    for fmt in ref.MOST:
+        h, cache, q, k, v, q_out, _ = append_case(pkg, D=64, dtype="f32", fmt=fmt, page=16, r=16, lens=[3, 3], counts=[4, 4], Hkv=1)
+        for scale in (1e-40, 0.0, 2.0 ** -126, 0.3):
+            cache.k_scales.fill_(scale)
+            before = ref.codes_of(cache.k_pages)
+            h.append(cache, q, torch.zeros_like(k), v, q_out, identity_rope(40, 64))
+            now = ref.codes_of(cache.k_pages)
+            p = cache.block_table.cpu()[:, 0].long()
+            assert (now[p, 0, 3:7] == 0).all() and torch.equal(now[p, 0, :3], before[p, 0, :3])
+            assert (cache.k_scales[p.cuda(), 0, 0] == scale).all()
+        h.close()
+
+
 def test_append_rows_without_a_place(pkg):
     for fmt in ref.MOST:
         h, cache, q, k, v, q_out, n_new = append_case(pkg, D=64, dtype="bf16", fmt=fmt, page=8, r=4, lens=[8, 8, 8, 8], counts=[9, 9, 9, 9], Hkv=1)
@@ -541,6 +555,7 @@ def test_refusals(pkg):
     Scales = type(s)
     assert attend(s) == 0
     assert attend(None) == 1 and attend(Scales(None, s.v_scales, 1, 16)) == 1 and attend(Scales(s.k_scales, s.v_scales, 2, 16)) == 1
+    assert attend(Scales(s.k_scales + 2, s.v_scales, 1, 16)) == 1 and b"aligned" in lib.prism_paged_error(h.h)
     for rows in (0, -1, 5, 32):
         assert attend(Scales(s.k_scales, s.v_scales, 1, rows)) == 2
         assert b"scale_rows" in lib.prism_paged_error(h.h)
