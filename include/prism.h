@@ -658,8 +658,8 @@ prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cac
                                     const prism_heads *v_out, void *stream);
 
 /* prism_paged_attend_window over such a cache.  Codes enter their products exactly,
- * the scales outside of them in fp32; bf16 queries keep their 8 bits, fp32 queries,
- * and probabilities times V's scale, 22 bits (two fp16 parts), sums 24.  A key that is
+ * the scales outside of them in fp32; queries keep their bits, probabilities times V's
+ * scale 24 in fp32 and 22 in bf16 (three and two fp16 parts), sums 24.  A key that is
  * NaN makes its KV head's results NaN; a value, that dim of them.  Errors: as
  * prism_paged_attend. */
 prism_status prism_paged_attend_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales, int32_t added,

@@ -39,11 +39,14 @@ __device__ __forceinline__ float2 f16x2_values(uint32_t h) {
     asm("{.reg .b16 l, u;\n mov.b32 {l, u}, %2;\n cvt.f32.f16 %0, l;\n cvt.f32.f16 %1, u;}" : "=f"(v.x), "=f"(v.y) : "r"(h));
     return v;
 }
-// Two values as two fp16 parts each, rounded: 22 bits of them.
-__device__ __forceinline__ void two_parts(float x, float y, uint32_t &p0, uint32_t &p1) {
+// Two values as three fp16 parts each, rounded: their sum is the value, down to 2^-25.
+__device__ __forceinline__ void three_parts16(float x, float y, uint32_t &p0, uint32_t &p1, uint32_t &p2) {
     p0 = cvt_f16x2(x, y);
-    const float2 v = f16x2_values(p0);
-    p1 = cvt_f16x2(x - v.x, y - v.y);
+    float2 v = f16x2_values(p0);
+    x -= v.x, y -= v.y;
+    p1 = cvt_f16x2(x, y);
+    v = f16x2_values(p1);
+    p2 = cvt_f16x2(x - v.x, y - v.y);
 }
 
 // 2^x; 0 below 2^-126.
@@ -74,9 +77,11 @@ template <int FORMAT> __device__ __forceinline__ void code_values(uint32_t codes
 //
 // q enters as fp16 times a power of two for its head that brings the largest value to
 // 2^14: a bf16 value keeps its 8 bits down to 2^-31 of that (and below within 2^-39 of
-// it); fp32 takes two parts, 22 bits.  W is two fp16 parts of p s^V over a power of two
-// for the head, 22 bits too (below 2^-17 of the head's largest fewer, within 2^-38 of
-// it); both parts in one product with up to four heads.
+// it); fp32 takes three parts, its 24 bits as far down.  W is fp16 parts of p s^V over a
+// power of two for the head: two for bf16, 22 bits, at most 4 units of 2^-24 of a weight
+// where the result's own rounding is 2^15 of them (a third: the cases above 252, 53, 35.5
+// us); three for fp32, 24 bits; below 2^-15 of the head's largest fewer, within 2^-38 of
+// it.  With up to four heads two parts share a product, in columns 0 to 3 and 4 to 7.
 //
 // Two running maxima, of the scores (for the sum of probabilities) and of the scores
 // with log2 s^V (for W, so that it stays in fp16's range whatever the scales are); both
@@ -90,13 +95,14 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     static constexpr bool kScaled = true;
     using Args = CodeAttendArgs;
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
-    static constexpr int kQ = sizeof(T) == 4 && MODE != kPacked ? 2 : 1;    // products of K and q
-    static constexpr int kParts = MODE == kPacked ? 1 : 2;                  // products of V and W
+    static constexpr int kQ = sizeof(T) == 2 ? 1 : MODE == kPacked ? 2 : 3;  // products of K and q
+    static constexpr int kParts = (sizeof(T) == 2 ? 2 : 3) - (MODE == kPacked ? 1 : 0);   // products of V and W
+    static_assert(sizeof(T) == 2 || MODE != kSixteen, "fp32 queries go eight heads at a time: sixteen take 96 registers");
     static constexpr int kMergeStride = D + 4;
     // a segment's end costs what two blocks of 8-bit rows do: 16 sequences of 1 to 8192 rows
     // with 1, 2 and 3 units 40.3, 34.0 and 33.4 us
     static constexpr int kCost = 2;
-    static constexpr int kCtas = MODE == kSixteen ? 2 : 3, kStages = (D == 128 ? 2 : 4) + (MODE == kSixteen ? 1 : 0);
+    static constexpr int kCtas = MODE == kSixteen || kQ == 3 ? 2 : 3, kStages = (D == 128 ? 2 : 4) + (kCtas == 2 ? 1 : 0);
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     static constexpr int kWindowRows = kClusterRows * 5 / 4, kWindowCluster = 2;     // see window_cluster
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a
@@ -148,16 +154,16 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
             const float up = __uint_as_float((uint32_t)(127 + e) << 23), down = __uint_as_float((uint32_t)(127 - e) << 23);
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-                uint32_t p[2][2];
-#pragma unroll
-                for (int i = 0; i < 2; ++i) two_parts(x[k][2 * i] * up, x[k][2 * i + 1] * up, p[0][i], p[1][i]);
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
+                    uint32_t p[3];
+                    three_parts16(x[k][2 * i] * up, x[k][2 * i + 1] * up, p[0], p[1], p[2]);
                     if (sizeof(T) == 4 && MODE == kPacked) {   // columns 4 to 7: the second parts
-                        qf[k][0][u][i] = g < 4 ? p[0][i] : p[1][i];
+                        qf[k][0][u][i] = g < 4 ? p[0] : p[1];
+                        qf[k][kQ - 1][u][i] = g < 4 ? p[2] : 0u;
                     } else {
-                        qf[k][0][u][i] = p[0][i];
-                        if (kQ == 2) qf[k][kQ - 1][u][i] = p[1][i];
+#pragma unroll
+                        for (int j = 0; j < kQ; ++j) qf[k][j][u][i] = p[j];
                     }
                 }
             }
@@ -223,7 +229,7 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
 #pragma unroll
                     for (int t = 0; t < NT; ++t)
 #pragma unroll
-                        for (int i = kQ - 1; i >= 0; --i)   // second parts first
+                        for (int i = kQ - 1; i >= 0; --i)   // last parts first
                             mma_f16(k & 1 ? s2[t] : s[t], a, qf[k][i][t][0], qf[k][i][t][1], k < 2 && i == kQ - 1);
                 }
             }
@@ -285,13 +291,15 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
                     const float p0 = power2(s[t][2 * u] - b0), p1 = power2(s[t][2 * u + 1] - b1), v = u ? v1 : v0;
                     l[t][0] += p0;
                     l[t][1] += p1;
-                    uint32_t x, y;
-                    two_parts(p0 * f[t][0] * v, p1 * f[t][1] * v, x, y);
+                    uint32_t x, y, z;
+                    three_parts16(p0 * f[t][0] * v, p1 * f[t][1] * v, x, y, z);
                     if (MODE == kPacked) {               // columns 4 to 7: the second parts
                         part[0][t][u] = transpose8((lane & 2) ? y : x);
+                        if (kParts == 2) part[kParts - 1][t][u] = transpose8((lane & 2) ? 0u : z);
                     } else {
                         part[0][t][u] = transpose8(x);
-                        part[kParts - 1][t][u] = transpose8(y);
+                        part[kParts > 1 ? 1 : 0][t][u] = transpose8(y);
+                        if (kParts == 3) part[kParts - 1][t][u] = transpose8(z);
                     }
                 }
             }
@@ -348,19 +356,23 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
 };
 
 template <int FORMAT, typename F> cudaError_t with_code_tile(bool bf16, int D, int heads, const F &f) {
-    auto type = [&](auto t) {
-        using T = decltype(t);
+    if (bf16) {
         if (D == 128)
-            return heads == 4 ? f(CodeTile<T, 128, kPacked, FORMAT>()) : heads == 8 ? f(CodeTile<T, 128, kEight, FORMAT>()) : f(CodeTile<T, 128, kSixteen, FORMAT>());
-        return heads == 4 ? f(CodeTile<T, 64, kPacked, FORMAT>()) : heads == 8 ? f(CodeTile<T, 64, kEight, FORMAT>()) : f(CodeTile<T, 64, kSixteen, FORMAT>());
-    };
-    return bf16 ? type(uint16_t()) : type(0.f);
+            return heads == 4 ? f(CodeTile<uint16_t, 128, kPacked, FORMAT>()) : heads == 8 ? f(CodeTile<uint16_t, 128, kEight, FORMAT>()) : f(CodeTile<uint16_t, 128, kSixteen, FORMAT>());
+        return heads == 4 ? f(CodeTile<uint16_t, 64, kPacked, FORMAT>()) : heads == 8 ? f(CodeTile<uint16_t, 64, kEight, FORMAT>()) : f(CodeTile<uint16_t, 64, kSixteen, FORMAT>());
+    }
+    if (D == 128) return heads == 4 ? f(CodeTile<float, 128, kPacked, FORMAT>()) : f(CodeTile<float, 128, kEight, FORMAT>());
+    return heads == 4 ? f(CodeTile<float, 64, kPacked, FORMAT>()) : f(CodeTile<float, 64, kEight, FORMAT>());
+}
+inline int code_head_tile(bool bf16, int G) {
+    const int ht = attend_head_tile(G);
+    return bf16 || ht < 16 ? ht : 8;
 }
 template <int FORMAT> cudaError_t prepare_codes(bool bf16, int D, int G) {
-    return with_code_tile<FORMAT>(bf16, D, attend_head_tile(G), [](auto tile) { return prepare_attend<decltype(tile), WindowRows>(); });
+    return with_code_tile<FORMAT>(bf16, D, code_head_tile(bf16, G), [](auto tile) { return prepare_attend<decltype(tile), WindowRows>(); });
 }
 template <int FORMAT> cudaError_t start_codes(const CodeAttendArgs &a, bool bf16, int D, int sms, cudaStream_t s) {
-    const int ht = attend_head_tile(a.Hq / a.Hkv);
+    const int ht = code_head_tile(bf16, a.Hq / a.Hkv);
     return with_code_tile<FORMAT>(bf16, D, ht, [&](auto tile) { return start_attend<decltype(tile), WindowRows>(a, ht, sms, s); });
 }
 

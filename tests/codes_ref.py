@@ -77,9 +77,8 @@ def seen(n, window, sinks):
 def attend(q, k_values, v_values, table, lens, scale, window=None, sinks=0, v_scales=None):
     """out, lse, weights (list of [Hkv, rows]) and the bounds of out, lse and weights, as
     paged_ref.attend's, of pages of values (64 bits, host).  What 8-bit caches have
-    besides is within them: queries of 22 bits add 4 U scale sum |q k| to a score's
-    error, of which the bound has 2 D U; weights of two fp16 parts 2^-22 of themselves,
-    of 2^-20.  With ``v_scales`` (those of v_values' blocks) the bound of out has their
+    besides is within them: weights of two fp16 parts (bf16) add 2^-22 of themselves,
+    of 2^-16, of three 2^-24, of 2^-20.  With ``v_scales`` (those of v_values' blocks) the bound of out has their
     floor too: fp16 ends at steps of 2^-24, the head's largest weight p s is at least
     2^12 of them over its base (2^13, and one bit for the base's whole number), so two
     parts leave 2^-25 / 2^12 of it for each row's code, 2^-36 with room."""
