@@ -303,24 +303,26 @@ template <typename P, typename Rows> struct RowFeed {
     }
 };
 
-// The same for 8-bit rows and their scales, one tile of two runs of kRunRows rows ahead.
+// The same for 8-bit rows and their scales, one tile of one or two runs of kRunRows rows
+// ahead.
 // Where runs divide pages and offsets are short (a.run), a run lies in one page and all
 // but its page and row is known from the piece or from the launch.
 constexpr int kRunRows = 16;
 template <typename P, typename Rows> struct CodeFeed {
     static constexpr int KT = P::KT, S = P::kStages, kStage = P::kStage, kRow = P::kRow, kChunks = kRow / 16, kRowsPer = 32 / kChunks;
     static constexpr int kStep = kPaWarps * KT, kCopies = kRunRows / kRowsPer, kAll = (1 << kCopies) - 1;
-    static_assert(KT == 2 * kRunRows, "a lane's scale is that of its row");
+    static constexpr int kRuns = KT / kRunRows;
+    static_assert(KT == kRuns * kRunRows && (kRuns == 1 || kRuns == 2), "a lane's scale is that of its row");
     Pieces<Rows, P::kCost> f;
     const int32_t *table;                                // of the sequence
     const char *k_at, *v_at;                             // of the head and of this lane's part of a run
-    const float *scales;                                 // K's of the head
+    const float *scales;                                 // K's of the head (of one run: V's in the upper lanes)
     uint64_t once;
     uint32_t to, ring_end;                               // the next stage, which is free; the last one's end
     uint32_t piece[2];                                   // of this lane's copies, even and odd ones
     int place, end, warp, tiles;
-    int page[2], row[2], in[2];                          // next tile's runs: bit i: this lane's row of copy i counts
-    int own;                                             // and whether row `lane` of the tile does
+    int page[kRuns], row[kRuns], in[kRuns];              // next tile's runs: bit i: this lane's row of copy i counts
+    int own;                                             // and whether row lane % KT of the tile does
     bool more, live;
     __device__ __forceinline__ uint32_t free_stage() const { return to; }
     __device__ __forceinline__ void begin(const CodeAttendArgs &a, const Pieces<Rows, P::kCost> &p, uint32_t at, int w, int n_tiles) {
@@ -344,7 +346,7 @@ template <typename P, typename Rows> struct CodeFeed {
         table = a.cache.table + (long long)f.b * a.cache.table_pages;
         k_at = a.cache.k + at;
         v_at = a.cache.v + at;
-        scales = a.k_scales + (long long)head * a.scale_blocks;
+        scales = (kRuns == 2 || lane < KT ? a.k_scales : a.v_scales) + (long long)head * a.scale_blocks;
         place = f.blk0 * kAttendUnit + warp * KT;
         end = f.blk0 * kAttendUnit + f.rows();
     }
@@ -360,10 +362,10 @@ template <typename P, typename Rows> struct CodeFeed {
         if (!more) return;
         const int lane = threadIdx.x & 31, key = f.seen.key(place);
         const bool all = f.seen.sees_all(key, KT);
-        own = all || f.seen.sees(key + lane);
+        own = all || f.seen.sees(key + lane % KT);
         if (a.run) {
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
+            for (int j = 0; j < kRuns; ++j) {
                 const int k = key + j * kRunRows, slot = a.by_page.of(k);
                 row[j] = k - slot * a.cache.page_size;
                 in[j] = kAll;
@@ -375,9 +377,9 @@ template <typename P, typename Rows> struct CodeFeed {
                     for (int i = 0; i < kCopies; ++i) in[j] |= f.seen.sees(k + i * kRowsPer + lane / kChunks) << i;
                 }
             }
-        } else {                                         // this lane's row
-            const int slot = a.by_page.of(key + lane);
-            row[0] = key + lane - slot * a.cache.page_size;
+        } else {                                         // this lane's row (lanes past KT repeat)
+            const int slot = a.by_page.of(key + lane % KT);
+            row[0] = key + lane % KT - slot * a.cache.page_size;
             page[0] = own ? table[slot] : 0;
         }
     }
@@ -410,9 +412,9 @@ template <typename P, typename Rows> struct CodeFeed {
             const float *s;
             bool ok = own;
             if (a.run) {
-                bool known[2];
+                bool known[kRuns];
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
+                for (int j = 0; j < kRuns; ++j) {
                     known[j] = (unsigned)page[j] < (unsigned)a.cache.n_pages;
                     if (!known[j]) {
                         set_err(a.err, kErrPage);        // an unseen run has page 0
@@ -421,8 +423,9 @@ template <typename P, typename Rows> struct CodeFeed {
                     if (a.run == 2) copies<kRowsPer * kRow>(a, j, known[j]);
                     else copies<0>(a, j, known[j]);
                 }
-                ok = ok && (lane < kRunRows ? known[0] : known[1]);
-                const int p = lane < kRunRows ? page[0] : page[1], r = lane < kRunRows ? row[0] : row[1];
+                constexpr int last = kRuns - 1;
+                ok = ok && (lane < kRunRows ? known[0] : known[last]);
+                const int p = lane < kRunRows ? page[0] : page[last], r = lane < kRunRows ? row[0] : row[last];
                 s = scales + (p * a.page_scales + a.by_scale.of(r + lane % kRunRows));
             } else {
                 if ((unsigned)page[0] >= (unsigned)a.cache.n_pages) {
@@ -444,7 +447,7 @@ template <typename P, typename Rows> struct CodeFeed {
             // the rows' scales behind them, K's, then V's
             const uint32_t st = to + 2 * KT * kRow + 4 * lane;
             cp4(st, s, ok);
-            cp4(st + 4 * KT, s + (a.v_scales - a.k_scales), ok);
+            if (kRuns == 2) cp4(st + 4 * KT, s + (a.v_scales - a.k_scales), ok);
             place += kStep;
             if (place >= end) walk(a);
             look_up(a);
@@ -731,14 +734,20 @@ template <typename P, typename Rows> cudaError_t start_attend(typename P::Args a
         a.cluster = window_cluster(segments, cap, P::kWindowRows, P::kWindowCluster, ctas);
         whole = a.cluster > 0;
     }
-    if (whole)
-        return launch_cluster(paged_attend_kernel<P, true, Rows>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<P>(), a.cluster, s, a);
+    auto clusters = [&](auto tile) {
+        using C = decltype(tile);
+        return launch_cluster(paged_attend_kernel<C, true, Rows>, dim3((unsigned)segments * a.cluster), dim3(kPaThreads), attend_smem<C>(), a.cluster, s, a);
+    };
+    if (whole) return cap <= 2LL * kAttendUnit * a.cluster ? clusters(typename P::Short()) : clusters(P());
     const int grid = (int)(most < ctas ? most : ctas);
     return launch_k(paged_attend_kernel<P, false, Rows>, dim3(grid), dim3(kPaThreads), attend_smem<P>(), s, true, a);
 }
 template <typename P, typename Rows> cudaError_t prepare_attend() {
-    const cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<P, false, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
-    return e != cudaSuccess ? e : cudaFuncSetAttribute(paged_attend_kernel<P, true, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
+    using C = typename P::Short;
+    cudaError_t e = cudaFuncSetAttribute(paged_attend_kernel<P, false, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attend_kernel<P, true, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<P>());
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(paged_attend_kernel<C, true, Rows>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)attend_smem<C>());
+    return e;
 }
 
 }  // namespace

@@ -88,9 +88,9 @@ template <int FORMAT> __device__ __forceinline__ void code_values(uint32_t codes
 // are whole numbers, so that rescaling is exact.  The tensor cores drop bits below their
 // accumulator: each tile's O is added by the CUDA cores.
 enum HeadMode : int { kPacked = 0, kEight = 1, kSixteen = 2 };
-template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
+template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTile {
     using T = T_;
-    static constexpr int D = D_, KT = 32, NT = MODE == kSixteen ? 2 : 1;
+    static constexpr int D = D_, KT = KT_, NT = MODE == kSixteen ? 2 : 1;
     static constexpr int kRow = D, kStage = 2 * KT * kRow + 8 * KT;   // bytes
     static constexpr bool kScaled = true;
     using Args = CodeAttendArgs;
@@ -102,7 +102,11 @@ template <typename T_, int D_, int MODE, int FORMAT> struct CodeTile {
     // a segment's end costs what two blocks of 8-bit rows do: 16 sequences of 1 to 8192 rows
     // with 1, 2 and 3 units 40.3, 34.0 and 33.4 us
     static constexpr int kCost = 2;
-    static constexpr int kCtas = MODE == kSixteen || kQ == 3 ? 2 : 3, kStages = (D == 128 ? 2 : 4) + (kCtas == 2 ? 1 : 0);
+    static constexpr int kCtas = MODE == kSixteen || kQ == 3 ? 2 : 3, kStages = (D == 128 ? 2 : 4) * 32 / KT + (kCtas == 2 ? 1 : 0);
+    // where a cluster's CTAs have few rows (see start_attend), tiles of 16 spread them over the
+    // warps: 8 KV heads of 100, 512, 1000 and 2000 rows 5.5, 6.0, 6.4 and 7.9 us in tiles of
+    // 32, 5.0, 5.6, 6.4 and 8.1 in tiles of 16 (sixteen heads' sums need a stage of 32)
+    using Short = CodeTile<T, D, MODE, FORMAT, MODE == kSixteen ? 32 : 16>;
     static constexpr int kClusterRows = (MODE == kSixteen ? 1024 : 512) * 128 / D;   // see attend_cluster
     static constexpr int kWindowRows = kClusterRows * 5 / 4, kWindowCluster = 2;     // see window_cluster
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a

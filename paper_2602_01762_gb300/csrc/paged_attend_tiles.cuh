@@ -28,6 +28,7 @@ template <int D_, int MODE> struct Bf16Tile {
     static constexpr int kRow = 2 * D, kStage = kPaStage;   // bytes
     static constexpr bool kScaled = false;
     using Args = AttendArgs;
+    using Short = Bf16Tile;
     static constexpr int kCtas = 2, kCost = 1;
     static constexpr int kHeads = MODE == kPacked ? 4 : 8 * NT;
     static constexpr int kParts = MODE == kPacked ? 2 : 3;   // products of P and V
@@ -210,6 +211,7 @@ template <int D_> struct F32Tile {
     static constexpr int kRow = 4 * D, kStage = kPaStage;   // bytes
     static constexpr bool kScaled = false;
     using Args = AttendArgs;
+    using Short = F32Tile;
     static constexpr int kCtas = 2, kCost = 1;
     static constexpr int kHeads = 4;
     static constexpr int kMergeStride = D + 4;
@@ -346,6 +348,7 @@ template <int D_, int NT> struct F32Mma {
     static constexpr int kRow = 4 * D, kStage = kPaStage;   // bytes
     static constexpr bool kScaled = false;
     using Args = AttendArgs;
+    using Short = F32Mma;
     static constexpr int kCtas = 2, kCost = 1;
     static constexpr int kHeads = 8 * NT;
     static constexpr int kMergeStride = D + 4;
