@@ -135,7 +135,23 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
         cp_group();
     };
     int w = w0 + team;
+    // new row i's angles, held to the table; of a tile's first kScAngles rows they are kept
+    auto position = [&](int i) {
+        const long long at = (long long)pos + i;
+        if (at >= 0 && at < a.rope_len) return (int)at;
+        set_err(a.err, kErrPosition);
+        return at < 0 ? 0 : a.rope_len - 1;
+    };
+    const uint32_t angles_at = (uint32_t)__cvta_generic_to_shared(angles);
+    if (KEYS && fits) {
+        const int count = min(a.per > 1 ? kRows : a.scale_rows, kScAngles);
+        for (int e = threadIdx.x; e < count * (D / 4); e += kScThreads) {
+            const int i = tile_first + e / (D / 4) - len;
+            if (i >= 0 && i < n) cp16(angles_at + 16 * e, a.rope + (long long)position(i) * D + 4 * (e % (D / 4)), true);
+        }
+    }
     fetch(w, 0);
+    fetch(w + teams, 1);
     int page = 0, row = 0;
     bool live = j_new < j_end;
     if (live) {
@@ -159,25 +175,13 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
     if (!live) mine = 0;
     float *const scale_at = scales + (long long)page * a.Hkv * a.scale_blocks + a.by_scale.of(row);
     float before = live && j_new > 0 && w < w1 ? scale_at[(long long)w * a.scale_blocks] : 0.f;
-    // the rows' angles, of a tile's first kScAngles rows
-    auto position = [&](int i) {                         // of new row i, held to the table
-        const long long at = (long long)pos + i;
-        if (at >= 0 && at < a.rope_len) return (int)at;
-        set_err(a.err, kErrPosition);
-        return at < 0 ? 0 : a.rope_len - 1;
-    };
     Gain<T, D> gain;
     const bool norm = a.g_k != nullptr;
     if (KEYS) {
         if (norm) gain.load(a.g_k);
-        const int count = min(a.per > 1 ? kRows : a.scale_rows, kScAngles);
-        for (int e = threadIdx.x; e < count * (D / 4); e += kScThreads) {
-            const int i = tile_first + e / (D / 4) - len;
-            if (i >= 0 && i < n) *(float4 *)(angles + 4 * e) = __ldg((const float4 *)(a.rope + (long long)position(i) * D) + e % (D / 4));
-        }
-        __syncthreads();
+        cp_wait_group<1>();
+        __syncthreads();                                 // the angles are there
     }
-    const uint32_t angles_at = (uint32_t)__cvta_generic_to_shared(angles);
     // Row j's values from what was read of it, before the norm's factor, which is returned.
     // The gain times a bf16 value is exact, and the factor meets a sum that is already
     // turned: two roundings fewer than in the order of the formula, and as many products.
@@ -255,7 +259,6 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
     const long long page_at = page * a.cache.page_stride + row * a.cache.row_stride;
     for (int turn = 0; w < w1; w += teams, turn ^= 1) {
         const float was = before;
-        fetch(w + teams, turn ^ 1);
         if (w + teams < w1) before = live && j_new > 0 ? scale_at[(long long)(w + teams) * a.scale_blocks] : 0.f;
         cp_wait_group<1>();
         F2 x[kScKeep][N], y[kScKeep][N];
@@ -267,6 +270,7 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
                 factor[c] = values(c * step + j0, mine >> c & 1, lds16(at), lds16(at + 512), x[c], y[c]);
                 if (mine >> c & 1) top = magnitude(x[c], y[c], factor[c], top);
             }
+        fetch(w + 2 * teams, turn);                      // what was read makes room
         further(w, [&](int, const F2 (&u)[N], const F2 (&v)[N], float f) { top = magnitude(u, v, f, top); });
         // over the block's lanes, then the team's warps; of a block with a NaN or an infinity
         // the largest finite value, with the sign bit for a mark
