@@ -91,9 +91,9 @@ struct StoreCodesArgs {
     const float *rope;
     const int32_t *pos, *n_new;
     int rope_len, B, max_new, Hkv;
-    // see store_codes_kernel: tiles of a sequence, heads of a CTA, its CTAs of keys and as many
-    // of values to a tile, CTAs, and of how many CTAs one is theirs
-    int team, per, tasks, span, splits, ctas, every;
+    // see store_codes_kernel: tiles of a CTA, such runs of a sequence, heads of a CTA, its CTAs
+    // of keys and as many of values to a run, CTAs, and of how many CTAs one is theirs
+    int team, per, keep, chain, tasks, span, splits, ctas, every;
     int beside;                          // the queries' kernel was launched before this one
     Divisor by_tasks, by_tiles, by_every, by_scale, by_page;   // by tasks, B tasks, every, scale_rows, page_size
     float eps;
@@ -146,6 +146,10 @@ cudaError_t launch_norm_rope(const NormRopeArgs &a, bool bf16, int D, bool appen
 int norm_rope_grad_ctas(int sms);
 cudaError_t launch_norm_rope_grad(const NormRopeGradArgs &a, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t prepare_store_codes_kernels(bool bf16, int D);
+cudaError_t prepare_e4m3_store(bool bf16, int D);
+cudaError_t prepare_int8_store(bool bf16, int D);
+cudaError_t start_e4m3_store(const NormRopeArgs &q, const StoreCodesArgs &a, bool bf16, int D, unsigned ctas, size_t shared, cudaStream_t s);
+cudaError_t start_int8_store(const NormRopeArgs &q, const StoreCodesArgs &a, bool bf16, int D, unsigned ctas, size_t shared, cudaStream_t s);
 // Norm and rotation of the queries, and their keys and values into the cache.
 cudaError_t launch_store_codes(const NormRopeArgs &q, const StoreCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);
 cudaError_t launch_read_codes(const ReadCodesArgs &a, CodeFormat format, bool bf16, int D, int sms, cudaStream_t s);

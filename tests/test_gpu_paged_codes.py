@@ -258,6 +258,43 @@ def test_append_is_exact(pkg, fmt, dtype, D, page, r):
         h.close()
 
 
+@pytest.mark.parametrize("dtype,D,Hkv,page,r", [("bf16", 128, 1, 16, 16), ("bf16", 64, 1, 32, 32), ("bf16", 128, 5, 16, 8), ("f32", 64, 2, 32, 32),
+                                                ("bf16", 128, 1, 16, 1), ("f32", 128, 3, 16, 2), ("bf16", 64, 1, 24, 3), ("bf16", 128, 1, 16, 4)])
+def test_append_of_many_tiles(pkg, dtype, D, Hkv, page, r):
+    """Prompts of more tiles than run at once, of which a CTA takes several: bit for bit, with lengths
+    that end a sequence in its first tile, in the middle of a CTA's run of them and at its end."""
+    n = 600 * r if r > 4 else 2048
+    counts = [n, 3 * r + 1, 0, n - r, n - 2 * r - 1, 1, n - 5, n // 2]
+    lens = [0, 1, 5, r - 1, 2 * r, 7, page, 3]
+    h, cache, q, k, v, q_out, n_new = append_case(pkg, D=D, dtype=dtype, fmt="int8", page=page, r=r, lens=lens, counts=counts, Hq=Hkv, Hkv=Hkv, seed=r)
+    want = [stored(cache, name, lens, x, counts, "int8") for name, x in (("k", k), ("v", v))]
+    h.append(cache, q, k, v, q_out, identity_rope(n + 2 * page, D), n_new=n_new)
+    assert h.status() == 0
+    for (codes, scales), name in zip(want, "kv"):
+        assert torch.equal(getattr(cache, name + "_scales").cpu().double(), scales), name
+        assert torch.equal(ref.codes_of(getattr(cache, name + "_pages")), codes), name
+    for b, c in enumerate(counts):
+        assert torch.equal(q_out[b, :c], q[b, :c]) and (q_out[b, c:] == 0).all()
+    h.close()
+
+
+@pytest.mark.parametrize("fmt", ["e4m3", "int8"])
+@pytest.mark.parametrize("dtype,D", [("bf16", 128), ("f32", 64)])
+@pytest.mark.parametrize("page,r", [(16, 16), (24, 24), (64, 64), (100, 100), (128, 64)])
+def test_append_one_token_anywhere_in_a_block(pkg, fmt, dtype, D, page, r):
+    """A token behind 0 to r - 1 rows of its block: bit for bit, the earlier rows' codes too."""
+    lens = list(range(0, 2 * r, max(r // 13, 1)))
+    counts = [b % 7 > 0 for b in range(len(lens))]
+    h, cache, q, k, v, q_out, n_new = append_case(pkg, D=D, dtype=dtype, fmt=fmt, page=page, r=r, lens=lens, counts=[int(c) for c in counts], Hq=4, Hkv=2, seed=r)
+    want = [stored(cache, name, lens, x, [int(c) for c in counts], fmt) for name, x in (("k", k), ("v", v))]
+    h.append(cache, q, k, v, q_out, identity_rope(2 * r + 2, D), n_new=n_new)
+    assert h.status() == 0
+    for (codes, scales), name in zip(want, "kv"):
+        assert torch.equal(getattr(cache, name + "_scales").cpu().double(), scales), name
+        assert torch.equal(ref.codes_of(getattr(cache, name + "_pages")), codes), name
+    h.close()
+
+
 @pytest.mark.parametrize("fmt", ["e4m3", "int8"])
 @pytest.mark.parametrize("layout", ["rows_first", "interleaved"])
 def test_append_to_other_layouts_token_by_token(pkg, fmt, layout):
