@@ -101,6 +101,8 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
     using R = Rope<T, D>;
     constexpr int N = R::N, E = R::E, kRows = R::kHeads;   // rows a warp has at a time
     constexpr int kStage = kScStage<KEEP>, kRing = kScRing<KEEP>;
+    // the warps' maxima, of two turns: what a warp writes in one, its team has read before
+    // the barrier of the turn between
     __shared__ float tops[2][kScThreads / 32];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane % R::kLanes, group = lane / R::kLanes;
     const int team = warp / a.team, teams = kScThreads / 32 / a.team, in_team = warp - team * a.team;
@@ -267,6 +269,7 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
                 if (in) f(j, u, v, factor);
             }
     };
+    auto team_barrier = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * a.team) : "memory"); };
     const int width = a.per > 1 ? R::kLanes * a.scale_rows : 32;   // lanes of a block
     const int thread = a.per > 1 ? lane % width : in_team * 32 + lane, threads = a.per > 1 ? width : 32 * a.team;
     int page = 0, row = 0, item = items, tile = t0 - 1;
@@ -297,7 +300,8 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
                 if (angles == angles_at + 3 * angle_bytes) angles = angles_at;
             }
         }
-        if (w >= w1) {
+        if (w >= w1) {                                   // a team without a head passes its barrier too: see tops
+            if (KEEP == 4 && a.team > 1) team_barrier();
             fetch(turn);
             continue;
         }
@@ -332,7 +336,7 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
         if (odd) top = -top;
         if (KEEP == 4 && a.team > 1) {
             if (lane == 0) tops[turn][warp] = top;
-            asm volatile("bar.sync %0, %1;" ::"r"(1 + team), "r"(32 * a.team) : "memory");
+            team_barrier();
             uint32_t mark = 0;
             float most = 0.f;
             for (int i = 0; i < a.team; ++i) {
