@@ -84,9 +84,10 @@ template <int FORMAT> __device__ __forceinline__ void code_values(uint32_t codes
 // it.  With up to four heads two parts share a product, in columns 0 to 3 and 4 to 7.
 //
 // Two running maxima, of the scores (for the sum of probabilities) and of the scores
-// with log2 s^V (for W, so that it stays in fp16's range whatever the scales are); both
-// are whole numbers, so that rescaling is exact.  The tensor cores drop bits below their
-// accumulator: each tile's O is added by the CUDA cores.
+// with log2 s^V (for W, so that it stays in fp16's range whatever the scales are; kept
+// as its distance from the first, in which log2 s^V is not lost beside a score of 2^24
+// or more); both are whole numbers, so that rescaling is exact.  The tensor cores
+// drop bits below their accumulator: each tile's O is added by the CUDA cores.
 enum HeadMode : int { kPacked = 0, kEight = 1, kSixteen = 2 };
 template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTile {
     using T = T_;
@@ -112,9 +113,11 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
     // p s^V over its base stays below 2^2, one for each of the slack and log2 s cut to a
     // whole number: W up to 2^15 leaves the most below.
     static constexpr float kSlackW = 1.f, kLift = 8192.f;
+    // The maximum of no score: scores of -inf are still -inf over it, so that none needs another base.
+    static constexpr float kLowest = -3.402823466e38f;
     uint32_t qf[D / 16][kQ][NT][2];
     float qs[NT][2];                                     // scale of the scores over q's power of two
-    float m[NT][2], n[NT][2], l[NT][2], f[NT][2];        // f: W over p s^V
+    float m[NT][2], n[NT][2], l[NT][2], f[NT][2];        // n: of the scores with log2 s^V, over m; f: W over p s^V
     F2 o[D / 16][NT][2];                                 // two dims of a head pair
 
     // Shared address of 16-byte piece c of row r: the eight lanes of a load (two rows of
@@ -181,8 +184,8 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
         for (int t = 0; t < NT; ++t) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                m[t][i] = n[t][i] = -INFINITY;
-                l[t][i] = 0.f;
+                m[t][i] = kLowest;
+                n[t][i] = l[t][i] = 0.f;
                 f[t][i] = kLift;
             }
 #pragma unroll
@@ -241,6 +244,7 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
             const float e0 = whole_log2(v0), e1 = whole_log2(v1);
             const bool all = seen.sees_all(base, 16);
             const bool in0 = all || seen.sees(base + g), in1 = all || seen.sees(base + g + 8);
+            float over[NT][4];                           // scores over the maximum
             bool grew = false;
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
@@ -254,7 +258,9 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
                 for (int i = 0; i < 2; ++i) {
                     if (!in0) s[t][i] = -INFINITY;
                     if (!in1) s[t][2 + i] = -INFINITY;
-                    grew |= fmaxf(s[t][i], s[t][2 + i]) > m[t][i] + kSlack || fmaxf(s[t][i] + e0, s[t][2 + i] + e1) > n[t][i] + kSlackW;
+                    over[t][i] = s[t][i] - m[t][i];
+                    over[t][2 + i] = s[t][2 + i] - m[t][i];
+                    grew |= fmaxf(s[t][i], s[t][2 + i]) > m[t][i] + kSlack || fmaxf(over[t][i] + e0, over[t][2 + i] + e1) > n[t][i] + kSlackW;
                 }
             }
             if (__any_sync(0xFFFFFFFFu, grew)) {
@@ -263,20 +269,26 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
                     float a[2];
 #pragma unroll
                     for (int i = 0; i < 2; ++i) {
-                        float z = fmaxf(s[t][i], s[t][2 + i]), y = fmaxf(s[t][i] + e0, s[t][2 + i] + e1);
+                        // the largest score, and the largest with log2 s^V over it
+                        float top = fmaxf(fmaxf(s[t][i], s[t][2 + i]), kLowest), y = fmaxf(s[t][i] - top + e0, s[t][2 + i] - top + e1);
 #pragma unroll
                         for (int x = 4; x < 32; x <<= 1) {
-                            z = fmaxf(z, __shfl_xor_sync(0xFFFFFFFFu, z, x));
-                            y = fmaxf(y, __shfl_xor_sync(0xFFFFFFFFu, y, x));
+                            const float o_top = __shfl_xor_sync(0xFFFFFFFFu, top, x), o_y = __shfl_xor_sync(0xFFFFFFFFu, y, x);
+                            const float most = fmaxf(top, o_top);
+                            y = fmaxf(y + (top - most), o_y + (o_top - most));
+                            top = most;
                         }
-                        z = fmaxf(m[t][i], ceilf(z));
+                        const float level = fmaxf(m[t][i], ceilf(top)), down = m[t][i] - level;
+                        y = ceilf(y + (top - level));
+                        m[t][i] = level;
+                        over[t][i] = s[t][i] - level;
+                        over[t][2 + i] = s[t][2 + i] - level;
                         // no further below than p f's range (scales below 2^-106 lose bits of W)
-                        y = fmaxf(fmaxf(n[t][i], ceilf(y)), z - 106.f);
-                        l[t][i] *= exp2f(m[t][i] - base_of(z));
-                        a[i] = exp2f(n[t][i] - base_of(y));
-                        m[t][i] = z;
+                        y = fmaxf(fmaxf(n[t][i] + down, y), -106.f);
+                        l[t][i] *= exp2f(down);
+                        a[i] = exp2f(n[t][i] + down - y);
                         n[t][i] = y;
-                        f[t][i] = exp2f(base_of(z) - base_of(y)) * kLift;
+                        f[t][i] = exp2f(-y) * kLift;
                     }
                     const F2 both = f2(a[0], a[1]);
 #pragma unroll
@@ -289,10 +301,9 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
             uint32_t part[kParts][NT][2];
 #pragma unroll
             for (int t = 0; t < NT; ++t) {
-                const float b0 = base_of(m[t][0]), b1 = base_of(m[t][1]);
 #pragma unroll
                 for (int u = 0; u < 2; ++u) {
-                    const float p0 = power2(s[t][2 * u] - b0), p1 = power2(s[t][2 * u + 1] - b1), v = u ? v1 : v0;
+                    const float p0 = power2(over[t][2 * u]), p1 = power2(over[t][2 * u + 1]), v = u ? v1 : v0;
                     l[t][0] += p0;
                     l[t][1] += p1;
                     uint32_t x, y, z;
@@ -340,10 +351,10 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
                 v += __shfl_xor_sync(0xFFFFFFFFu, v, 8);
                 v += __shfl_xor_sync(0xFFFFFFFFu, v, 16);
                 if (g == 0 && 8 * t + c + i < kHeads) {
-                    sm[8 * t + c + i] = m[t][i];
+                    sm[8 * t + c + i] = v == 0.f ? -INFINITY : m[t][i];
                     sl[8 * t + c + i] = v;
                 }
-                back[i] = m[t][i] == -INFINITY ? 0.f : exp2f(n[t][i] - m[t][i]) / kLift;
+                back[i] = exp2f(n[t][i]) / kLift;
             }
 #pragma unroll
             for (int d = 0; d < D / 16; ++d) {
