@@ -113,7 +113,7 @@ cudaError_t launch_store_codes(const NormRopeArgs &queries, const StoreCodesArgs
     // one launch where all of it runs at once, else the queries' rows on a kernel that takes
     // less of an SM.  Measured, 32 query and 8 KV heads: 16 rows 3.3 and 3.9 us (and 2 us of a
     // launch), 8 prompts of 1021 to 2048 rows 59 and 56 us.
-    a.beside = a.ctas + (long long)others > wave;
+    a.beside = a.ctas + (long long)others > wave || !q.one_row;   // that launch takes a row a warp
     if (a.beside) {
         const cudaError_t e = launch_norm_rope(queries, bf16, D, false, sms, s);
         if (e != cudaSuccess) return e;

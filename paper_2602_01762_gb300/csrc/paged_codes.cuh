@@ -423,7 +423,7 @@ __device__ __forceinline__ void store_tile(const StoreCodesArgs &a, int run, int
 // one, which lets it start once its own wait is over: rows, lengths and cache are final
 // then, the two run side by side, and the wait at the end makes this one's end the end of
 // both.
-template <typename T, int D, int FORMAT, int KEEP, bool ROWS>
+template <typename T, int D, int FORMAT, int KEEP>
 __global__ void __launch_bounds__(kScThreads, kScCtas<KEEP>) store_codes_kernel(NormRopeArgs q, StoreCodesArgs a) {
     extern __shared__ __align__(16) unsigned char dyn[];
     if (!a.beside) pdl_wait();
@@ -434,7 +434,7 @@ __global__ void __launch_bounds__(kScThreads, kScCtas<KEEP>) store_codes_kernel(
         if (y < a.splits) store_tile<T, D, FORMAT, KEEP, true>(a, run, y * a.span, a.k, a.cache.k, a.k_scales, dyn);
         else store_tile<T, D, FORMAT, KEEP, false>(a, run, (y - a.splits) * a.span, a.v, a.cache.v, a.v_scales, dyn);
     } else {
-        norm_rope_rows<T, D, false, ROWS>(q, (unsigned)(i - min(turn + 1, a.ctas)), dyn);
+        norm_rope_rows<T, D, false, false>(q, (unsigned)(i - min(turn + 1, a.ctas)), dyn);
     }
     if (a.beside) pdl_wait();
 }
@@ -447,16 +447,14 @@ template <typename F> cudaError_t with_rows(bool bf16, int D, const F &f) {
 }
 template <int FORMAT> cudaError_t prepare_store(bool bf16, int D) {
     return with_rows(bf16, D, [&](auto t, auto d) {
-        cudaError_t e = cudaFuncSetAttribute(store_codes_kernel<decltype(t), d, FORMAT, 4, false>, cudaFuncAttributeMaxDynamicSharedMemorySize, kScShared);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(store_codes_kernel<decltype(t), d, FORMAT, 4, true>, cudaFuncAttributeMaxDynamicSharedMemorySize, kScShared);
-        return e;
+        return cudaFuncSetAttribute(store_codes_kernel<decltype(t), d, FORMAT, 4>, cudaFuncAttributeMaxDynamicSharedMemorySize, kScShared);
     });
 }
 template <int FORMAT> cudaError_t start_store(const NormRopeArgs &q, const StoreCodesArgs &a, bool bf16, int D, unsigned ctas, size_t shared, cudaStream_t s) {
     return with_rows(bf16, D, [&](auto t, auto d) {
         using T = decltype(t);
         auto go = [&](auto k) {
-            return launch_k(q.one_row ? store_codes_kernel<T, d, FORMAT, k, false> : store_codes_kernel<T, d, FORMAT, k, true>, dim3(ctas), dim3(kScThreads), shared, s, true, q, a);
+            return launch_k(store_codes_kernel<T, d, FORMAT, k>, dim3(ctas), dim3(kScThreads), shared, s, true, q, a);
         };
         return a.keep == 4 ? go(std::integral_constant<int, 4>()) : a.keep == 2 ? go(std::integral_constant<int, 2>()) : go(std::integral_constant<int, 1>());
     });
