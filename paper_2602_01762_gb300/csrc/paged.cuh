@@ -81,7 +81,7 @@ struct CodeAttendArgs : AttendArgs {
     int short_page, short_row, page_scales;   // then: page_stride, row_stride, scales of a page
 };
 
-// Rows quantised into a cache of codes; the first and last row of a cache read back.
+// Rows quantised into a cache of codes.
 struct StoreCodesArgs {
     HeadsView k, v;
     PagedView cache;
@@ -100,6 +100,7 @@ struct StoreCodesArgs {
     int *err;
 };
 
+// Rows of such a cache read back.
 struct ReadCodesArgs {
     HeadsView k_out, v_out;
     PagedView cache;
@@ -119,7 +120,7 @@ struct EvictArgs {
     int *err;
 };
 
-constexpr int kAttendCost = 1;           // units that a segment costs beside its keys, at least
+constexpr int kAttendMaxCost = 2;        // units that a segment costs beside its keys, at most (see P::kCost)
 // Query heads that share a pass over the rows; the most passes over a KV head's rows
 // that its G query heads take.
 inline int attend_head_tile(int G) { return G <= 4 ? 4 : G <= 8 ? 8 : 16; }

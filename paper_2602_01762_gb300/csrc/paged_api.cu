@@ -175,9 +175,11 @@ prism_status prism_paged_create(const prism_paged_config *cfg, int32_t device, p
     if (!(c.softmax_scale >= 0.f) || std::isinf(c.softmax_scale) || !(c.rms_eps >= 0.f) || std::isinf(c.rms_eps))
         return fail(nullptr, PRISM_ERR_INVALID_ARG, "softmax_scale and rms_eps must be finite and not negative");
     const long long rows = (long long)c.max_pages * c.page_size;
-    // work units and row numbers are 32-bit
+    // work units and row numbers are 32-bit: 2^30 units where each segment costs one, and with at least 64 units to a
+    // segment there (no more than 2^24 of them) below 2^31 where it costs two
+    static_assert(kAttendMaxCost <= 32, "units of a handle's largest call");
     if (rows > (1LL << 30) || (long long)c.max_batch * c.n_q_heads > (1LL << 24) ||
-        (long long)c.max_batch * c.n_q_heads * (rows / kAttendUnit + 1 + kAttendCost) > (1LL << 30))
+        (long long)c.max_batch * c.n_q_heads * (rows / kAttendUnit + 2) > (1LL << 30))
         return fail(nullptr, PRISM_ERR_CAPACITY, "max_batch * n_q_heads * max_pages * page_size is too large");
 
     prism_paged *p = new (std::nothrow) prism_paged;

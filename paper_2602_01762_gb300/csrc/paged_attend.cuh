@@ -724,6 +724,7 @@ inline int window_cluster(long long segments, long long cap, int rows, int most,
 
 // ht: heads of a tile.
 template <typename P, typename Rows> cudaError_t start_attend(typename P::Args a, int ht, int sms, cudaStream_t s) {
+    static_assert(P::kCost <= kAttendMaxCost, "units are counted when a handle is made");
     const int G = a.Hq / a.Hkv;
     const long long cap = attend_rows(a), segments = a.B * (long long)a.Hkv * ((G + ht - 1) / ht);
     const long long most = segments * (P::kCost + (cap + kAttendUnit - 1) / kAttendUnit);
