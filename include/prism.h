@@ -609,7 +609,8 @@ prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, 
  * window and a few first rows that stay visible.  Rows that are not seen are not
  * read, their weights stay as they are, and the block-table entries of pages without
  * a seen row are not read: those pages may belong to another sequence.  No seen row
- * gives zeros and -inf.  Errors: as prism_paged_attend. */
+ * gives zeros and -inf.  The cost goes by the rows that are seen; with weights a second
+ * kernel still counts through all rows.  Errors: as prism_paged_attend. */
 prism_status prism_paged_attend_window(prism_paged *p, const prism_paged_cache *cache, int32_t added, int32_t window, int32_t sinks,
                                        const void *q, void *out, float *lse, void *stream);
 
@@ -640,7 +641,12 @@ typedef struct {
  * step of it.  A block whose first row is new starts afresh.  NaN and infinities do
  * not count for the scale: in e4m3 they are stored as NaN, in int8, which has no code
  * for them, they make the scale, and so the block's rows, NaN until it starts afresh.
- * Blocks that receive rows belong to one sequence.  Errors: as prism_paged_append. */
+ * Rows that are taken back (kv_len lowered over them) leave their block the scale that
+ * they gave it, and the kept rows their codes in that scale, until a row goes to the
+ * block's first slot again: a rejected row that is larger than the kept ones costs them
+ * bits, and one with a NaN or an infinity in int8 the whole block.
+ * Blocks that receive rows belong to one sequence.  Errors: as prism_paged_append, and
+ * CAPACITY where batch * (max_new / scale_rows + 2) * Hkv exceeds 2^28. */
 prism_status prism_paged_append_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales,
                                       const prism_rows *rows, void *stream);
 
@@ -658,8 +664,9 @@ prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cac
                                     const prism_heads *v_out, void *stream);
 
 /* prism_paged_attend_window over such a cache.  Codes enter their products exactly,
- * the scales outside of them in fp32; queries keep their bits, probabilities times V's
- * scale 24 in fp32 and 22 in bf16 (three and two fp16 parts), sums 24.  A key that is
+ * the scales outside of them in fp32; queries keep their bits (dims below 2^-31 of their
+ * head's largest fewer), probabilities times V's scale 24 in fp32 and 22 in bf16 (three
+ * and two fp16 parts), sums 24.  A key that is
  * NaN makes its KV head's results NaN; a value, that dim of them.  Errors: as
  * prism_paged_attend. */
 prism_status prism_paged_attend_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales, int32_t added,
