@@ -11,8 +11,8 @@
 // Measured, D = 128, bf16 queries: e4m3, 64 sequences of 6001 to 16384 rows, G = 8, 233 us
 // (6.3 TB/s); one of 131071, G = 4, 50 us (5.4, of which 39 us are the bytes and the rest
 // its start and joins); int8 with a scale a row, 16 sequences of 1 to 8192 rows, 34 us
-// (4.1); 517 rows 6.2 us. A tile of 16 rows takes 377 instructions a warp with e4m3 (a
-// pair of codes is one conversion) and 483 with int8; three CTAs an SM give the warps that
+// (4.1); 517 rows 6.2 us. A tile of 16 rows takes 362 instructions a warp with e4m3 (a
+// pair of codes is one conversion) and 469 with int8; three CTAs an SM give the warps that
 // hide them (two: 276 us for the first case; four, of 128 registers: 298).
 #pragma once
 
@@ -100,8 +100,9 @@ template <typename T_, int D_, int MODE, int FORMAT, int KT_ = 32> struct CodeTi
     static constexpr int kParts = (sizeof(T) == 2 ? 2 : 3) - (MODE == kPacked ? 1 : 0);   // products of V and W
     static_assert(sizeof(T) == 2 || MODE != kSixteen, "fp32 queries go eight heads at a time: sixteen take 96 registers");
     static constexpr int kMergeStride = D + 4;
-    // a segment's end costs what two blocks of 8-bit rows do: 16 sequences of 1 to 8192 rows
-    // with 1, 2 and 3 units 40.3, 34.0 and 33.4 us
+    // a segment's end costs what two blocks of 8-bit rows do, or three: with 1, 2 and 3 units 16
+    // sequences of 1 to 8192 int8 rows 36.5, 34.3 and 33.2 us, 64 of 1 to 2048 43.9, 37.5 and 36.6,
+    // 64 of 6001 to 16384 e4m3 rows 232.6, 231.5 and 231.0, 64 with a window of 4096 97.2, 95.7 and 96.1
     static constexpr int kCost = 2;
     static constexpr int kCtas = MODE == kSixteen || kQ == 3 ? 2 : 3, kStages = (D == 128 ? 2 : 4) * 32 / KT + (kCtas == 2 ? 1 : 0);
     // where a cluster's CTAs have few rows (see start_attend), tiles of 16 spread them over the

@@ -3,9 +3,12 @@
 // Row j of L is seen where j < sinks or j >= L - window.  The blocks of 64 rows without
 // a seen row are not part of the work that is split, so that the cost goes by the
 // window, not by the sequence: rows that are not seen are not read, and neither are the
-// block-table entries of pages without a seen row, whose pages can be given back.
+// block-table entries of pages without a seen row, whose pages can be given back.  The
+// weights of a cache that has them are another kernel's, which still counts through all
+// blocks of the sequences and passes over those that are not seen.
 // Measured, 16 sequences of 1000 to 65536 rows, 8 KV heads of 128 and 4 query heads each,
-// a window of 1024 and 4 sinks, bf16: 15.7 us (67 MB, 4.3 TB/s; 4.6 us to the first rows).
+// a window of 1024 and 4 sinks, bf16: 15.7 us (67 MB, 4.3 TB/s; 4.6 us to the first rows);
+// with weights 12 us more, 13 where every sequence has 65536 rows.
 #include "paged_attend_tiles.cuh"
 
 namespace prism {
