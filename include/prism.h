@@ -600,7 +600,8 @@ prism_status prism_paged_append(prism_paged *p, const prism_paged_cache *cache, 
  * does not depend on the order in which CTAs run.  A score of -inf drops its row, NaN
  * or +inf makes its head NaN, and with it the weights of the sequence's rows of that
  * KV head, for good (no error bit tells); an infinite value in V makes that dim of its
- * KV head's outputs infinite or NaN.  Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
+ * KV head's outputs infinite or NaN, as do finite ones whose sum, weighted by up to 2^8
+ * before it is divided, leaves fp32's range.  Errors: INVALID_ARG, SHAPE, CAPACITY, CUDA. */
 prism_status prism_paged_attend(prism_paged *p, const prism_paged_cache *cache, int32_t added, const void *q, void *out,
                                 float *lse, void *stream);
 
@@ -652,7 +653,7 @@ prism_status prism_paged_append_codes(prism_paged *p, const prism_paged_cache *c
 
 /* Rows of such a cache read back: row start[b] + i, i < n_rows[b], of sequence b goes
  * to row i of k_out and v_out, wtype [batch, max_rows, Hkv, D] (code times scale,
- * rounded once); rows past n_rows[b] are left as they are.  Rows beyond kv_len are
+ * rounded once; infinite where a magnitude of 1.9 2^127 or more was rounded up to 2^128); rows past n_rows[b] are left as they are.  Rows beyond kv_len are
  * read as any other.  A row outside the block table is written as zeros (cache bit),
  * as is one of a page outside the pool.
  *   start    int32 [batch], or NULL: 0
@@ -667,8 +668,8 @@ prism_status prism_paged_read_codes(prism_paged *p, const prism_paged_cache *cac
  * the scales outside of them in fp32; queries keep their bits (dims below 2^-31 of their
  * head's largest fewer), probabilities times V's scale 24 in fp32 and 22 in bf16 (three
  * and two fp16 parts), sums 24.  A key that is
- * NaN makes its KV head's results NaN; a value, that dim of them.  Errors: as
- * prism_paged_attend. */
+ * NaN makes its KV head's results NaN; a value, that dim of them; infinite scores and
+ * values as in prism_paged_attend.  Errors: as prism_paged_attend. */
 prism_status prism_paged_attend_codes(prism_paged *p, const prism_paged_cache *cache, const prism_paged_scales *scales, int32_t added,
                                       int32_t window, int32_t sinks, const void *q, void *out, float *lse, void *stream);
 

@@ -74,3 +74,47 @@ def test_scores_that_grow_by_more_than_they_hold(size):
                 want = float(vs[top]) * top
                 # scores differ by `size` at least: exp(-2^10) is 0
                 assert float((out.double() - want).abs().max()) <= (2.0 ** -8 if dtype == "bf16" else 2.0 ** -20) * want, (dtype, Hq, order)
+
+
+@pytest.mark.parametrize("rows", ["one", "some", "all"])
+def test_infinite_scores(rows):
+    """A score of -inf drops its row (all of them: zeros and -inf), one of +inf makes its head NaN and no other."""
+    import paper_2602_01762_gb300 as p
+    n, page, D, Hkv = 200, 16, 64, 2
+    cols = -(-n // page)
+    for dtype in DT:
+        for G, fmt in ((4, "int8"), (8, "e4m3"), (12, "int8")):
+            g = torch.Generator().manual_seed(G)
+            k = torch.randint(1, 13, (cols, Hkv, page, D), generator=g).float()
+            v = torch.randint(-12, 13, (cols, Hkv, page, D), generator=g).float()
+            ks, vs = (torch.exp2(torch.randint(-6, -3, (cols, Hkv, page), generator=g).float()) for _ in range(2))
+            slots = {"one": [37], "some": [0, 16, 17, 40, 99, 199], "all": list(range(n))}[rows]
+            at = [(s // page, s % page) for s in slots]
+            for c, r in at:
+                ks[c, 0, r] = float("inf")
+            q = torch.rand(2, Hkv * G, D, generator=g) + 0.5
+            q[0, :G] *= -1                                       # -inf where ks is infinite; the second sequence +inf
+            q = q.to(DT[dtype]).cuda()
+            h = p.PagedAttention(n_q_heads=Hkv * G, n_kv_heads=Hkv, head_dim=D, dtype=dtype, page_size=page, max_batch=2, max_pages=cols)
+            table = torch.arange(cols, dtype=torch.int32, device="cuda")[None].expand(2, -1).contiguous()
+            cache = h.cache(k.to(ref.TYPE[fmt]).cuda(), v.to(ref.TYPE[fmt]).cuda(), table, torch.full((2,), n, dtype=torch.int32, device="cuda"),
+                            k_scales=ks.cuda(), v_scales=vs.cuda())
+            out, lse = torch.empty_like(q), torch.empty(2, Hkv * G, device="cuda")
+            h.attend(cache, q, out, lse=lse, added=0)
+            assert h.status() == 0
+            h.close()
+            assert torch.isnan(out[1, :G]).all() and torch.isnan(lse[1, :G]).all()
+            x, y = (t.permute(1, 0, 2, 3).reshape(Hkv, -1, D)[:, :n] for t in (ref.values(k, ks), ref.values(v, vs)))
+            for b in range(2):
+                for head in range(Hkv):
+                    if b == 1 and head == 0:
+                        continue
+                    z = q[b, head * G:(head + 1) * G].cpu().double() @ x[head].T * D ** -0.5
+                    got, got_lse = out[b, head * G:(head + 1) * G].cpu().double(), lse[b, head * G:(head + 1) * G].cpu().double()
+                    if torch.isinf(z).all():
+                        assert (got == 0).all() and (got_lse == -float("inf")).all()
+                        continue
+                    w = torch.softmax(z, -1)
+                    # scores of at most 2^9, whose fp32 sums and scaling err by 2^-12 at most
+                    tol = 2.0 ** -10 * (w @ y[head].abs()) + (2.0 ** -8 * (w @ y[head]).abs() if dtype == "bf16" else 0.0)
+                    assert ((got - w @ y[head]).abs() <= tol).all() and ((got_lse - torch.logsumexp(z, -1)).abs() <= 2.0 ** -10).all()
